@@ -36,7 +36,8 @@
  *   enqueued: on error nothing is launched and no output is touched.
  *   Faults during kernel execution surface at the caller's next sync.
  * - Pointers must be 16-byte aligned and row strides multiples of 8
- *   elements (16 bytes), else BPC_EALIGN.
+ *   elements (16 bytes), else BPC_EALIGN (int32 and int64 arrays: their own
+ *   size).
  * - Calls share no mutable state except a thread-local error message (and,
  *   for bpc_decode_attention_noalloc, that GPU's static scratch), so they
  *   are reentrant; two calls that share an output or a workspace must not
@@ -483,6 +484,163 @@ int bpc_decode_attention_noalloc(const uint16_t* q,
                                  int32_t* score_out,
                                  uint32_t* qcode_out,
                                  void* stream);
+
+/*
+ * bpc_qk_norm_rope -- the queries and keys that the entry points above take,
+ * from the rows of a projection: per head an RMS norm, and the rotation by the
+ * token's position, in one pass.  For every row x [128] of q and of k:
+ *     y = x * rsqrt(mean(x^2) + eps) * w       (y = x without weights)
+ *     for each pair (i, j) of the first R coordinates, with the position p of
+ *     the row's token:  y_i' = y_i c - y_j s,  y_j' = y_j c + y_i s,
+ *     c = cos_sin[p][f], s = cos_sin[p][R/2 + f],
+ * where pair f is (f, f + R/2), or (2f, 2f + 1) with `interleaved`.  fp32
+ * throughout, rounded to bf16 once.
+ *
+ * q          [B, Hq, T, D] bf16, strides (sq_b, sq_h, sq_t); Hq = 0 (and NULL
+ *            pointers): no queries
+ * q_out      the same shape, strides (sqo_*): either q itself with q's
+ *            strides, or memory that overlaps none of the inputs
+ * wq         [Hq, D] bf16 norm weights, head stride sw_q (0 = one row of
+ *            weights for all heads), or NULL: no norm
+ * k, k_out, wk, Hkv  likewise (k_out may be the cache); Hq + Hkv >= 1
+ * eps        finite, >= 0
+ * cos_sin    [table_rows, R] fp32, contiguous: R/2 cosines, then R/2 sines of
+ *            each position
+ * R          0 (no rotation; pos and cos_sin unused) or a multiple of 16, at
+ *            most 128
+ * pos        [B, T] int32, stride sp_b (0 = shared).  The rows of a token whose
+ *            position is not in [0, table_rows) are not written.
+ * No workspace; one kernel launch.
+ */
+int bpc_qk_norm_rope(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
+                     uint16_t* q_out, int64_t sqo_b, int64_t sqo_h, int64_t sqo_t,
+                     const uint16_t* wq, int64_t sw_q,
+                     const uint16_t* k, int64_t sk_b, int64_t sk_h, int64_t sk_t,
+                     uint16_t* k_out, int64_t sko_b, int64_t sko_h, int64_t sko_t,
+                     const uint16_t* wk, int64_t sw_k,
+                     int B, int Hq, int Hkv, int T, int D,
+                     float eps,
+                     const float* cos_sin, int table_rows, int R, int interleaved,
+                     const int32_t* pos, int64_t sp_b,
+                     void* stream);
+
+/*
+ * bpc_append_kv_paged -- append of new tokens to a cache in pages, each
+ * sequence at a length of its own, with the norm and rotation of
+ * bpc_qk_norm_rope on the way.  For every sequence b and t < count[b], with
+ * slot = pos[b] + t:
+ *     K[table[b][slot / page_size]][h][slot % page_size] = rotated k_new[b][h][t]
+ *     V[...]                                             = v_new[b][h][t]
+ * A token whose slot lies in no page of the table, whose page is not in
+ * [0, num_pages), or whose rotation position is not in [0, table_rows) is not
+ * stored; nothing else in the pages is written.
+ *
+ * k_new, v_new [B, Hkv, T, D] bf16, strides as in bpc_append_kv
+ * K, V       [num_pages, Hkv, page_size, D] bf16 pools of pages, strides
+ *            (sK_p, sK_h, sK_n) and (sV_p, sV_h, sV_n).  A contiguous cache
+ *            [B, Hkv, Ncap, D] is one of B pages.
+ * block_table [B, max_pages] int32, stride st_b; no page serves two of the
+ *            slots written
+ * page_size  a power of two, 16 to 2^20
+ * pos        [B] int32: slot of each sequence's first new token
+ * count      [B] int32: new tokens of each sequence, or NULL: T of each
+ * rope_pos   [B, T] int32, stride sr_b: rotation position of each token (the
+ *            depth of a drafted token, say), or NULL: its slot
+ * wk, sw_k, eps, cos_sin, table_rows, R, interleaved  as in bpc_qk_norm_rope
+ * No workspace; one kernel launch.
+ */
+int bpc_append_kv_paged(const uint16_t* k_new, int64_t sKn_b, int64_t sKn_h, int64_t sKn_t,
+                        const uint16_t* v_new, int64_t sVn_b, int64_t sVn_h, int64_t sVn_t,
+                        uint16_t* K, int64_t sK_p, int64_t sK_h, int64_t sK_n,
+                        uint16_t* V, int64_t sV_p, int64_t sV_h, int64_t sV_n,
+                        const int32_t* block_table, int64_t st_b, int max_pages,
+                        int num_pages, int page_size,
+                        const int32_t* pos, const int32_t* count,
+                        int B, int Hkv, int T, int D,
+                        const uint16_t* wk, int64_t sw_k, float eps,
+                        const float* cos_sin, int table_rows, int R, int interleaved,
+                        const int32_t* rope_pos, int64_t sr_b,
+                        void* stream);
+
+/*
+ * bpc_prefill_attention -- dense attention of T query tokens over N keys, the
+ * prefill whose keys bpc_build_hash then hashes.  Query t has position
+ * p = pos0 + t, key n position n:
+ *     s_n = sm_scale * q_t . K_n
+ *     s_n = softcap * tanh(s_n / softcap)          (softcap > 0)
+ *     s_n = s_n - slopes[head] * |p - n|           (slopes given)
+ *     out_t = softmax over the visible n of s_n, applied to V_n,
+ * visible being max(0, key_begin[b][t]) <= n < min(N, key_end[b][t]).  Without
+ * key_begin: from 0; without key_end: to p + 1 (causal).  A document mask is
+ * key_begin at the first token of each token's document; a prefix mask is
+ * key_end at the prefix's end where that lies behind the token.  A token that
+ * sees no key (padding) gets zeros; what K and V hold at keys that a token does
+ * not see does not reach it, whatever it is.
+ *
+ * q          [B, Hq, T, D] bf16, strides (sq_b, sq_h, sq_t)
+ * K, V       [B, Hkv, >=N, D] bf16, strides as in bpc_decode_attention; any
+ *            group size G = Hq / Hkv up to 128
+ * pos0       >= 0
+ * softcap    0 (none) or finite > 0
+ * slopes     [Hq] fp32 or NULL
+ * key_begin, key_end  [B, T] int32, strides sb_b, se_b (0 = shared), or NULL
+ * out        [B, Hq, T, D] bf16, strides (so_b, so_h, so_t) (written)
+ * workspace  at least bpc_prefill_workspace_bytes(...) bytes (0 for most
+ *            sizes), 256-byte aligned; its contents on entry do not matter.
+ * fp32 scores, statistics and sums; the probabilities enter the second product
+ * as bf16, out is rounded once.  One launch, or two where few query rows face
+ * many keys (the key axis is then split and joined).
+ */
+size_t bpc_prefill_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D);
+int bpc_prefill_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
+                          const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n,
+                          const uint16_t* V, int64_t sV_b, int64_t sV_h, int64_t sV_n,
+                          int B, int Hq, int Hkv, int T, int N, int pos0, int D,
+                          float sm_scale, float softcap, const float* slopes,
+                          const int32_t* key_begin, int64_t sb_b,
+                          const int32_t* key_end, int64_t se_b,
+                          uint16_t* out, int64_t so_b, int64_t so_h, int64_t so_t,
+                          void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * bpc_tree_attention -- dense attention of T drafted tokens over the cache
+ * that holds them: the verification of tokens drafted with the sparse step, or
+ * (T = 1) a dense step over a ragged or paged cache.  Sequence b has lens[b]
+ * tokens before the drafts; draft t is cached at slot lens[b] + t.  It sees
+ * every slot below lens[b], and draft j where bit j of tree[b][t] is set (its
+ * ancestors and itself).  Scores, cap and bias as in bpc_prefill_attention,
+ * where the position of draft t is lens[b] + the number of drafts other than
+ * itself that it sees (its depth).  A draft that sees no slot gets zeros.
+ *
+ * q          [B, Hq, T, D] bf16, strides (sq_b, sq_h, sq_t); 1 <= T <= 64
+ * K, V       without block_table [B, Hkv, >=N, D], strides (batch, head, row);
+ *            with it pools [num_pages, Hkv, page_size, D], strides (page, head,
+ *            row), as in bpc_append_kv_paged
+ * block_table [B, >= ceil(N / page_size)] int32, stride st_b, or NULL.  The
+ *            slots of a page that is not in [0, num_pages) are not seen.
+ * page_size  a power of two, 16 to 2^20 (ignored without block_table)
+ * lens       [B] int32.  A sequence whose lens[b] is not in [0, N - T] is
+ *            skipped: its rows of out stay as they are.
+ * tree       [B, T] int64 bit masks, stride sm_b, or NULL: a chain (draft t sees
+ *            drafts 0..t).  Bits from T on are ignored.
+ * N          slots that any sequence may use, drafts included (sets the
+ *            workspace; need not be near the lengths)
+ * sm_scale, softcap, slopes, out, workspace  as in bpc_prefill_attention, with
+ *            bpc_tree_workspace_bytes(...)
+ */
+size_t bpc_tree_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D);
+int bpc_tree_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
+                       const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n,
+                       const uint16_t* V, int64_t sV_b, int64_t sV_h, int64_t sV_n,
+                       const int32_t* block_table, int64_t st_b, int num_pages, int page_size,
+                       const int32_t* lens,
+                       const int64_t* tree, int64_t sm_b,
+                       int B, int Hq, int Hkv, int T, int N, int D,
+                       float sm_scale, float softcap, const float* slopes,
+                       uint16_t* out, int64_t so_b, int64_t so_h, int64_t so_t,
+                       void* workspace, size_t workspace_bytes,
+                       void* stream);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,7 @@ import torch
 __all__ = [
     "BPCError",
     "append_kv",
+    "append_kv_paged",
     "LIB_PATH",
     "build_hash",
     "build_workspace_bytes",
@@ -33,8 +34,13 @@ __all__ = [
     "decode_noalloc_max_bytes",
     "decode_per_head_workspace_bytes",
     "dense_attention",
+    "prefill_attention",
+    "prefill_workspace_bytes",
+    "qk_norm_rope",
     "select_hard",
     "select_hard_workspace_bytes",
+    "tree_attention",
+    "tree_workspace_bytes",
     "DECODE_STAGES",
     "DECODE_STAGE_NAMES",
     "version",
@@ -110,6 +116,24 @@ _lib.bpc_decode_attention_noalloc.restype = _i
 _lib.bpc_decode_attention_noalloc.argtypes = _DECODE_ARGS[:-3] + [_p]
 _lib.bpc_decode_attention_profiled.restype = _i
 _lib.bpc_decode_attention_profiled.argtypes = _DECODE_ARGS + [ctypes.POINTER(_p), _i]
+
+_f = ctypes.c_float
+_lib.bpc_qk_norm_rope.restype = _i
+_ROPE_TENSOR = [_p, _i64, _i64, _i64, _p, _i64, _i64, _i64, _p, _i64]
+_lib.bpc_qk_norm_rope.argtypes = _ROPE_TENSOR * 2 + [_i, _i, _i, _i, _i, _f, _p, _i, _i, _i, _p, _i64, _p]
+_lib.bpc_append_kv_paged.restype = _i
+_lib.bpc_append_kv_paged.argtypes = [_p, _i64, _i64, _i64] * 4 + [_p, _i64, _i, _i, _i, _p, _p, _i, _i, _i, _i,
+                                                                  _p, _i64, _f, _p, _i, _i, _i, _p, _i64, _p]
+_lib.bpc_prefill_workspace_bytes.restype = _sz
+_lib.bpc_prefill_workspace_bytes.argtypes = [_i] * 6
+_lib.bpc_prefill_attention.restype = _i
+_lib.bpc_prefill_attention.argtypes = [_p, _i64, _i64, _i64] * 3 + [_i] * 7 + [_f, _f, _p, _p, _i64, _p, _i64,
+                                                                             _p, _i64, _i64, _i64, _p, _sz, _p]
+_lib.bpc_tree_workspace_bytes.restype = _sz
+_lib.bpc_tree_workspace_bytes.argtypes = [_i] * 6
+_lib.bpc_tree_attention.restype = _i
+_lib.bpc_tree_attention.argtypes = [_p, _i64, _i64, _i64] * 3 + [_p, _i64, _i, _i, _p, _p, _i64] + [_i] * 6 + \
+    [_f, _f, _p, _p, _i64, _i64, _i64, _p, _sz, _p]
 
 DECODE_STAGES = 3
 DECODE_STAGE_NAMES = ("score", "attend", "merge")
@@ -646,4 +670,300 @@ def dense_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scale:
     _check(_lib.bpc_dense_attention(_ptr(q), _ptr(K), *_kv_strides(K), _ptr(V), *_kv_strides(V), B, Hq, Hkv, N, D,
                                     float(sm_scale), _ptr(out), _ptr(workspace), workspace.numel(), _stream(stream)),
            "bpc_dense_attention")
+    return out
+
+
+# ---------------------------------------------------------------------------
+# Rows on their way into the cache, and attention of many query rows
+# ---------------------------------------------------------------------------
+def _strides3(t: torch.Tensor):
+    """(batch, head, token) strides of [B, H, T, 128]; 0 for an extent of one,
+    whose stride torch leaves open."""
+    (a, b, c, _), (x, y, z, _) = t.shape, t.stride()
+    return x if a > 1 else 0, y if b > 1 else 0, z if c > 1 else 0
+
+
+def _ints(t: Optional[torch.Tensor], name: str, shape, dtype=torch.int32) -> int:
+    """Checks an index array (1 or 2 dims, innermost contiguous); returns its
+    batch stride.  An expanded batch dimension (stride 0) shares one row."""
+    if t is None:
+        return 0
+    _need(t, name, dtype, len(shape))
+    _extent(t, name, shape)
+    return t.stride(0) if len(shape) == 2 and t.shape[0] > 1 else 0
+
+
+def _written(t: torch.Tensor, name: str, shape) -> None:
+    _need(t, name, torch.bfloat16, 4)
+    _extent(t, name, shape)
+    if any(n > 1 and s < 128 for n, s in zip(t.shape[:3], t.stride())):
+        raise ValueError(f"{name}: its rows must not overlap (strides {tuple(t.stride())})")
+
+
+def _norm_weight(w: Optional[torch.Tensor], name: str, H: int) -> int:
+    """Head stride of norm weights given as [128] (one row for all heads) or [H, 128]."""
+    if w is None:
+        return 0
+    if isinstance(w, torch.Tensor) and w.dim() == 1:
+        _need(w, name, torch.bfloat16, 1)
+        _extent(w, name, (128,))
+        return 0
+    _need(w, name, torch.bfloat16, 2)
+    _extent(w, name, (H, 128))
+    return w.stride(0) if H > 1 else 0
+
+
+def _table(cos_sin: Optional[torch.Tensor]):
+    """(rows, R) of a rotation table [positions, R]; (0, 0) without one."""
+    if cos_sin is None:
+        return 0, 0
+    _need(cos_sin, "cos_sin", torch.float32, 2)
+    rows, R = cos_sin.shape
+    if rows < 1 or R % 16 or not 16 <= R <= 128 or not cos_sin.is_contiguous():
+        raise ValueError(f"cos_sin must be a contiguous [positions, R] tensor, R a multiple of 16 up to 128, got {(rows, R)}")
+    return rows, R
+
+
+@contextlib.contextmanager
+def _switch(dev, stream):
+    with torch.cuda.device(dev):
+        if isinstance(stream, torch.cuda.Stream):
+            with torch.cuda.stream(stream):
+                yield
+        else:
+            yield
+
+
+def _place(dev: torch.device, stream):
+    """The context of a call on tensors of `dev`: that device current, and what
+    is allocated within it allocated on `stream`, so that its memory is not
+    reused elsewhere while the kernels run."""
+    if stream is None and dev.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    if isinstance(stream, torch.cuda.Stream) and stream.device != dev:
+        raise ValueError(f"the stream is on {stream.device}, the tensors are on {dev}")
+    return _switch(dev, stream)
+
+
+def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: Optional[torch.Tensor],
+                 cos_sin: Optional[torch.Tensor], *, wq: Optional[torch.Tensor] = None,
+                 wk: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
+    """RMS norm of each head's queries and keys and their rotation by position,
+    in one pass; returns (q_out, k_out), allocated where not given.
+
+    q [B, Hq, T, 128] and k [B, Hkv, T, 128] bf16, any strides over contiguous
+    rows (views of a fused projection, say); either may be None.  wq, wk: norm
+    weights [128] or [H, 128] bf16; None: no norm.  cos_sin [positions, R] fp32:
+    R/2 cosines, then R/2 sines of each position, rotating the first R
+    coordinates (R a multiple of 16, up to 128) in pairs (i, i + R/2), or
+    (2i, 2i + 1) with `interleaved`; None: no rotation.  pos [B, T] int32; the
+    rows of a token whose position is not in the table are not written.
+    q_out, k_out may be q and k themselves, or the rows of a cache."""
+    if q is None and k is None:
+        raise ValueError("q and k cannot both be None")
+    for t, nm in ((q, "q"), (k, "k")):
+        if t is not None:
+            _need(t, nm, torch.bfloat16, 4)
+            _extent(t, nm, (None, None, None, 128))
+    B, _, T, D = (k if q is None else q).shape
+    Hq, Hkv = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
+    if q is not None and k is not None:
+        _extent(k, "k", (B, Hkv, T, D))
+    if B < 1 or T < 1 or Hq + Hkv < 1:
+        raise ValueError("q and k must hold at least one row")
+    for t, src, nm in ((q_out, q, "q_out"), (k_out, k, "k_out")):
+        if t is not None:
+            if src is None:
+                raise ValueError(f"{nm} is given without its input")
+            _written(t, nm, src.shape)
+    rows, R = _table(cos_sin)
+    if R and pos is None:
+        raise ValueError("pos is required with cos_sin")
+    sp = _ints(pos, "pos", (B, T)) if R else 0
+    sq, sk = _norm_weight(wq, "wq", Hq), _norm_weight(wk, "wk", Hkv)
+    _on_gpu(q, k, pos if R else None, cos_sin, wq, wk, q_out, k_out)
+    dev = (k if q is None else q).device
+    with _place(dev, stream):
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=dev)
+        none = (None, 0, 0, 0, None, 0, 0, 0, None, 0)
+        _check(_lib.bpc_qk_norm_rope(
+            *(none if q is None else (_ptr(q), *_strides3(q), _ptr(q_out), *_strides3(q_out), _ptr(wq), sq)),
+            *(none if k is None else (_ptr(k), *_strides3(k), _ptr(k_out), *_strides3(k_out), _ptr(wk), sk)),
+            B, Hq, Hkv, T, D, float(eps), _ptr(cos_sin), rows, R, int(interleaved), _ptr(pos) if R else None, sp,
+            _stream(stream)), "bpc_qk_norm_rope")
+    return q_out, k_out
+
+
+def append_kv_paged(k_new: torch.Tensor, v_new: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
+                    block_table: torch.Tensor, pos: torch.Tensor, *, count: Optional[torch.Tensor] = None,
+                    cos_sin: Optional[torch.Tensor] = None, rope_pos: Optional[torch.Tensor] = None,
+                    wk: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                    stream=None) -> None:
+    """Append to a paged cache, each sequence at its own length: token t of
+    k_new, v_new [B, Hkv, T, 128] bf16 (t < count[b], int32 [B], default T) goes
+    to slot pos[b] + t, that is row slot % page of page block_table[b, slot //
+    page] of the pools K, V [pages, Hkv, page, 128] (page a power of two from 16
+    on), its key normed with wk and rotated as by qk_norm_rope on the way, by
+    its slot or by rope_pos [B, T].  Tokens without a page, or without a row of
+    cos_sin, are not stored."""
+    for t, nm in ((k_new, "k_new"), (v_new, "v_new"), (K, "K"), (V, "V")):
+        _need(t, nm, torch.bfloat16, 4)
+    B, Hkv, T, D = k_new.shape
+    pages, _, page, _ = K.shape
+    _extent(k_new, "k_new", (("ge", 1), ("ge", 1), ("ge", 1), 128))
+    _extent(v_new, "v_new", (B, Hkv, T, D))
+    _extent(K, "K", (("ge", 1), Hkv, None, D))
+    _extent(V, "V", (pages, Hkv, page, D))
+    if page < 16 or page > 1 << 20 or page & (page - 1):
+        raise ValueError(f"K: pages of {page} rows, must be a power of two, 16 to 2^20")
+    _written(K, "K", K.shape)
+    _written(V, "V", V.shape)
+    st = _ints(block_table, "block_table", (B, ("ge", 1)))
+    _ints(pos, "pos", (B,))
+    _ints(count, "count", (B,))
+    rows, R = _table(cos_sin)
+    if rope_pos is not None and not R:
+        raise ValueError("rope_pos needs cos_sin")
+    sr = _ints(rope_pos, "rope_pos", (B, T))
+    sw = _norm_weight(wk, "wk", Hkv)
+    _on_gpu(k_new, v_new, K, V, block_table, pos, count, cos_sin, rope_pos, wk)
+    with _place(K.device, stream):
+        _check(_lib.bpc_append_kv_paged(
+            _ptr(k_new), *_strides3(k_new), _ptr(v_new), *_strides3(v_new), _ptr(K), *_strides3(K), _ptr(V),
+            *_strides3(V), _ptr(block_table), st, block_table.shape[1], pages, page, _ptr(pos), _ptr(count), B, Hkv, T,
+            D, _ptr(wk), sw, float(eps), _ptr(cos_sin), rows, R, int(interleaved), _ptr(rope_pos), sr,
+            _stream(stream)), "bpc_append_kv_paged")
+
+
+def prefill_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, D: int = 128) -> int:
+    return int(_lib.bpc_prefill_workspace_bytes(B, Hq, Hkv, T, N, D))
+
+
+def tree_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, D: int = 128) -> int:
+    return int(_lib.bpc_tree_workspace_bytes(B, Hq, Hkv, T, N, D))
+
+
+def _attn_inputs(q, K, V, slopes, out, workspace):
+    """Checks shared by prefill_attention and tree_attention; returns the sizes of q and the KV heads."""
+    _need(q, "q", torch.bfloat16, 4)
+    _need(K, "K", torch.bfloat16, 4)
+    _need(V, "V", torch.bfloat16, 4)
+    _extent(q, "q", (("ge", 1), ("ge", 1), ("ge", 1), 128))
+    B, Hq, T, D = q.shape
+    Hkv = K.shape[1]
+    if Hkv < 1 or Hq % Hkv:
+        raise ValueError(f"Hq={Hq} must be a multiple of Hkv={Hkv}")
+    if slopes is not None:
+        _need(slopes, "slopes", torch.float32, 1)
+        _extent(slopes, "slopes", (Hq,))
+    if out is not None:
+        _written(out, "out", q.shape)
+    if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 tensor")
+    return B, Hq, Hkv, T, D
+
+
+def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scale: Optional[float] = None,
+                      N: Optional[int] = None, *, pos0: Optional[int] = None, softcap: float = 0.0,
+                      slopes: Optional[torch.Tensor] = None, key_begin: Optional[torch.Tensor] = None,
+                      key_end: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Dense attention of a prefill: q [B, Hq, T, 128] bf16 over the first N of
+    the cached keys K, V [B, Hkv, >=N, 128]; returns out [B, Hq, T, 128] bf16.
+
+    Query t has position pos0 + t (default: the queries are the last T of the N
+    tokens) and sees keys key_begin[b, t] <= n < key_end[b, t] (int32 [B, T];
+    default: from 0, to its own position, both clipped to [0, N)): begin at each
+    document's first token for a document mask, end at the prefix's end for a
+    prefix mask.  Scores are capped to softcap * tanh(s / softcap) when softcap
+    > 0, then lowered by slopes[head] * distance.  A token that sees nothing
+    gets zeros."""
+    B, Hq, Hkv, T, D = _attn_inputs(q, K, V, slopes, out, workspace)
+    N = K.shape[2] if N is None else N
+    if N < 1:
+        raise ValueError(f"N={N} must be >= 1")
+    _extent(K, "K", (B, Hkv, ("ge", N), D))
+    _extent(V, "V", (B, Hkv, ("ge", N), D))
+    if pos0 is None:
+        if T > N:
+            raise ValueError(f"{T} queries are more than the N={N} tokens: pos0 must be given")
+        pos0 = N - T
+    if not 0 <= pos0 <= 1 << 30:
+        raise ValueError(f"pos0={pos0} must be in [0, 2^30]")
+    sb = _ints(key_begin, "key_begin", (B, T))
+    se = _ints(key_end, "key_end", (B, T))
+    _on_gpu(q, K, V, slopes, key_begin, key_end, out, workspace)
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(D)
+    with _place(q.device, stream):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if workspace is None:
+            need = _lib.bpc_prefill_workspace_bytes(B, Hq, Hkv, T, N, D)
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        _check(_lib.bpc_prefill_attention(
+            _ptr(q), *_strides3(q), _ptr(K), *_kv_strides(K), _ptr(V), *_kv_strides(V), B, Hq, Hkv, T, N, pos0, D,
+            float(sm_scale), float(softcap), _ptr(slopes), _ptr(key_begin), sb, _ptr(key_end), se, _ptr(out),
+            *_strides3(out), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)),
+            "bpc_prefill_attention")
+    return out
+
+
+def tree_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torch.Tensor,
+                   tree: Optional[torch.Tensor] = None, sm_scale: Optional[float] = None, N: Optional[int] = None, *,
+                   block_table: Optional[torch.Tensor] = None, softcap: float = 0.0,
+                   slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Dense attention of T <= 64 drafted tokens q [B, Hq, T, 128] bf16 over the
+    cache that holds them, sequence b's at slots lens[b] .. lens[b] + T - 1 (lens
+    int32 [B]); returns out [B, Hq, T, 128] bf16.
+
+    Draft t sees the slots below lens[b] and the drafts j whose bit is set in
+    tree[b, t] (int64 [B, T]; None: a chain, drafts 0..t).  K, V are the
+    contiguous cache [B, Hkv, >=N, 128], or with block_table (int32 [B, pages of
+    a sequence]) pools of pages [pages, Hkv, page, 128] as append_kv_paged writes
+    them.  N: slots that any sequence may use (default: what the cache or the
+    table holds).  softcap and slopes as in prefill_attention, a draft's position
+    being lens[b] plus its depth.  A sequence whose lens[b] is not in [0, N - T]
+    is skipped: its rows of `out` stay as they are (undefined where `out` is
+    allocated here)."""
+    B, Hq, Hkv, T, D = _attn_inputs(q, K, V, slopes, out, workspace)
+    if block_table is None:
+        N = K.shape[2] if N is None else N
+        _extent(K, "K", (B, Hkv, ("ge", N), D))
+        _extent(V, "V", (B, Hkv, ("ge", N), D))
+        pages = page = st = 0
+    else:
+        pages, _, page, _ = K.shape
+        _extent(K, "K", (("ge", 1), Hkv, None, D))
+        _extent(V, "V", (pages, Hkv, page, D))
+        if page < 16 or page > 1 << 20 or page & (page - 1):
+            raise ValueError(f"K: pages of {page} rows, must be a power of two, 16 to 2^20")
+        st = _ints(block_table, "block_table", (B, ("ge", 1)))
+        most = block_table.shape[1] * page
+        N = min(most, 1 << 30) if N is None else N
+        if N > most:
+            raise ValueError(f"N={N}: the block_table holds {most} slots per sequence")
+    if not 1 <= T <= min(64, N):
+        raise ValueError(f"T={T} drafted tokens: must be 1 to 64, and at most N={N}")
+    _ints(lens, "lens", (B,))
+    sm = _ints(tree, "tree", (B, T), torch.int64)
+    _on_gpu(q, K, V, lens, tree, block_table, slopes, out, workspace)
+    if sm_scale is None:
+        sm_scale = 1.0 / math.sqrt(D)
+    with _place(q.device, stream):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if workspace is None:
+            need = _lib.bpc_tree_workspace_bytes(B, Hq, Hkv, T, N, D)
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        _check(_lib.bpc_tree_attention(
+            _ptr(q), *_strides3(q), _ptr(K), *_kv_strides(K), _ptr(V), *_kv_strides(V), _ptr(block_table), st, pages,
+            page, _ptr(lens), _ptr(tree), sm, B, Hq, Hkv, T, N, D, float(sm_scale), float(softcap), _ptr(slopes),
+            _ptr(out), *_strides3(out), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+            _stream(stream)), "bpc_tree_attention")
     return out

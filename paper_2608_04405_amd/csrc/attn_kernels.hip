@@ -1,0 +1,580 @@
+// Dense attention of many query rows: a masked prefill, and a tree of drafted
+// tokens over a contiguous or paged cache.
+//
+// The G query heads of a KV head share its keys, so a row of the product is a
+// (token, head) pair, r = t G + g, and 32 rows make a row block.  A wavefront
+// computes, for 32 rows and tiles of 32 keys,
+//   S^T = K Q^T   (32x32x16 bf16 MFMA: a lane holds 16 scores of ONE row)
+//   O^T += V^T P^T
+// with the softmax's running maximum and sum in that lane, so neither needs
+// more than one exchange with the other half of the wavefront per tile.  The
+// keys a lane holds in S^T are those its half supplies to the second product,
+// so the probabilities go from the accumulators to bf16 operands in place;
+// rounding them to bf16 (2^-9 relative each, averaged by the sum) is what lets
+// both products run on the matrix cores.  Sums and statistics stay fp32.
+//
+// K and V tiles go from global memory to LDS without passing registers, double
+// buffered.  A row of 256 bytes holds its sixteen 16-byte chunks at position
+// chunk ^ swz(row): eight consecutive rows' equal chunks (the K operand) and
+// four consecutive rows' neighbouring chunk pairs (the transposing reads that
+// make the V operand) then lie in different banks.
+#include "bpc_internal.h"
+
+namespace bpc {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kRowBytes = kHeadDim * 2;
+constexpr int kBlockRows = 32;  // query rows of a wavefront
+
+__device__ __forceinline__ uint32_t swz(uint32_t row) {
+  return (row & 8u) | ((row & 3u) << 1) | ((row >> 2) & 1u);
+}
+
+__device__ __forceinline__ uint32_t cvt_pk_bf16(float lo, float hi) {
+  bf16x2 p;
+  p[0] = (__bf16)lo, p[1] = (__bf16)hi;
+  return __builtin_bit_cast(uint32_t, p);
+}
+
+// maximum of a lane's value and that of the lane 32 away, in both
+__device__ __forceinline__ float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ int wave_min(int x) { return wave_reduce_maxmin<false>(x); }
+__device__ __forceinline__ int wave_max(int x) { return wave_reduce_maxmin<true>(x); }
+
+// 64 lanes' 16 bytes each, from `base` + their own offset to LDS at `dst` +
+// 16 lane.  Written out because the compiler would otherwise wait for every
+// such copy in flight before any LDS read; the kernel waits by itself (dma_wait).
+// No register is written, so there is nothing in flight that the compiler does
+// not know of but the LDS bytes, which it cannot touch before dma_wait.
+__device__ __forceinline__ void dma16(const char* base, uint32_t off, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :
+               : "v"(off), "s"(base), "s"(dst)
+               : "memory");
+}
+template <int N>
+__device__ __forceinline__ void dma_wait() {  // until at most N copies of this wavefront are in flight
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
+template <typename T>
+__device__ __forceinline__ T lds_read(uint32_t at) {
+  return *(__attribute__((address_space(3))) T*)at;
+}
+
+// a value that every lane reads at the same address, through the scalar cache
+// (a vector load would have to wait for the copies in flight before it)
+__device__ __forceinline__ int32_t uniform_load(const int32_t* p) {
+  return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
+}
+
+// RB row blocks of 32 rows by KW groups of wavefronts that take alternate key
+// tiles of KT keys; RB KW wavefronts.
+template <int RB, int KW, int KT, bool TREE, bool CAP, bool BIAS>
+struct AttnShape {
+  static constexpr int kThreads = RB * KW * 64;
+  static constexpr int kTileBytes = KT * kRowBytes;    // K or V of a tile
+  static constexpr int kLds = KW * 2 * 2 * kTileBytes;  // K and V, two buffers, per group
+};
+
+template <int RB, int KW, int KT, bool TREE, bool CAP, bool BIAS>
+__global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nrb, int items) {
+  using S = AttnShape<RB, KW, KT, TREE, CAP, BIAS>;
+  constexpr int NB = KT / 32;   // 32-key blocks of a tile
+  constexpr int RPW = KT / RB;  // rows of a tile's K (and V) that a wavefront copies
+  static_assert(RPW % 4 == 0, "a copy moves four rows");
+  extern __shared__ char smem[];
+  __shared__ int draft_place[TREE && BIAS ? 64 : 1];
+  // consecutive workgroups go to different XCDs; give each XCD a run of
+  // consecutive items, which share their keys in its L2
+  const int per_xcd = (items + 7) / 8;
+  const int item = (blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
+  if (item >= items || (int)(blockIdx.x >> 3) >= per_xcd) return;
+  const int rb = nrb - 1 - item % nrb;  // later rows see more keys: longest first
+  const int split = item / nrb % a.splits, bh = item / nrb / a.splits;
+  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int grp = wid / RB, rbw = wid % RB;
+  const int half = lane >> 5, col = lane & 31;
+  const int G = a.G, rows = a.T * G;
+  const int wg_row0 = rb * RB * kBlockRows;
+
+  // ---- the keys that any row of the workgroup sees -------------------------
+  int klo = 0, khi = 0, len = 0;
+  if (TREE) {
+    len = a.lens[b];
+    if (len < 0 || len > a.N - a.T) return;  // no such sequence: its rows stay as they are
+    khi = len + a.T;
+  } else {
+    const int t0 = wg_row0 / G, t1 = min(rows - 1, wg_row0 + RB * kBlockRows - 1) / G;
+    int lo = INT32_MAX, hi = 0;
+    for (int t = t0 + lane; t <= t1; t += 64) {
+      const int f = a.key_begin ? max(a.key_begin[b * a.s_begin + t], 0) : 0;
+      const int e = a.key_end ? min(a.key_end[b * a.s_end + t], a.N) : (int)min((int64_t)a.N, (int64_t)a.pos0 + t + 1);
+      if (f < e) lo = min(lo, f), hi = max(hi, e);
+    }
+    klo = wave_min(lo), khi = wave_max(hi);
+    if (klo >= khi) klo = khi = 0;
+  }
+
+  // ---- this lane's row ------------------------------------------------------
+  const int row = wg_row0 + rbw * kBlockRows + col;
+  const bool live = row < rows;
+  const int t = live ? row / G : 0, g = live ? row - t * G : 0;
+  int lo = INT32_MIN, hi = INT32_MAX;  // rows past the last see everything: they never make a tile partial
+  uint64_t sees = ~0ull;
+  int place = 0;  // position, for the distance
+  if (TREE) {
+    hi = len;
+    if (live) {
+      const uint64_t all = a.T >= 64 ? ~0ull : (1ull << a.T) - 1;
+      sees = (a.tree ? a.tree[b * a.s_tree + t] : (2ull << t) - 1) & all;
+      place = len + __popcll(sees & ~(1ull << t));
+    }
+  } else if (live) {
+    lo = a.key_begin ? max(a.key_begin[b * a.s_begin + t], 0) : 0;
+    hi = a.key_end ? min(a.key_end[b * a.s_end + t], a.N) : (int)min((int64_t)a.N, (int64_t)a.pos0 + t + 1);
+    place = a.pos0 + t;
+  }
+  // every row's keys cover [all_lo, all_hi); no row sees a key outside [any_lo, any_hi)
+  int all_lo = 0, all_hi = len, any_lo = 0, any_hi = khi;
+  if (!TREE) {
+    all_lo = wave_max(lo), all_hi = wave_min(hi);
+    any_lo = wave_min(live && lo < hi ? lo : INT32_MAX), any_hi = wave_max(live && lo < hi ? hi : 0);
+  }
+  if (TREE && BIAS) {
+    // the distance counts a draft at its depth in the tree
+    if (threadIdx.x < a.T) {
+      const int j = threadIdx.x;
+      const uint64_t js = (a.tree ? a.tree[b * a.s_tree + j] : (2ull << j) - 1) & (a.T >= 64 ? ~0ull : (1ull << a.T) - 1);
+      draft_place[j] = len + __popcll(js & ~(1ull << j));
+    }
+    __syncthreads();
+  }
+  const float slope = BIAS && live ? a.slopes[h * G + g] * kLog2e : 0.f;
+
+  bf16x8 qf[8];
+  {
+    const uint16_t* qp = a.q + b * a.sq_b + (int64_t)(h * G + g) * a.sq_h + (int64_t)t * a.sq_t + 8 * half;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      u32x4 x = live ? *reinterpret_cast<const u32x4*>(qp + 16 * s) : u32x4{0, 0, 0, 0};
+      qf[s] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+
+  // ---- tiles of this workgroup ---------------------------------------------
+  const int base0 = klo / KT * KT;
+  const int total = (khi - base0 + KT * KW - 1) / (KT * KW);
+  const int per = (total + a.splits - 1) / a.splits;
+  const int it0 = split * per, it1 = min(total, it0 + per);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
+  const uint32_t ldsK = lds0 + grp * 4 * S::kTileBytes, ldsV = ldsK + 2 * S::kTileBytes;
+
+  const bool paged = TREE && a.table;
+  const int32_t* table = paged ? a.table + b * a.st_b : nullptr;
+  const char* Kb = reinterpret_cast<const char*>(a.K + (paged ? 0 : b * a.sK_b) + h * a.sK_h);
+  const char* Vb = reinterpret_cast<const char*>(a.V + (paged ? 0 : b * a.sV_b) + h * a.sV_h);
+  const int64_t kstep = a.sK_n * 2, vstep = a.sV_n * 2;
+  const int pmask = (1 << a.page_shift) - 1;
+  // a page that the table does not name hides its keys; rare enough to look only once
+  bool bad_pages = false;
+  if (paged && it0 < it1) {
+    const int p0 = (base0 + it0 * KT * KW) >> a.page_shift, p1 = (min(khi, base0 + it1 * KT * KW) - 1) >> a.page_shift;
+    bool bad = false;
+    for (int p = p0 + lane; p <= p1; p += 64) bad |= (uint32_t)table[p] >= (uint32_t)a.num_pages;
+    bad_pages = __any(bad);
+  }
+
+  const int r4 = lane >> 4;  // row within a copy's four
+  auto issue = [&](int it, int buf) {
+    const int n0 = base0 + (it * KW + grp) * KT + rbw * RPW;
+#pragma unroll
+    for (int u = 0; u < (RPW + 15) / 16; ++u) {
+      constexpr int RU = RPW < 16 ? RPW : 16;  // rows of one page at least
+      const int nu = min(n0 + 16 * u, khi - 1);
+      const char *kt, *vt;
+      int last;  // last row that may be read, from kt and vt on
+      if (paged) {
+        const uint32_t pg = (uint32_t)uniform_load(table + (nu >> a.page_shift));
+        const int64_t page = pg < (uint32_t)a.num_pages ? pg : 0;
+        kt = Kb + page * a.sK_b * 2 + (nu & pmask) * kstep;
+        vt = Vb + page * a.sV_b * 2 + (nu & pmask) * vstep;
+      } else {
+        kt = Kb + nu * kstep, vt = Vb + nu * vstep;
+      }
+      last = khi - 1 - nu;
+#pragma unroll
+      for (int i = 0; i < RU / 4; ++i) {
+        const int rt = 16 * u + 4 * i;  // row within this wavefront's share
+        const uint32_t r = min(4 * i + r4, last);
+        const uint32_t chunk = ((uint32_t)lane & 15u) ^ swz((uint32_t)(rbw * RPW + rt + r4));
+        const uint32_t dst = (uint32_t)buf * S::kTileBytes + (rbw * RPW + rt) * kRowBytes;
+        dma16(kt, r * (uint32_t)kstep + chunk * 16, ldsK + dst);
+        dma16(vt, r * (uint32_t)vstep + chunk * 16, ldsV + dst);
+      }
+    }
+  };
+  constexpr int kCopies = 2 * (RPW / 4);  // copies a wavefront issues per tile
+
+  f32x16 o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+  }
+  float mrun = -INFINITY, lsum = 0.f;
+
+  const uint32_t kswz = swz(col & 15) ^ half;
+  uint32_t kaddr[8], vaddr[4];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) kaddr[s] = ldsK + col * kRowBytes + ((2 * s) ^ kswz) * 16;
+  {
+    const int i16 = lane & 15, gd = r4 & 1;
+    const uint32_t chunk = 2 * gd + ((i16 & 3) >> 1), f = swz(4 * half + (i16 >> 2));
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+      vaddr[d] = ldsV + (4 * half + (i16 >> 2)) * kRowBytes + ((4 * d + chunk) ^ f) * 16 + (i16 & 1) * 8;
+  }
+  const float c1 = a.sm_scale * kLog2e;
+  const float cap2 = a.softcap * kLog2e, capk = CAP ? 2.f * kLog2e * a.sm_scale / a.softcap : 0.f;
+
+  auto compute = [&](int it, int buf) {
+    const int n0 = base0 + (it * KW + grp) * KT;
+    if (n0 >= any_hi || n0 + KT <= any_lo) return;
+    const bool full = n0 >= all_lo && n0 + KT <= all_hi && !bad_pages;
+    const uint32_t bo = buf * S::kTileBytes;
+    f32x16 acc[NB];
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[k][e] = 0.f;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, lds_read<u32x4>(kaddr[s] + bo + k * 32 * kRowBytes));
+        acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], acc[k], 0, 0, 0);
+      }
+    }
+    // key of score e of block k: n0 + 32 k + 8 (e / 4) + 4 half + e % 4
+    const int nl = n0 + 4 * half;
+    if (CAP || BIAS) {
+#pragma unroll
+      for (int k = 0; k < NB; ++k) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float z = acc[k][e];
+          // cap tanh(x) = cap - 2 cap / (1 + e^2x)
+          if (CAP)
+            z = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * capk)), cap2);
+          else
+            z *= c1;
+          if (BIAS) {
+            int n = nl + 32 * k + 8 * (e / 4) + e % 4;
+            if (TREE && n0 + KT > len) n = (uint32_t)(n - len) < (uint32_t)a.T ? draft_place[n - len] : n;
+            z = fmaf(-slope, (float)abs(place - n), z);
+          }
+          acc[k][e] = z;
+        }
+      }
+    }
+    auto visible = [&](int n) {
+      if (!TREE) return n >= lo && n < hi;
+      const uint32_t j = (uint32_t)(n - len);
+      return n < len || (j < 64u && ((sees >> (j & 63u)) & 1u));
+    };
+    if (!full) {
+#pragma unroll
+      for (int k = 0; k < NB; ++k) {
+        bool hidden[2] = {false, false};
+        if (bad_pages) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int n = n0 + 32 * k + 16 * u;
+            hidden[u] = n < khi && (uint32_t)uniform_load(table + (n >> a.page_shift)) >= (uint32_t)a.num_pages;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int n = nl + 32 * k + 8 * (e / 4) + e % 4;
+          acc[k][e] = visible(n) && n < khi && !hidden[e / 8] ? acc[k][e] : -INFINITY;
+        }
+      }
+    }
+    float mt = acc[0][0];
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mt = fmaxf(mt, acc[k][e]);
+    }
+    mt = max_halves(mt);
+    if (!CAP && !BIAS) mt *= c1;
+    // the reference point of the exponentials moves only when a score lies more
+    // than 2^8 above it, so that the products are seldom rescaled; any point
+    // gives the same quotient
+    if (__any(mt > mrun + 8.f)) {
+      const float mn = fmaxf(mrun, mt);
+      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrun - mn);
+      mrun = mn;
+      lsum *= f;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] *= f;
+      }
+    }
+    const float mu = mrun == -INFINITY ? 0.f : mrun;
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = __builtin_amdgcn_exp2f((CAP || BIAS) ? acc[k][e] - mu : fmaf(acc[k][e], c1, -mu));
+        acc[k][e] = p;
+        lsum += p;
+      }
+    }
+    // a key that a row does not see must not reach it through 0 * V either:
+    // values that are not finite are left out of the product and added below
+    bool odd = false;
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4 pw;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pw[e] = cvt_pk_bf16(acc[k][8 * s + 2 * e], acc[k][8 * s + 2 * e + 1]);
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          // keys 16 s + 4 half + j and 16 s + 8 + 4 half + j: the second lies eight
+          // rows on, whose swizzle differs in bit 3
+          const uint32_t at = bo + (32 * k + 16 * s) * kRowBytes;
+          s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vaddr[d] + at));
+          s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) s16x4*)(vaddr[d ^ 2] + at + 8 * kRowBytes));
+          if (!full) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool n0f = (v0[e] & 0x7F80) == 0x7F80, n1f = (v1[e] & 0x7F80) == 0x7F80;
+              odd |= n0f | n1f;
+              v0[e] = n0f ? (short)0 : v0[e], v1[e] = n1f ? (short)0 : v1[e];
+            }
+          }
+          bf16x8 vf;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            vf[e] = __builtin_bit_cast(__bf16, (short)v0[e]);
+            vf[4 + e] = __builtin_bit_cast(__bf16, (short)v1[e]);
+          }
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[d], 0, 0, 0);
+        }
+      }
+    }
+    if (!full && __any(odd)) {
+#pragma unroll 1
+      for (int i = 0; i < KT; ++i) {
+        const int n = n0 + i;
+        const bool hidden = bad_pages && n < khi && (uint32_t)uniform_load(table + (n >> a.page_shift)) >= (uint32_t)a.num_pages;
+        const bool see = visible(n) && n < khi && !hidden;
+        const uint32_t rowat = ldsV + bo + i * kRowBytes + 8 * half;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {  // coordinates 8 c + 4 half + 0..3
+          const u32x2 x = lds_read<u32x2>(rowat + ((uint32_t)c ^ swz(i & 15)) * 16);
+          const uint32_t w[4] = {x.x << 16, x.x & 0xFFFF0000u, x.y << 16, x.y & 0xFFFF0000u};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (see && (w[e] & 0x7F800000u) == 0x7F800000u) o[c / 4][4 * (c % 4) + e] += __uint_as_float(w[e]);
+        }
+      }
+    }
+  };
+
+  if (it0 < it1) issue(it0, 0);
+  for (int it = it0; it < it1; ++it) {
+    const int buf = (it - it0) & 1;
+    if (it + 1 < it1) {
+      issue(it + 1, buf ^ 1);
+      dma_wait<kCopies>();
+    } else {
+      dma_wait<0>();
+    }
+    if (RB > 1) __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+    compute(it, buf);
+    lds_done();  // the reads of this buffer, before it is filled again
+    if (RB > 1) __builtin_amdgcn_s_barrier();
+  }
+
+  // ---- results ---------------------------------------------------------------
+  lsum = sum_halves(lsum);
+  if (KW > 1) {
+    // the groups of a row block join in LDS: [group][row block][coordinate / 4][row] of 4 fp32, then (max, sum) [group][row block][row]
+    __syncthreads();
+    float4* so = reinterpret_cast<float4*>(smem);
+    float2* sm = reinterpret_cast<float2*>(smem + (KW - 1) * RB * kBlockRows * kHeadDim * sizeof(float));
+    if (half == 0) sm[(grp * RB + rbw) * kBlockRows + col] = make_float2(mrun, lsum);
+    __syncthreads();
+    float mx = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) mx = fmaxf(mx, sm[(k * RB + rbw) * kBlockRows + col].x);
+    float tot = 0.f;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) {
+      const float2 x = sm[(k * RB + rbw) * kBlockRows + col];
+      tot += x.y == 0.f ? 0.f : x.y * __builtin_amdgcn_exp2f(x.x - mx);
+    }
+    const float f = lsum == 0.f ? 0.f : __builtin_amdgcn_exp2f(mrun - mx);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[d][e] *= f;
+    }
+    if (grp > 0) {
+#pragma unroll
+      for (int c = 0; c < 16; ++c)
+        so[(((grp - 1) * RB + rbw) * 32 + 2 * c + half) * kBlockRows + col] =
+            make_float4(o[c / 4][4 * (c % 4)], o[c / 4][4 * (c % 4) + 1], o[c / 4][4 * (c % 4) + 2], o[c / 4][4 * (c % 4) + 3]);
+    }
+    __syncthreads();
+    if (grp > 0) return;
+#pragma unroll
+    for (int k = 0; k < KW - 1; ++k) {
+#pragma unroll
+      for (int c = 0; c < 16; ++c) {
+        const float4 x = so[((k * RB + rbw) * 32 + 2 * c + half) * kBlockRows + col];
+        o[c / 4][4 * (c % 4)] += x.x, o[c / 4][4 * (c % 4) + 1] += x.y;
+        o[c / 4][4 * (c % 4) + 2] += x.z, o[c / 4][4 * (c % 4) + 3] += x.w;
+      }
+    }
+    mrun = mx, lsum = tot;
+  }
+  if (!live) return;
+  if (a.splits > 1) {
+    const int64_t at = ((int64_t)bh * rows + row) * a.splits + split;
+    if (half == 0) a.part_ml[at] = make_float2(mrun, lsum);
+    if (lsum == 0.f) return;
+    float* po = a.part_o + at * kHeadDim + 4 * half;
+#pragma unroll
+    for (int c = 0; c < 16; ++c)
+      *reinterpret_cast<float4*>(po + 8 * c) =
+          make_float4(o[c / 4][4 * (c % 4)], o[c / 4][4 * (c % 4) + 1], o[c / 4][4 * (c % 4) + 2], o[c / 4][4 * (c % 4) + 3]);
+    return;
+  }
+  const float inv = lsum == 0.f ? 0.f : 1.f / lsum;  // a row that sees no key: zeros
+  uint16_t* op = a.out + b * a.so_b + (int64_t)(h * G + g) * a.so_h + (int64_t)t * a.so_t + 4 * half;
+#pragma unroll
+  for (int c = 0; c < 16; ++c) {
+    *reinterpret_cast<uint2*>(op + 8 * c) =
+        make_uint2(cvt_pk_bf16(o[c / 4][4 * (c % 4)] * inv, o[c / 4][4 * (c % 4) + 1] * inv),
+                   cvt_pk_bf16(o[c / 4][4 * (c % 4) + 2] * inv, o[c / 4][4 * (c % 4) + 3] * inv));
+  }
+}
+
+// The splits of a row joined: a wavefront per row, two coordinates per lane.
+template <bool TREE>
+__global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
+  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (bh, t, g)
+  const int rows = a.T * a.G, lane = threadIdx.x & 63;
+  const int64_t bh = r / rows;
+  if (bh >= (int64_t)a.B * a.Hkv) return;
+  const int row = (int)(r - bh * rows), t = row / a.G, g = row - t * a.G;
+  const int b = (int)(bh / a.Hkv), h = (int)(bh - (int64_t)b * a.Hkv);
+  if (TREE) {
+    const int len = a.lens[b];
+    if (len < 0 || len > a.N - a.T) return;
+  }
+  const float2* ml = a.part_ml + r * a.splits;
+  const float* po = a.part_o + r * a.splits * kHeadDim + 2 * lane;
+  float mx = -INFINITY, tot = 0.f, x0 = 0.f, x1 = 0.f;
+  for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, ml[s].x);
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 p = ml[s];
+    if (p.y == 0.f) continue;  // the split saw no key of this row: its sum was not written
+    const float f = __builtin_amdgcn_exp2f(p.x - mx);
+    const float2 v = *reinterpret_cast<const float2*>(po + (int64_t)s * kHeadDim);
+    tot = fmaf(p.y, f, tot), x0 = fmaf(v.x, f, x0), x1 = fmaf(v.y, f, x1);
+  }
+  const float inv = tot == 0.f ? 0.f : 1.f / tot;
+  uint16_t* op = a.out + b * a.so_b + (int64_t)(h * a.G + g) * a.so_h + (int64_t)t * a.so_t;
+  *reinterpret_cast<uint32_t*>(op + 2 * lane) = cvt_pk_bf16(x0 * inv, x1 * inv);
+}
+
+template <int RB, int KW, int KT, bool TREE>
+static hipError_t launch_attn_shape(const AttnArgs& a) {
+  const int rows = a.T * a.G, nrb = (rows + RB * kBlockRows - 1) / (RB * kBlockRows);
+  const int items = a.B * a.Hkv * nrb * a.splits;
+  const int grid = (items + 7) / 8 * 8;
+#define BPC_ATTN(CAP, BIAS)                                                                                       \
+  {                                                                                                               \
+    auto* f = attn_kernel<RB, KW, KT, TREE, CAP, BIAS>;                                                           \
+    constexpr int lds = AttnShape<RB, KW, KT, TREE, CAP, BIAS>::kLds;                                             \
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, lds); \
+    if (e != hipSuccess) return e;                                                                                \
+    f<<<grid, RB * KW * 64, lds, a.stream>>>(a, nrb, items);                                                      \
+  }
+  if (a.softcap > 0.f) {
+    if (a.slopes) BPC_ATTN(true, true) else BPC_ATTN(true, false)
+  } else {
+    if (a.slopes) BPC_ATTN(false, true) else BPC_ATTN(false, false)
+  }
+#undef BPC_ATTN
+  return hipGetLastError();
+}
+
+AttnPlan attn_plan(int B, int Hkv, int G, int T, int N) {
+  AttnPlan p{};
+  const int64_t rows = (int64_t)T * G;
+  p.rb = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  const int64_t blocks = (rows + p.rb * kBlockRows - 1) / (p.rb * kBlockRows) * B * Hkv;
+  const int unit = p.rb == 1 ? 128 : 64;  // keys per step of a workgroup
+  const int64_t most = ((int64_t)N + 2 * unit - 1) / (2 * unit);
+  int64_t s = 1024 / blocks;
+  s = s > most ? most : s;
+  s = s > 64 ? 64 : s;
+  p.splits = s < 1 ? 1 : (int)s;
+  size_t o = 0;
+  auto take = [&](size_t bytes) {
+    size_t at = o;
+    o += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  if (p.splits > 1) {
+    const size_t n = (size_t)B * Hkv * rows * p.splits;
+    p.off_ml = take(n * sizeof(float2));
+    p.off_o = take(n * kHeadDim * sizeof(float));
+  }
+  p.total = o;
+  return p;
+}
+
+template <bool TREE>
+static hipError_t launch_attn_as(const AttnArgs& a, const AttnPlan& p) {
+  hipError_t e = p.rb == 1   ? launch_attn_shape<1, 4, 32, TREE>(a)
+                 : p.rb == 2 ? launch_attn_shape<2, 2, 32, TREE>(a)
+                             : launch_attn_shape<4, 1, 64, TREE>(a);
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t rows = (int64_t)a.B * a.Hkv * a.T * a.G;
+  attn_merge_kernel<TREE><<<(unsigned)((rows + 3) / 4), 256, 0, a.stream>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_attn(const AttnArgs& a, const AttnPlan& p) {
+  return a.lens ? launch_attn_as<true>(a, p) : launch_attn_as<false>(a, p);
+}
+
+}  // namespace bpc

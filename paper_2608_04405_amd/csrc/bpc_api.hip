@@ -557,6 +557,268 @@ int bpc_select_hard_ws(const float* err, int64_t sE_b, int64_t sE_h, int B, int 
 }
 
 // ---------------------------------------------------------------------------
+// Rows on their way into the cache, and attention of many query rows
+// ---------------------------------------------------------------------------
+
+// A bf16 tensor of B x H x T rows whose extents are given, so that the stride of
+// an extent of one does not matter; rows may be interleaved in any order.
+static int check_rows(const char* name, const void* p, int64_t sb, int64_t sh, int64_t st) {
+  if (!p) return fail(BPC_EINVAL, "%s is NULL", name);
+  if (sb < 0 || sh < 0 || st < 0) return fail(BPC_EINVAL, "%s strides must be >= 0", name);
+  if (!aligned16(p) || (sb % 8) || (sh % 8) || (st % 8))
+    return fail(BPC_EALIGN, "%s must be 16-byte aligned with strides multiple of 8 elements", name);
+  return BPC_OK;
+}
+
+// A tensor that is written: no two of its rows in the same place
+static int check_written(const char* name, const void* p, int64_t sb, int64_t sh, int64_t st, int B, int H, int T) {
+  int rc = check_rows(name, p, sb, sh, st);
+  if (rc) return rc;
+  if ((B > 1 && sb < kHeadDim) || (H > 1 && sh < kHeadDim) || (T > 1 && st < kHeadDim))
+    return fail(BPC_EINVAL, "%s: strides of written rows must be at least 128", name);
+  return BPC_OK;
+}
+
+static int check_rotation(const float* cos_sin, int table_rows, int R) {
+  if (R < 0 || R > kHeadDim || R % 16) return fail(BPC_EINVAL, "R=%d must be a multiple of 16, 0 to 128", R);
+  if (R == 0) return BPC_OK;
+  if (!cos_sin || table_rows < 1) return fail(BPC_EINVAL, "cos_sin with at least one row is required when R > 0");
+  if (!aligned16(cos_sin)) return fail(BPC_EALIGN, "cos_sin must be 16-byte aligned");
+  return BPC_OK;
+}
+
+static int check_norm(const char* name, const uint16_t* w, int64_t sw) {
+  if (!w) return BPC_OK;
+  if (sw < 0) return fail(BPC_EINVAL, "%s stride must be >= 0", name);
+  if (!aligned16(w) || (sw % 8)) return fail(BPC_EALIGN, "%s must be 16-byte aligned with a stride multiple of 8", name);
+  return BPC_OK;
+}
+
+static int check_eps(float eps) {
+  if (!(eps >= 0.0f) || !__builtin_isfinite(eps)) return fail(BPC_EINVAL, "eps must be finite and >= 0");
+  return BPC_OK;
+}
+
+static int check_int32(const char* name, const int32_t* p, int64_t stride) {
+  if (!p) return fail(BPC_EINVAL, "%s is NULL", name);
+  if (stride < 0) return fail(BPC_EINVAL, "%s stride must be >= 0", name);
+  if (!aligned4(p)) return fail(BPC_EALIGN, "%s must be 4-byte aligned", name);
+  return BPC_OK;
+}
+
+// sequences, heads and tokens of a call whose wavefronts a 32-bit grid counts
+static int check_tokens(int B, int H, int T) {
+  if (B < 1 || H < 1 || T < 1) return fail(BPC_EINVAL, "B=%d, heads=%d, T=%d must all be >= 1", B, H, T);
+  if (H > (1 << 16)) return fail(BPC_EUNSUPPORTED, "%d heads: at most 65536", H);
+  if ((int64_t)B * T > (int64_t)(1 << 30)) return fail(BPC_EUNSUPPORTED, "B T = %lld tokens: at most 2^30", (long long)B * T);
+  return BPC_OK;
+}
+
+static int page_shift(int page_size) {
+  if (page_size < 16 || page_size > (1 << 20) || (page_size & (page_size - 1))) return -1;
+  return __builtin_ctz((unsigned)page_size);
+}
+
+int bpc_qk_norm_rope(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t, uint16_t* q_out, int64_t sqo_b,
+                     int64_t sqo_h, int64_t sqo_t, const uint16_t* wq, int64_t sw_q, const uint16_t* k, int64_t sk_b,
+                     int64_t sk_h, int64_t sk_t, uint16_t* k_out, int64_t sko_b, int64_t sko_h, int64_t sko_t,
+                     const uint16_t* wk, int64_t sw_k, int B, int Hq, int Hkv, int T, int D, float eps,
+                     const float* cos_sin, int table_rows, int R, int interleaved, const int32_t* pos, int64_t sp_b,
+                     void* stream) {
+  g_last_error[0] = 0;
+  int st;
+  if (Hq < 0 || Hkv < 0) return fail(BPC_EINVAL, "Hq=%d and Hkv=%d must be >= 0", Hq, Hkv);
+  if (Hq > (1 << 16) || Hkv > (1 << 16)) return fail(BPC_EUNSUPPORTED, "at most 65536 heads");
+  if ((st = check_tokens(B, Hq + Hkv, T))) return st;
+  if ((st = check_head_dim(D))) return st;
+  if ((st = check_eps(eps))) return st;
+  if ((st = check_rotation(cos_sin, table_rows, R))) return st;
+  if (R && (st = check_int32("pos", pos, sp_b))) return st;
+  RopeArgs a{};
+  if (Hq) {
+    if ((st = check_rows("q", q, sq_b, sq_h, sq_t))) return st;
+    if ((st = check_written("q_out", q_out, sqo_b, sqo_h, sqo_t, B, Hq, T))) return st;
+    if ((st = check_norm("wq", wq, sw_q))) return st;
+    a.q = RopeTensor{q, sq_b, sq_h, sq_t, q_out, sqo_b, sqo_h, sqo_t, wq, sw_q, Hq};
+  }
+  if (Hkv) {
+    if ((st = check_rows("k", k, sk_b, sk_h, sk_t))) return st;
+    if ((st = check_written("k_out", k_out, sko_b, sko_h, sko_t, B, Hkv, T))) return st;
+    if ((st = check_norm("wk", wk, sw_k))) return st;
+    a.k = RopeTensor{k, sk_b, sk_h, sk_t, k_out, sko_b, sko_h, sko_t, wk, sw_k, Hkv};
+  }
+  a.pos = pos, a.sp_b = sp_b, a.cos_sin = cos_sin, a.table_rows = table_rows, a.R = R, a.inter = interleaved != 0;
+  a.eps = eps, a.B = B, a.T = T, a.stream = static_cast<hipStream_t>(stream);
+  hipError_t e = launch_qk_norm_rope(a);
+  if (e != hipSuccess) return hip_fail(e, "bpc_qk_norm_rope launch");
+  return BPC_OK;
+}
+
+int bpc_append_kv_paged(const uint16_t* k_new, int64_t sKn_b, int64_t sKn_h, int64_t sKn_t, const uint16_t* v_new,
+                        int64_t sVn_b, int64_t sVn_h, int64_t sVn_t, uint16_t* K, int64_t sK_p, int64_t sK_h,
+                        int64_t sK_n, uint16_t* V, int64_t sV_p, int64_t sV_h, int64_t sV_n,
+                        const int32_t* block_table, int64_t st_b, int max_pages, int num_pages, int page_size,
+                        const int32_t* pos, const int32_t* count, int B, int Hkv, int T, int D, const uint16_t* wk,
+                        int64_t sw_k, float eps, const float* cos_sin, int table_rows, int R, int interleaved,
+                        const int32_t* rope_pos, int64_t sr_b, void* stream) {
+  g_last_error[0] = 0;
+  int st;
+  if ((st = check_tokens(B, Hkv, T))) return st;
+  if ((st = check_head_dim(D))) return st;
+  const int shift = page_shift(page_size);
+  if (shift < 0) return fail(BPC_EINVAL, "page_size=%d must be a power of two, 16 to 2^20", page_size);
+  if (num_pages < 1 || max_pages < 1) return fail(BPC_EINVAL, "num_pages=%d and max_pages=%d must be >= 1", num_pages, max_pages);
+  if ((st = check_rows("k_new", k_new, sKn_b, sKn_h, sKn_t))) return st;
+  if ((st = check_rows("v_new", v_new, sVn_b, sVn_h, sVn_t))) return st;
+  if ((st = check_written("K", K, sK_p, sK_h, sK_n, num_pages, Hkv, page_size))) return st;
+  if ((st = check_written("V", V, sV_p, sV_h, sV_n, num_pages, Hkv, page_size))) return st;
+  if ((st = check_int32("block_table", block_table, st_b))) return st;
+  if ((st = check_int32("pos", pos, 0))) return st;
+  if (count && (st = check_int32("count", count, 0))) return st;
+  if ((st = check_norm("wk", wk, sw_k))) return st;
+  if ((st = check_eps(eps))) return st;
+  if ((st = check_rotation(cos_sin, table_rows, R))) return st;
+  if (rope_pos && (st = check_int32("rope_pos", rope_pos, sr_b))) return st;
+  AppendPagedArgs a{};
+  a.kn = k_new, a.skn_b = sKn_b, a.skn_h = sKn_h, a.skn_t = sKn_t;
+  a.vn = v_new, a.svn_b = sVn_b, a.svn_h = sVn_h, a.svn_t = sVn_t;
+  a.K = K, a.sK_p = sK_p, a.sK_h = sK_h, a.sK_n = sK_n;
+  a.V = V, a.sV_p = sV_p, a.sV_h = sV_h, a.sV_n = sV_n;
+  a.table = block_table, a.st_b = st_b, a.max_pages = max_pages, a.num_pages = num_pages, a.page_shift = shift;
+  a.pos = pos, a.count = count, a.rope_pos = rope_pos, a.sr_b = sr_b;
+  a.cos_sin = cos_sin, a.table_rows = table_rows, a.R = R, a.inter = interleaved != 0;
+  a.wk = wk, a.sw_h = sw_k, a.eps = eps, a.B = B, a.Hkv = Hkv, a.T = T;
+  a.stream = static_cast<hipStream_t>(stream);
+  hipError_t e = launch_append_paged(a);
+  if (e != hipSuccess) return hip_fail(e, "bpc_append_kv_paged launch");
+  return BPC_OK;
+}
+
+constexpr int kMaxAttnGroup = 128;
+
+static bool attn_sizes_ok(int B, int Hq, int Hkv, int T, int N, int D) {
+  return B >= 1 && Hkv >= 1 && Hq >= Hkv && Hq % Hkv == 0 && Hq / Hkv <= kMaxAttnGroup && T >= 1 && N >= 1 && D == kHeadDim &&
+         N <= (1 << 30) && (int64_t)B * Hkv <= (1 << 20) && (int64_t)T * (Hq / Hkv) <= (1 << 30);
+}
+
+// what the two attention entry points have in common
+static int check_attn(const AttnArgs& a, int Hq, int D, const AttnPlan& plan, const void* workspace, size_t workspace_bytes) {
+  int st;
+  if ((st = check_rows("q", a.q, a.sq_b, a.sq_h, a.sq_t))) return st;
+  if ((st = check_kv("K", a.K, a.sK_b, a.sK_h, a.sK_n))) return st;
+  if ((st = check_kv("V", a.V, a.sV_b, a.sV_h, a.sV_n))) return st;
+  if (a.sK_n > (1 << 24) || a.sV_n > (1 << 24)) return fail(BPC_EUNSUPPORTED, "row strides of K and V: at most 2^24 elements");
+  if ((st = check_written("out", a.out, a.so_b, a.so_h, a.so_t, a.B, Hq, a.T))) return st;
+  if (!(a.sm_scale > 0.0f) || !__builtin_isfinite(a.sm_scale)) return fail(BPC_EINVAL, "sm_scale must be finite and > 0");
+  if (!(a.softcap >= 0.0f) || !__builtin_isfinite(a.softcap)) return fail(BPC_EINVAL, "softcap must be finite and >= 0");
+  if (a.slopes && !aligned4(a.slopes)) return fail(BPC_EALIGN, "slopes must be 4-byte aligned");
+  const int64_t blocks = ((int64_t)a.T * a.G + plan.rb * 32 - 1) / (plan.rb * 32) * a.B * a.Hkv * plan.splits;
+  if (blocks > (int64_t)(1 << 30)) return fail(BPC_EUNSUPPORTED, "%lld workgroups: too many rows in one call", (long long)blocks);
+  if (plan.total) {
+    if (!workspace || workspace_bytes < plan.total)
+      return fail(BPC_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : 0, plan.total);
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(BPC_EALIGN, "workspace must be 256-byte aligned");
+  }
+  return BPC_OK;
+}
+
+static int check_attn_sizes(int B, int Hq, int Hkv, int T, int N, int D) {
+  int st;
+  if ((st = check_sizes(B, Hkv, N))) return st;
+  if (T < 1) return fail(BPC_EINVAL, "T=%d must be >= 1", T);
+  if (Hq < Hkv || Hq % Hkv) return fail(BPC_EINVAL, "Hq=%d must be a positive multiple of Hkv=%d", Hq, Hkv);
+  if ((st = check_head_dim(D))) return st;
+  if (!attn_sizes_ok(B, Hq, Hkv, T, N, D))
+    return fail(BPC_EUNSUPPORTED, "B=%d, Hq=%d, Hkv=%d, T=%d: groups of at most %d heads, B Hkv <= 2^20, T Hq / Hkv <= 2^30", B,
+                Hq, Hkv, T, kMaxAttnGroup);
+  return BPC_OK;
+}
+
+static void attn_workspace(AttnArgs& a, const AttnPlan& plan, void* workspace) {
+  a.splits = plan.splits;
+  if (!plan.total) return;
+  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + plan.off_ml);
+  a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.off_o);
+}
+
+size_t bpc_prefill_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D) {
+  return attn_sizes_ok(B, Hq, Hkv, T, N, D) ? attn_plan(B, Hkv, Hq / Hkv, T, N).total : 0;
+}
+
+int bpc_prefill_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t, const uint16_t* K, int64_t sK_b,
+                          int64_t sK_h, int64_t sK_n, const uint16_t* V, int64_t sV_b, int64_t sV_h, int64_t sV_n, int B,
+                          int Hq, int Hkv, int T, int N, int pos0, int D, float sm_scale, float softcap,
+                          const float* slopes, const int32_t* key_begin, int64_t sb_b, const int32_t* key_end,
+                          int64_t se_b, uint16_t* out, int64_t so_b, int64_t so_h, int64_t so_t, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  g_last_error[0] = 0;
+  int st;
+  if ((st = check_attn_sizes(B, Hq, Hkv, T, N, D))) return st;
+  if (pos0 < 0 || pos0 > (1 << 30)) return fail(BPC_EINVAL, "pos0=%d must be in [0, 2^30]", pos0);
+  AttnArgs a{};
+  a.q = q, a.sq_b = sq_b, a.sq_h = sq_h, a.sq_t = sq_t;
+  a.K = K, a.sK_b = sK_b, a.sK_h = sK_h, a.sK_n = sK_n;
+  a.V = V, a.sV_b = sV_b, a.sV_h = sV_h, a.sV_n = sV_n;
+  a.B = B, a.Hkv = Hkv, a.G = Hq / Hkv, a.T = T, a.N = N, a.pos0 = pos0;
+  a.key_begin = key_begin, a.s_begin = sb_b, a.key_end = key_end, a.s_end = se_b;
+  a.sm_scale = sm_scale, a.softcap = softcap, a.slopes = slopes;
+  a.out = out, a.so_b = so_b, a.so_h = so_h, a.so_t = so_t;
+  a.stream = static_cast<hipStream_t>(stream);
+  const AttnPlan plan = attn_plan(B, Hkv, a.G, T, N);
+  if ((st = check_attn(a, Hq, D, plan, workspace, workspace_bytes))) return st;
+  if (key_begin && (st = check_int32("key_begin", key_begin, sb_b))) return st;
+  if (key_end && (st = check_int32("key_end", key_end, se_b))) return st;
+  attn_workspace(a, plan, workspace);
+  hipError_t e = launch_attn(a, plan);
+  if (e != hipSuccess) return hip_fail(e, "bpc_prefill_attention launch");
+  return BPC_OK;
+}
+
+size_t bpc_tree_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D) {
+  return T <= 64 && T <= N && attn_sizes_ok(B, Hq, Hkv, T, N, D) ? attn_plan(B, Hkv, Hq / Hkv, T, N).total : 0;
+}
+
+int bpc_tree_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t, const uint16_t* K, int64_t sK_b,
+                       int64_t sK_h, int64_t sK_n, const uint16_t* V, int64_t sV_b, int64_t sV_h, int64_t sV_n,
+                       const int32_t* block_table, int64_t st_b, int num_pages, int page_size, const int32_t* lens,
+                       const int64_t* tree, int64_t sm_b, int B, int Hq, int Hkv, int T, int N, int D, float sm_scale,
+                       float softcap, const float* slopes, uint16_t* out, int64_t so_b, int64_t so_h, int64_t so_t,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error[0] = 0;
+  int st;
+  if ((st = check_attn_sizes(B, Hq, Hkv, T, N, D))) return st;
+  if (T > 64) return fail(BPC_EUNSUPPORTED, "T=%d: at most 64 drafted tokens", T);
+  if (T > N) return fail(BPC_EINVAL, "T=%d drafts need as many slots, N=%d", T, N);
+  AttnArgs a{};
+  a.q = q, a.sq_b = sq_b, a.sq_h = sq_h, a.sq_t = sq_t;
+  a.K = K, a.sK_b = sK_b, a.sK_h = sK_h, a.sK_n = sK_n;
+  a.V = V, a.sV_b = sV_b, a.sV_h = sV_h, a.sV_n = sV_n;
+  a.B = B, a.Hkv = Hkv, a.G = Hq / Hkv, a.T = T, a.N = N;
+  a.lens = lens, a.tree = reinterpret_cast<const uint64_t*>(tree), a.s_tree = sm_b;
+  a.sm_scale = sm_scale, a.softcap = softcap, a.slopes = slopes;
+  a.out = out, a.so_b = so_b, a.so_h = so_h, a.so_t = so_t;
+  a.stream = static_cast<hipStream_t>(stream);
+  const AttnPlan plan = attn_plan(B, Hkv, a.G, T, N);
+  if ((st = check_attn(a, Hq, D, plan, workspace, workspace_bytes))) return st;
+  if ((st = check_int32("lens", lens, 0))) return st;
+  if (tree) {
+    if (sm_b < 0) return fail(BPC_EINVAL, "tree stride must be >= 0");
+    if (reinterpret_cast<uintptr_t>(tree) & 7u) return fail(BPC_EALIGN, "tree must be 8-byte aligned");
+  }
+  if (block_table) {
+    if ((st = check_int32("block_table", block_table, st_b))) return st;
+    const int shift = page_shift(page_size);
+    if (shift < 0) return fail(BPC_EINVAL, "page_size=%d must be a power of two, 16 to 2^20", page_size);
+    if (num_pages < 1) return fail(BPC_EINVAL, "num_pages=%d must be >= 1", num_pages);
+    a.table = block_table, a.st_b = st_b, a.num_pages = num_pages, a.page_shift = shift;
+  }
+  attn_workspace(a, plan, workspace);
+  hipError_t e = launch_attn(a, plan);
+  if (e != hipSuccess) return hip_fail(e, "bpc_tree_attention launch");
+  return BPC_OK;
+}
+
+// ---------------------------------------------------------------------------
 // Decode without a caller workspace: the workspace is `scratch`, a static
 // device array of kScratchBytes that every GPU the library runs on holds
 // until the process ends.  In host code `scratch` only names the symbol; its

@@ -222,6 +222,91 @@ hipError_t launch_norm(const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK
                        const float* P, int64_t sP_b, int64_t sP_h, const uint32_t* codes, int64_t sC_b, int64_t sC_h,
                        float* err, hipStream_t stream);
 
+// ---- rows on their way into the cache -------------------------------------
+struct RopeTensor {
+  const uint16_t* in;
+  int64_t si_b, si_h, si_t;
+  uint16_t* out;
+  int64_t so_b, so_h, so_t;
+  const uint16_t* w;  // norm weights, or nullptr
+  int64_t sw_h;
+  int H;
+};
+struct RopeArgs {
+  RopeTensor q, k;
+  const int32_t* pos;
+  int64_t sp_b;
+  const float* cos_sin;
+  int table_rows, R, inter;
+  float eps;
+  int B, T;
+  hipStream_t stream;
+};
+hipError_t launch_qk_norm_rope(const RopeArgs& a);
+
+struct AppendPagedArgs {
+  const uint16_t* kn;
+  int64_t skn_b, skn_h, skn_t;
+  const uint16_t* vn;
+  int64_t svn_b, svn_h, svn_t;
+  uint16_t* K;
+  int64_t sK_p, sK_h, sK_n;
+  uint16_t* V;
+  int64_t sV_p, sV_h, sV_n;
+  const int32_t* table;
+  int64_t st_b;
+  int max_pages, num_pages, page_shift;
+  const int32_t* pos;
+  const int32_t* count;
+  const int32_t* rope_pos;
+  int64_t sr_b;
+  const float* cos_sin;
+  int table_rows, R, inter;
+  const uint16_t* wk;
+  int64_t sw_h;
+  float eps;
+  int B, Hkv, T;
+  hipStream_t stream;
+};
+hipError_t launch_append_paged(const AppendPagedArgs& a);
+
+// ---- attention of many query rows -----------------------------------------
+struct AttnArgs {
+  const uint16_t* q;
+  int64_t sq_b, sq_h, sq_t;
+  const uint16_t* K;  // sK_b, sV_b: stride of a sequence, or of a page
+  int64_t sK_b, sK_h, sK_n;
+  const uint16_t* V;
+  int64_t sV_b, sV_h, sV_n;
+  int B, Hkv, G, T, N;
+  int pos0;  // prefill: position of the first query
+  const int32_t* key_begin;
+  int64_t s_begin;
+  const int32_t* key_end;
+  int64_t s_end;
+  const int32_t* lens;  // tree attention: cached tokens before the drafts
+  const uint64_t* tree;
+  int64_t s_tree;
+  const int32_t* table;
+  int64_t st_b;
+  int num_pages, page_shift;
+  float sm_scale, softcap;
+  const float* slopes;
+  uint16_t* out;
+  int64_t so_b, so_h, so_t;
+  int splits;
+  float2* part_ml;  // [B, Hkv, T G][splits] (max, sum), and o[128]
+  float* part_o;
+  hipStream_t stream;
+};
+// how a call is cut: 32-row blocks per workgroup, and pieces of the key axis
+struct AttnPlan {
+  int rb, splits;
+  size_t off_ml, off_o, total;
+};
+AttnPlan attn_plan(int B, int Hkv, int G, int T, int N);
+hipError_t launch_attn(const AttnArgs& a, const AttnPlan& p);
+
 struct BuildArgs {
   const uint16_t* K;
   int64_t sK_b, sK_h, sK_n;

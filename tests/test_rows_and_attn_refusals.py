@@ -1,0 +1,256 @@
+"""What qk_norm_rope, append_kv_paged, prefill_attention and tree_attention
+refuse, on the CPU: the binding by tensor extents, the C entries by their
+arguments (their pointers are fake, and every call fails a check)."""
+
+import ctypes
+import os
+
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2608_04405_amd", "libbpc.so")
+pytestmark = pytest.mark.skipif(not os.path.exists(LIB), reason="libbpc.so not built")
+
+OK, EINVAL, EUNSUP, EALIGN, EWS, EHIP = 0, -1, -2, -3, -4, -5
+FAKE = 0x10000
+bf, f32, i32, i64 = torch.bfloat16, torch.float32, torch.int32, torch.int64
+
+
+@pytest.fixture(scope="module")
+def bpc():
+    import paper_2608_04405_amd as m
+    return m
+
+
+def z(*shape, dtype=bf):
+    return torch.zeros(*shape, dtype=dtype)
+
+
+def expect(fn, word):
+    with pytest.raises((ValueError, TypeError)) as e:
+        fn()
+    assert word in str(e.value), str(e.value)
+
+
+# ------------------------------------------------------------- the binding
+def rope(bpc, **kw):
+    a = dict(q=z(2, 8, 5, 128), k=z(2, 2, 5, 128), pos=z(2, 5, dtype=i32), cos_sin=z(9, 64, dtype=f32))
+    a.update(kw)
+    return bpc.qk_norm_rope(a.pop("q"), a.pop("k"), a.pop("pos"), a.pop("cos_sin"), **a)
+
+
+def append(bpc, **kw):
+    a = dict(k_new=z(2, 2, 5, 128), v_new=z(2, 2, 5, 128), K=z(7, 2, 16, 128), V=z(7, 2, 16, 128), block_table=z(2, 3, dtype=i32),
+             pos=z(2, dtype=i32))
+    a.update(kw)
+    return bpc.append_kv_paged(**a)
+
+
+def prefill(bpc, **kw):
+    a = dict(q=z(2, 8, 5, 128), K=z(2, 2, 9, 128), V=z(2, 2, 9, 128))
+    a.update(kw)
+    return bpc.prefill_attention(a.pop("q"), a.pop("K"), a.pop("V"), **a)
+
+
+def tree(bpc, **kw):
+    a = dict(q=z(2, 8, 5, 128), K=z(2, 2, 32, 128), V=z(2, 2, 32, 128), lens=z(2, dtype=i32))
+    a.update(kw)
+    return bpc.tree_attention(a.pop("q"), a.pop("K"), a.pop("V"), a.pop("lens"), **a)
+
+
+def test_good_shapes_reach_the_device_check(bpc):
+    expect(lambda: rope(bpc, wq=z(128), wk=z(2, 128), q_out=z(2, 8, 5, 128)), "GPU")
+    expect(lambda: rope(bpc, q=None, pos=z(1, 5, dtype=i32).expand(2, 5)), "GPU")
+    expect(lambda: append(bpc, count=z(2, dtype=i32), cos_sin=z(9, 128, dtype=f32), rope_pos=z(2, 5, dtype=i32), wk=z(128)), "GPU")
+    expect(lambda: prefill(bpc, slopes=z(8, dtype=f32), key_begin=z(2, 5, dtype=i32), key_end=z(2, 5, dtype=i32), softcap=3.0), "GPU")
+    expect(lambda: tree(bpc, tree=z(2, 5, dtype=i64), slopes=z(8, dtype=f32)), "GPU")
+    expect(lambda: tree(bpc, block_table=z(2, 2, dtype=i32), N=30), "GPU")
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(q=None, k=None), "both"),
+    (dict(q=z(2, 8, 5, 64)), "q"),
+    (dict(q=z(2, 8, 5, 128, dtype=torch.float16)), "q"),
+    (dict(k=z(3, 2, 5, 128)), "k"),
+    (dict(k=z(2, 2, 4, 128)), "k"),
+    (dict(q=z(2, 8, 0, 128), k=None, pos=z(2, 0, dtype=i32)), "row"),
+    (dict(pos=None), "pos"),
+    (dict(pos=z(2, 4, dtype=i32)), "pos"),
+    (dict(pos=z(2, 5, dtype=i64)), "pos"),
+    (dict(cos_sin=z(9, 24, dtype=f32)), "cos_sin"),
+    (dict(cos_sin=z(9, 144, dtype=f32)), "cos_sin"),
+    (dict(cos_sin=z(9, 128, dtype=f32)[:, :64]), "cos_sin"),
+    (dict(cos_sin=z(9, 64)), "cos_sin"),
+    (dict(wq=z(127)), "wq"),
+    (dict(wk=z(3, 128)), "wk"),
+    (dict(wq=z(128, dtype=f32)), "wq"),
+    (dict(q_out=z(2, 8, 4, 128)), "q_out"),
+    (dict(q_out=z(1, 8, 5, 128).expand(2, 8, 5, 128)), "overlap"),
+    (dict(k=None, k_out=z(2, 2, 5, 128)), "k_out"),
+])
+def test_rope_refuses(bpc, kw, word):
+    expect(lambda: rope(bpc, **kw), word)
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(v_new=z(2, 2, 4, 128)), "v_new"),
+    (dict(K=z(7, 3, 16, 128)), "K"),
+    (dict(V=z(6, 2, 16, 128)), "V"),
+    (dict(V=z(7, 2, 32, 128)), "V"),
+    (dict(K=z(7, 2, 24, 128), V=z(7, 2, 24, 128)), "power"),
+    (dict(K=z(7, 2, 8, 128), V=z(7, 2, 8, 128)), "power"),
+    (dict(K=z(1, 2, 16, 128).expand(7, 2, 16, 128)), "overlap"),
+    (dict(block_table=z(3, 3, dtype=i32)), "block_table"),
+    (dict(block_table=z(2, 0, dtype=i32)), "block_table"),
+    (dict(pos=z(3, dtype=i32)), "pos"),
+    (dict(pos=z(2, dtype=i64)), "pos"),
+    (dict(count=z(1, dtype=i32)), "count"),
+    (dict(rope_pos=z(2, 5, dtype=i32)), "rope_pos"),
+    (dict(rope_pos=z(2, 4, dtype=i32), cos_sin=z(9, 64, dtype=f32)), "rope_pos"),
+    (dict(wk=z(2, 64)), "wk"),
+])
+def test_append_paged_refuses(bpc, kw, word):
+    expect(lambda: append(bpc, **kw), word)
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(q=z(2, 9, 5, 128)), "multiple"),
+    (dict(K=z(2, 2, 9, 64)), "K"),
+    (dict(K=z(1, 2, 9, 128)), "K"),
+    (dict(V=z(2, 2, 8, 128)), "V"),
+    (dict(N=10), "K"),
+    (dict(N=0), "N"),
+    (dict(N=4), "pos0"),
+    (dict(pos0=-1), "pos0"),
+    (dict(pos0=1 << 31), "pos0"),
+    (dict(slopes=z(7, dtype=f32)), "slopes"),
+    (dict(slopes=z(8)), "slopes"),
+    (dict(key_begin=z(2, 4, dtype=i32)), "key_begin"),
+    (dict(key_end=z(2, 5, dtype=i64)), "key_end"),
+    (dict(key_end=z(5, 2, dtype=i32).t()), "key_end"),
+    (dict(out=z(2, 8, 5, 128, dtype=f32)), "out"),
+    (dict(out=z(2, 8, 6, 128)), "out"),
+    (dict(out=z(2, 1, 5, 128).expand(2, 8, 5, 128)), "overlap"),
+    (dict(workspace=z(8)), "workspace"),
+])
+def test_prefill_refuses(bpc, kw, word):
+    expect(lambda: prefill(bpc, **kw), word)
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(q=z(2, 8, 65, 128), K=z(2, 2, 99, 128), V=z(2, 2, 99, 128)), "drafted"),
+    (dict(N=4), "drafted"),
+    (dict(N=33), "K"),
+    (dict(lens=z(3, dtype=i32)), "lens"),
+    (dict(lens=z(2, dtype=i64)), "lens"),
+    (dict(tree=z(2, 5, dtype=i32)), "tree"),
+    (dict(tree=z(2, 4, dtype=i64)), "tree"),
+    (dict(block_table=z(3, 2, dtype=i32)), "block_table"),
+    (dict(block_table=z(2, 2, dtype=i32), N=65), "block_table"),
+    (dict(block_table=z(2, 2, dtype=i32), K=z(2, 2, 24, 128), V=z(2, 2, 24, 128)), "power"),
+    (dict(block_table=z(2, 2, dtype=i32), V=z(3, 2, 32, 128)), "V"),
+])
+def test_tree_refuses(bpc, kw, word):
+    expect(lambda: tree(bpc, **kw), word)
+
+
+# ------------------------------------------------------------- the C entries
+@pytest.fixture(scope="module")
+def lib():
+    L = ctypes.CDLL(LIB)
+    L.bpc_last_error.restype = ctypes.c_char_p
+    for f in (L.bpc_prefill_workspace_bytes, L.bpc_tree_workspace_bytes):
+        f.restype = ctypes.c_size_t
+    return L
+
+
+def call(lib, name, spec, kw):
+    """spec: (name, ctype, value) of every argument."""
+    unknown = set(kw) - {n for n, _, _ in spec}
+    assert not unknown, unknown
+    f = getattr(lib, name)
+    f.restype = ctypes.c_int
+    return f(*(t(kw.get(n, v)) for n, t, v in spec))
+
+
+P, S, I, F, Z = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
+
+
+def rows(name, h, t=8 * 128):
+    return [(name, P, FAKE), (name + "_b", S, h * 640), (name + "_h", S, 640), (name + "_t", S, 128)]
+
+
+ROPE = (rows("q", 8) + rows("qo", 8) + [("wq", P, None), ("swq", S, 0)] + rows("k", 2) + rows("ko", 2) + [("wk", P, None), ("swk", S, 0)] +
+        [("B", I, 2), ("Hq", I, 8), ("Hkv", I, 2), ("T", I, 5), ("D", I, 128), ("eps", F, 1e-6), ("cs", P, FAKE), ("rows", I, 9), ("R", I, 64),
+         ("inter", I, 0), ("pos", P, FAKE), ("sp", S, 5), ("stream", P, None)])
+APPEND = (rows("kn", 2) + rows("vn", 2) + rows("K", 2) + rows("V", 2) +
+          [("table", P, FAKE), ("st", S, 3), ("max_pages", I, 3), ("pages", I, 7), ("page", I, 16), ("pos", P, FAKE), ("count", P, None),
+           ("B", I, 2), ("Hkv", I, 2), ("T", I, 5), ("D", I, 128), ("wk", P, None), ("swk", S, 0), ("eps", F, 0.0), ("cs", P, None), ("rows", I, 0),
+           ("R", I, 0), ("inter", I, 0), ("rpos", P, None), ("sr", S, 0), ("stream", P, None)])
+SCORE = [("sm", F, 0.088), ("cap", F, 0.0), ("slopes", P, None)]
+OUT = rows("o", 8) + [("ws", P, FAKE), ("wsb", Z, 1 << 40), ("stream", P, None)]
+PREFILL = (rows("q", 8) + rows("K", 2) + rows("V", 2) +
+           [("B", I, 2), ("Hq", I, 8), ("Hkv", I, 2), ("T", I, 5), ("N", I, 5000), ("pos0", I, 0), ("D", I, 128)] + SCORE +
+           [("begin", P, None), ("sb", S, 0), ("end", P, None), ("se", S, 0)] + OUT)
+TREE = (rows("q", 8) + rows("K", 2) + rows("V", 2) +
+        [("table", P, FAKE), ("st", S, 400), ("pages", I, 900), ("page", I, 16), ("lens", P, FAKE), ("tree", P, None), ("sm_b", S, 0), ("B", I, 2),
+         ("Hq", I, 8), ("Hkv", I, 2), ("T", I, 5), ("N", I, 5000), ("D", I, 128)] + SCORE + OUT)
+
+ANY_ATTN = [
+    (dict(q=None), EINVAL), (dict(K=None), EINVAL), (dict(V=None), EINVAL), (dict(o=None), EINVAL), (dict(B=0), EINVAL), (dict(T=0), EINVAL),
+    (dict(N=0), EINVAL), (dict(Hq=9), EINVAL), (dict(Hq=2 * 129), EUNSUP), (dict(D=64), EUNSUP), (dict(sm=0.0), EINVAL),
+    (dict(sm=float("inf")), EINVAL), (dict(cap=-1.0), EINVAL), (dict(cap=float("nan")), EINVAL), (dict(slopes=FAKE + 2), EALIGN),
+    (dict(q=FAKE + 2), EALIGN), (dict(o=FAKE + 8), EALIGN), (dict(K_t=100), EINVAL), (dict(K_t=132), EALIGN), (dict(V_t=1 << 25), EUNSUP),
+    (dict(o_h=64), EINVAL), (dict(q_h=-8), EINVAL), (dict(ws=None), EWS), (dict(wsb=256), EWS), (dict(ws=FAKE + 16), EALIGN),
+]
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(q=None), EINVAL), (dict(qo=None), EINVAL), (dict(k=None), EINVAL), (dict(ko=None), EINVAL), (dict(Hq=0, Hkv=0), EINVAL),
+    (dict(Hq=-1), EINVAL), (dict(B=0), EINVAL), (dict(T=0), EINVAL), (dict(D=64), EUNSUP), (dict(eps=-1.0), EINVAL), (dict(eps=float("nan")), EINVAL),
+    (dict(R=24), EINVAL), (dict(R=144), EINVAL), (dict(cs=None), EINVAL), (dict(rows=0), EINVAL), (dict(cs=FAKE + 4), EALIGN), (dict(pos=None), EINVAL),
+    (dict(pos=FAKE + 2), EALIGN), (dict(sp=-1), EINVAL), (dict(q=FAKE + 2), EALIGN), (dict(q_t=132), EALIGN), (dict(qo_t=64), EINVAL),
+    (dict(wq=FAKE + 2), EALIGN), (dict(wk=FAKE, swk=-8), EINVAL), (dict(T=1 << 30), EUNSUP), (dict(Hq=1 << 17), EUNSUP),
+])
+def test_rope_entry_rejects(lib, kw, code):
+    assert call(lib, "bpc_qk_norm_rope", ROPE, kw) == code
+    assert lib.bpc_last_error() != b""
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(kn=None), EINVAL), (dict(vn=None), EINVAL), (dict(K=None), EINVAL), (dict(V=None), EINVAL), (dict(table=None), EINVAL),
+    (dict(pos=None), EINVAL), (dict(page=24), EINVAL), (dict(page=8), EINVAL), (dict(page=1 << 21), EINVAL), (dict(pages=0), EINVAL),
+    (dict(max_pages=0), EINVAL), (dict(B=0), EINVAL), (dict(T=0), EINVAL), (dict(Hkv=0), EINVAL), (dict(D=64), EUNSUP), (dict(K_t=64), EINVAL),
+    (dict(V_b=0), EINVAL), (dict(K=FAKE + 8), EALIGN), (dict(count=FAKE + 1), EALIGN), (dict(R=16), EINVAL), (dict(wk=FAKE + 2), EALIGN),
+    (dict(rpos=FAKE + 2), EALIGN), (dict(eps=-1.0), EINVAL), (dict(st=-1), EINVAL),
+])
+def test_append_paged_entry_rejects(lib, kw, code):
+    assert call(lib, "bpc_append_kv_paged", APPEND, kw) == code
+    assert lib.bpc_last_error() != b""
+
+
+@pytest.mark.parametrize("kw,code", ANY_ATTN + [
+    (dict(pos0=-1), EINVAL), (dict(begin=FAKE + 2), EALIGN), (dict(end=FAKE, se=-1), EINVAL), (dict(T=1 << 30), EUNSUP),
+])
+def test_prefill_entry_rejects(lib, kw, code):
+    assert call(lib, "bpc_prefill_attention", PREFILL, kw) == code
+    assert lib.bpc_last_error() != b""
+
+
+@pytest.mark.parametrize("kw,code", ANY_ATTN + [
+    (dict(T=65), EUNSUP), (dict(N=4), EINVAL), (dict(lens=None), EINVAL), (dict(lens=FAKE + 2), EALIGN), (dict(tree=FAKE + 4), EALIGN),
+    (dict(tree=FAKE, sm_b=-1), EINVAL), (dict(page=17), EINVAL), (dict(pages=0), EINVAL), (dict(st=-1), EINVAL),
+])
+def test_tree_entry_rejects(lib, kw, code):
+    assert call(lib, "bpc_tree_attention", TREE, kw) == code
+    assert lib.bpc_last_error() != b""
+
+
+def test_workspace_sizes(lib):
+    pre, tr = lib.bpc_prefill_workspace_bytes, lib.bpc_tree_workspace_bytes
+    assert pre(2, 32, 8, 8192, 8192, 128) == 0  # enough rows: the key axis stays whole
+    assert pre(1, 32, 8, 64, 65536, 128) > 0 and pre(1, 32, 8, 64, 65536, 128) % 256 == 0
+    assert tr(1, 32, 8, 1, 4096, 128) > 0
+    assert tr(1, 32, 8, 65, 4096, 128) == 0 and tr(1, 32, 8, 8, 4, 128) == 0
+    assert pre(1, 32, 8, 64, 65536, 64) == 0 and pre(1, 30, 8, 64, 65536, 128) == 0
