@@ -185,7 +185,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
     return stream.cuda_stream or None
 
 
@@ -231,16 +231,17 @@ def _exact_out(t: Optional[torch.Tensor], name: str, dtype, shape) -> None:
 
 def _on_gpu(*tensors) -> None:
     """Every given tensor (None entries skipped) on one GPU."""
-    dev = None
+    dev = -1
     for t in tensors:
         if t is None:
             continue
-        if t.device.type != "cuda":
+        d = t.get_device()
+        if d < 0:
             raise ValueError("every tensor must be on a GPU")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise ValueError(f"tensors on different devices: {dev} and {t.device}")
+        if dev < 0:
+            dev = d
+        elif d != dev:
+            raise ValueError(f"tensors on different devices: cuda:{dev} and {t.device}")
 
 
 def _budget(k: int, N: int, Ncap: int) -> None:
@@ -676,6 +677,17 @@ def dense_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scale:
 # ---------------------------------------------------------------------------
 # Rows on their way into the cache, and attention of many query rows
 # ---------------------------------------------------------------------------
+def _rows(t: torch.Tensor, name: str):
+    """The shape of a bf16 [B, H, T, 128] tensor with contiguous rows."""
+    if type(t) is torch.Tensor and t.dtype is torch.bfloat16:
+        s = t.shape
+        if len(s) == 4 and s[3] == 128 and t.stride(3) == 1 and 0 not in s:
+            return s
+    _need(t, name, torch.bfloat16, 4)
+    _extent(t, name, (("ge", 1), ("ge", 1), ("ge", 1), 128))
+    return t.shape
+
+
 def _strides3(t: torch.Tensor):
     """(batch, head, token) strides of [B, H, T, 128]; 0 for an extent of one,
     whose stride torch leaves open."""
@@ -683,26 +695,32 @@ def _strides3(t: torch.Tensor):
     return x if a > 1 else 0, y if b > 1 else 0, z if c > 1 else 0
 
 
-def _ints(t: Optional[torch.Tensor], name: str, shape, dtype=torch.int32) -> int:
+def _indices(t: Optional[torch.Tensor], name: str, shape, dtype=torch.int32) -> int:
     """Checks an index array (1 or 2 dims, innermost contiguous); returns its
     batch stride.  An expanded batch dimension (stride 0) shares one row."""
     if t is None:
         return 0
+    if type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return shape[-1] if len(shape) == 2 else 0
     _need(t, name, dtype, len(shape))
     _extent(t, name, shape)
-    return t.stride(0) if len(shape) == 2 and t.shape[0] > 1 else 0
+    return t.stride(0) if len(shape) == 2 and shape[0] > 1 else 0
 
 
 def _written(t: torch.Tensor, name: str, shape) -> None:
-    _need(t, name, torch.bfloat16, 4)
-    _extent(t, name, shape)
-    if any(n > 1 and s < 128 for n, s in zip(t.shape[:3], t.stride())):
+    _rows(t, name)
+    if t.shape != shape:
+        _extent(t, name, shape)
+    (a, b, c, _), (x, y, z, _) = shape, t.stride()
+    if (x < 128 and a > 1) or (y < 128 and b > 1) or (z < 128 and c > 1):
         raise ValueError(f"{name}: its rows must not overlap (strides {tuple(t.stride())})")
 
 
 def _norm_weight(w: Optional[torch.Tensor], name: str, H: int) -> int:
     """Head stride of norm weights given as [128] (one row for all heads) or [H, 128]."""
     if w is None:
+        return 0
+    if type(w) is torch.Tensor and w.dtype is torch.bfloat16 and w.shape == (128,) and w.is_contiguous():
         return 0
     if isinstance(w, torch.Tensor) and w.dim() == 1:
         _need(w, name, torch.bfloat16, 1)
@@ -717,11 +735,30 @@ def _table(cos_sin: Optional[torch.Tensor]):
     """(rows, R) of a rotation table [positions, R]; (0, 0) without one."""
     if cos_sin is None:
         return 0, 0
-    _need(cos_sin, "cos_sin", torch.float32, 2)
+    if type(cos_sin) is not torch.Tensor or cos_sin.dtype is not torch.float32 or cos_sin.dim() != 2:
+        _need(cos_sin, "cos_sin", torch.float32, 2)
     rows, R = cos_sin.shape
     if rows < 1 or R % 16 or not 16 <= R <= 128 or not cos_sin.is_contiguous():
         raise ValueError(f"cos_sin must be a contiguous [positions, R] tensor, R a multiple of 16 up to 128, got {(rows, R)}")
     return rows, R
+
+
+def _block_table(t: torch.Tensor, B: int):
+    """(batch stride, pages of a sequence) of a page table [B, pages]."""
+    if type(t) is not torch.Tensor or t.dtype is not torch.int32 or t.dim() != 2 or t.stride(1) != 1:
+        _need(t, "block_table", torch.int32, 2)
+    b, n = t.shape
+    if b != B or n < 1:
+        _extent(t, "block_table", (B, ("ge", 1)))
+    return t.stride(0) if B > 1 else 0, n
+
+
+def _page_rows(page: int) -> None:
+    if page < 16 or page > 1 << 20 or page & (page - 1):
+        raise ValueError(f"K: pages of {page} rows, must be a power of two, 16 to 2^20")
+
+
+_HERE = contextlib.nullcontext()
 
 
 @contextlib.contextmanager
@@ -734,15 +771,18 @@ def _switch(dev, stream):
             yield
 
 
-def _place(dev: torch.device, stream):
-    """The context of a call on tensors of `dev`: that device current, and what
-    is allocated within it allocated on `stream`, so that its memory is not
+def _place(t: torch.Tensor, stream):
+    """The context of a call on tensors of t's device: that device current, and
+    what is allocated within it allocated on `stream`, so that its memory is not
     reused elsewhere while the kernels run."""
-    if stream is None and dev.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    if isinstance(stream, torch.cuda.Stream) and stream.device != dev:
-        raise ValueError(f"the stream is on {stream.device}, the tensors are on {dev}")
-    return _switch(dev, stream)
+    if stream is None and t.get_device() == torch._C._cuda_getDevice():
+        return _HERE
+    if isinstance(stream, torch.cuda.Stream) and stream.device != t.device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors are on {t.device}")
+    return _switch(t.device, stream)
+
+
+_NO_ROWS = (None, 0, 0, 0, None, 0, 0, 0, None, 0)
 
 
 def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: Optional[torch.Tensor],
@@ -762,39 +802,40 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: Opti
     q_out, k_out may be q and k themselves, or the rows of a cache."""
     if q is None and k is None:
         raise ValueError("q and k cannot both be None")
-    for t, nm in ((q, "q"), (k, "k")):
-        if t is not None:
-            _need(t, nm, torch.bfloat16, 4)
-            _extent(t, nm, (None, None, None, 128))
-    B, _, T, D = (k if q is None else q).shape
-    Hq, Hkv = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
-    if q is not None and k is not None:
-        _extent(k, "k", (B, Hkv, T, D))
-    if B < 1 or T < 1 or Hq + Hkv < 1:
-        raise ValueError("q and k must hold at least one row")
+    Hq = Hkv = 0
+    if q is not None:
+        B, Hq, T, _ = _rows(q, "q")
+    if k is not None:
+        kB, Hkv, kT, _ = _rows(k, "k")
+        if q is None:
+            B, T = kB, kT
+        elif kB != B or kT != T:
+            _extent(k, "k", (B, Hkv, T, 128))
     for t, src, nm in ((q_out, q, "q_out"), (k_out, k, "k_out")):
         if t is not None:
             if src is None:
                 raise ValueError(f"{nm} is given without its input")
             _written(t, nm, src.shape)
     rows, R = _table(cos_sin)
-    if R and pos is None:
+    sp = 0
+    if not R:
+        pos = None
+    elif pos is None:
         raise ValueError("pos is required with cos_sin")
-    sp = _ints(pos, "pos", (B, T)) if R else 0
+    else:
+        sp = _indices(pos, "pos", (B, T))
     sq, sk = _norm_weight(wq, "wq", Hq), _norm_weight(wk, "wk", Hkv)
-    _on_gpu(q, k, pos if R else None, cos_sin, wq, wk, q_out, k_out)
-    dev = (k if q is None else q).device
-    with _place(dev, stream):
+    _on_gpu(q, k, pos, cos_sin, wq, wk, q_out, k_out)
+    with _place(k if q is None else q, stream):
         if q is not None and q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+            q_out = q.new_empty(q.shape)
         if k is not None and k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=dev)
-        none = (None, 0, 0, 0, None, 0, 0, 0, None, 0)
+            k_out = k.new_empty(k.shape)
         _check(_lib.bpc_qk_norm_rope(
-            *(none if q is None else (_ptr(q), *_strides3(q), _ptr(q_out), *_strides3(q_out), _ptr(wq), sq)),
-            *(none if k is None else (_ptr(k), *_strides3(k), _ptr(k_out), *_strides3(k_out), _ptr(wk), sk)),
-            B, Hq, Hkv, T, D, float(eps), _ptr(cos_sin), rows, R, int(interleaved), _ptr(pos) if R else None, sp,
-            _stream(stream)), "bpc_qk_norm_rope")
+            *(_NO_ROWS if q is None else (q.data_ptr(), *_strides3(q), q_out.data_ptr(), *_strides3(q_out), _ptr(wq), sq)),
+            *(_NO_ROWS if k is None else (k.data_ptr(), *_strides3(k), k_out.data_ptr(), *_strides3(k_out), _ptr(wk), sk)),
+            B, Hq, Hkv, T, 128, eps, _ptr(cos_sin), rows, R, interleaved, _ptr(pos), sp, _stream(stream)),
+            "bpc_qk_norm_rope")
     return q_out, k_out
 
 
@@ -810,33 +851,30 @@ def append_kv_paged(k_new: torch.Tensor, v_new: torch.Tensor, K: torch.Tensor, V
     on), its key normed with wk and rotated as by qk_norm_rope on the way, by
     its slot or by rope_pos [B, T].  Tokens without a page, or without a row of
     cos_sin, are not stored."""
-    for t, nm in ((k_new, "k_new"), (v_new, "v_new"), (K, "K"), (V, "V")):
-        _need(t, nm, torch.bfloat16, 4)
-    B, Hkv, T, D = k_new.shape
-    pages, _, page, _ = K.shape
-    _extent(k_new, "k_new", (("ge", 1), ("ge", 1), ("ge", 1), 128))
-    _extent(v_new, "v_new", (B, Hkv, T, D))
-    _extent(K, "K", (("ge", 1), Hkv, None, D))
-    _extent(V, "V", (pages, Hkv, page, D))
-    if page < 16 or page > 1 << 20 or page & (page - 1):
-        raise ValueError(f"K: pages of {page} rows, must be a power of two, 16 to 2^20")
+    B, Hkv, T, _ = _rows(k_new, "k_new")
+    if _rows(v_new, "v_new") != k_new.shape:
+        _extent(v_new, "v_new", (B, Hkv, T, 128))
+    pages, Hk, page, _ = _rows(K, "K")
+    if Hk != Hkv:
+        _extent(K, "K", (pages, Hkv, page, 128))
     _written(K, "K", K.shape)
-    _written(V, "V", V.shape)
-    st = _ints(block_table, "block_table", (B, ("ge", 1)))
-    _ints(pos, "pos", (B,))
-    _ints(count, "count", (B,))
+    _written(V, "V", K.shape)
+    _page_rows(page)
+    st, max_pages = _block_table(block_table, B)
+    _indices(pos, "pos", (B,))
+    _indices(count, "count", (B,))
     rows, R = _table(cos_sin)
     if rope_pos is not None and not R:
         raise ValueError("rope_pos needs cos_sin")
-    sr = _ints(rope_pos, "rope_pos", (B, T))
+    sr = _indices(rope_pos, "rope_pos", (B, T))
     sw = _norm_weight(wk, "wk", Hkv)
     _on_gpu(k_new, v_new, K, V, block_table, pos, count, cos_sin, rope_pos, wk)
-    with _place(K.device, stream):
+    with _place(K, stream):
         _check(_lib.bpc_append_kv_paged(
-            _ptr(k_new), *_strides3(k_new), _ptr(v_new), *_strides3(v_new), _ptr(K), *_strides3(K), _ptr(V),
-            *_strides3(V), _ptr(block_table), st, block_table.shape[1], pages, page, _ptr(pos), _ptr(count), B, Hkv, T,
-            D, _ptr(wk), sw, float(eps), _ptr(cos_sin), rows, R, int(interleaved), _ptr(rope_pos), sr,
-            _stream(stream)), "bpc_append_kv_paged")
+            k_new.data_ptr(), *_strides3(k_new), v_new.data_ptr(), *_strides3(v_new), K.data_ptr(), *_strides3(K), V.data_ptr(),
+            *_strides3(V), _ptr(block_table), st, max_pages, pages, page, _ptr(pos), _ptr(count), B, Hkv, T,
+            128, _ptr(wk), sw, eps, _ptr(cos_sin), rows, R, interleaved, _ptr(rope_pos), sr, _stream(stream)),
+            "bpc_append_kv_paged")
 
 
 def prefill_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, D: int = 128) -> int:
@@ -848,14 +886,12 @@ def tree_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, D: int = 128
 
 
 def _attn_inputs(q, K, V, slopes, out, workspace):
-    """Checks shared by prefill_attention and tree_attention; returns the sizes of q and the KV heads."""
-    _need(q, "q", torch.bfloat16, 4)
-    _need(K, "K", torch.bfloat16, 4)
-    _need(V, "V", torch.bfloat16, 4)
-    _extent(q, "q", (("ge", 1), ("ge", 1), ("ge", 1), 128))
-    B, Hq, T, D = q.shape
-    Hkv = K.shape[1]
-    if Hkv < 1 or Hq % Hkv:
+    """Checks shared by prefill_attention and tree_attention; returns the sizes
+    of q and of K."""
+    B, Hq, T, _ = _rows(q, "q")
+    Kb, Hkv, Kn, _ = _rows(K, "K")
+    Vb, Vh, Vn, _ = _rows(V, "V")
+    if Hq % Hkv:
         raise ValueError(f"Hq={Hq} must be a multiple of Hkv={Hkv}")
     if slopes is not None:
         _need(slopes, "slopes", torch.float32, 1)
@@ -864,7 +900,12 @@ def _attn_inputs(q, K, V, slopes, out, workspace):
         _written(out, "out", q.shape)
     if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous uint8 tensor")
-    return B, Hq, Hkv, T, D
+    return B, Hq, Hkv, T, Kb, Kn, Vb, Vh, Vn
+
+
+def _cache_rows(K, V, B, Hkv, N) -> None:
+    _extent(K, "K", (B, Hkv, ("ge", N), 128))
+    _extent(V, "V", (B, Hkv, ("ge", N), 128))
 
 
 def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scale: Optional[float] = None,
@@ -882,34 +923,33 @@ def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scal
     prefix mask.  Scores are capped to softcap * tanh(s / softcap) when softcap
     > 0, then lowered by slopes[head] * distance.  A token that sees nothing
     gets zeros."""
-    B, Hq, Hkv, T, D = _attn_inputs(q, K, V, slopes, out, workspace)
-    N = K.shape[2] if N is None else N
+    B, Hq, Hkv, T, Kb, Kn, Vb, Vh, Vn = _attn_inputs(q, K, V, slopes, out, workspace)
+    N = Kn if N is None else N
     if N < 1:
         raise ValueError(f"N={N} must be >= 1")
-    _extent(K, "K", (B, Hkv, ("ge", N), D))
-    _extent(V, "V", (B, Hkv, ("ge", N), D))
+    if Kb != B or Vb != B or Vh != Hkv or Kn < N or Vn < N:
+        _cache_rows(K, V, B, Hkv, N)
     if pos0 is None:
         if T > N:
             raise ValueError(f"{T} queries are more than the N={N} tokens: pos0 must be given")
         pos0 = N - T
     if not 0 <= pos0 <= 1 << 30:
         raise ValueError(f"pos0={pos0} must be in [0, 2^30]")
-    sb = _ints(key_begin, "key_begin", (B, T))
-    se = _ints(key_end, "key_end", (B, T))
+    sb = _indices(key_begin, "key_begin", (B, T))
+    se = _indices(key_end, "key_end", (B, T))
     _on_gpu(q, K, V, slopes, key_begin, key_end, out, workspace)
     if sm_scale is None:
-        sm_scale = 1.0 / math.sqrt(D)
-    with _place(q.device, stream):
+        sm_scale = 1.0 / math.sqrt(128)
+    with _place(q, stream):
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
         if workspace is None:
-            need = _lib.bpc_prefill_workspace_bytes(B, Hq, Hkv, T, N, D)
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+            need = _lib.bpc_prefill_workspace_bytes(B, Hq, Hkv, T, N, 128)
+            workspace = q.new_empty(need, dtype=torch.uint8) if need else None
         _check(_lib.bpc_prefill_attention(
-            _ptr(q), *_strides3(q), _ptr(K), *_kv_strides(K), _ptr(V), *_kv_strides(V), B, Hq, Hkv, T, N, pos0, D,
-            float(sm_scale), float(softcap), _ptr(slopes), _ptr(key_begin), sb, _ptr(key_end), se, _ptr(out),
-            *_strides3(out), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)),
-            "bpc_prefill_attention")
+            q.data_ptr(), *_strides3(q), K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], B, Hq, Hkv, T, N, pos0, 128,
+            sm_scale, softcap, _ptr(slopes), _ptr(key_begin), sb, _ptr(key_end), se, out.data_ptr(), *_strides3(out),
+            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "bpc_prefill_attention")
     return out
 
 
@@ -931,39 +971,38 @@ def tree_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torc
     being lens[b] plus its depth.  A sequence whose lens[b] is not in [0, N - T]
     is skipped: its rows of `out` stay as they are (undefined where `out` is
     allocated here)."""
-    B, Hq, Hkv, T, D = _attn_inputs(q, K, V, slopes, out, workspace)
+    B, Hq, Hkv, T, Kb, Kn, Vb, Vh, Vn = _attn_inputs(q, K, V, slopes, out, workspace)
+    pages = page = st = 0
     if block_table is None:
-        N = K.shape[2] if N is None else N
-        _extent(K, "K", (B, Hkv, ("ge", N), D))
-        _extent(V, "V", (B, Hkv, ("ge", N), D))
-        pages = page = st = 0
+        N = Kn if N is None else N
+        if Kb != B or Vb != B or Vh != Hkv or Kn < N or Vn < N:
+            _cache_rows(K, V, B, Hkv, N)
     else:
-        pages, _, page, _ = K.shape
-        _extent(K, "K", (("ge", 1), Hkv, None, D))
-        _extent(V, "V", (pages, Hkv, page, D))
-        if page < 16 or page > 1 << 20 or page & (page - 1):
-            raise ValueError(f"K: pages of {page} rows, must be a power of two, 16 to 2^20")
-        st = _ints(block_table, "block_table", (B, ("ge", 1)))
-        most = block_table.shape[1] * page
+        pages, page = Kb, Kn
+        if Vb != pages or Vh != Hkv or Vn != page:
+            _extent(V, "V", (pages, Hkv, page, 128))
+        _page_rows(page)
+        st, most = _block_table(block_table, B)
+        most *= page
         N = min(most, 1 << 30) if N is None else N
         if N > most:
             raise ValueError(f"N={N}: the block_table holds {most} slots per sequence")
     if not 1 <= T <= min(64, N):
         raise ValueError(f"T={T} drafted tokens: must be 1 to 64, and at most N={N}")
-    _ints(lens, "lens", (B,))
-    sm = _ints(tree, "tree", (B, T), torch.int64)
+    _indices(lens, "lens", (B,))
+    sm = _indices(tree, "tree", (B, T), torch.int64)
     _on_gpu(q, K, V, lens, tree, block_table, slopes, out, workspace)
     if sm_scale is None:
-        sm_scale = 1.0 / math.sqrt(D)
-    with _place(q.device, stream):
+        sm_scale = 1.0 / math.sqrt(128)
+    with _place(q, stream):
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
         if workspace is None:
-            need = _lib.bpc_tree_workspace_bytes(B, Hq, Hkv, T, N, D)
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+            need = _lib.bpc_tree_workspace_bytes(B, Hq, Hkv, T, N, 128)
+            workspace = q.new_empty(need, dtype=torch.uint8) if need else None
         _check(_lib.bpc_tree_attention(
-            _ptr(q), *_strides3(q), _ptr(K), *_kv_strides(K), _ptr(V), *_kv_strides(V), _ptr(block_table), st, pages,
-            page, _ptr(lens), _ptr(tree), sm, B, Hq, Hkv, T, N, D, float(sm_scale), float(softcap), _ptr(slopes),
-            _ptr(out), *_strides3(out), _ptr(workspace), 0 if workspace is None else workspace.numel(),
-            _stream(stream)), "bpc_tree_attention")
+            q.data_ptr(), *_strides3(q), K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], _ptr(block_table), st, pages,
+            page, lens.data_ptr(), _ptr(tree), sm, B, Hq, Hkv, T, N, 128, sm_scale, softcap, _ptr(slopes), out.data_ptr(),
+            *_strides3(out), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)),
+            "bpc_tree_attention")
     return out

@@ -18,6 +18,8 @@
 // chunk ^ swz(row): eight consecutive rows' equal chunks (the K operand) and
 // four consecutive rows' neighbouring chunk pairs (the transposing reads that
 // make the V operand) then lie in different banks.
+#include <atomic>
+
 #include "bpc_internal.h"
 
 namespace bpc {
@@ -514,6 +516,17 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
   *reinterpret_cast<uint32_t*>(op + 2 * lane) = cvt_pk_bf16(x0 * inv, x1 * inv);
 }
 
+static hipError_t allow_lds(const void* f, int bytes, std::atomic<uint64_t>& allowed) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev < 64 && (allowed.load() & bit)) return hipSuccess;
+  e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess && dev < 64) allowed.fetch_or(bit);
+  return e;
+}
+
 template <int RB, int KW, int KT, bool TREE>
 static hipError_t launch_attn_shape(const AttnArgs& a) {
   const int rows = a.T * a.G, nrb = (rows + RB * kBlockRows - 1) / (RB * kBlockRows);
@@ -523,8 +536,8 @@ static hipError_t launch_attn_shape(const AttnArgs& a) {
   {                                                                                                               \
     auto* f = attn_kernel<RB, KW, KT, TREE, CAP, BIAS>;                                                           \
     constexpr int lds = AttnShape<RB, KW, KT, TREE, CAP, BIAS>::kLds;                                             \
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, lds); \
-    if (e != hipSuccess) return e;                                                                                \
+    static std::atomic<uint64_t> allowed{0}; /* devices on which the kernel may use that much LDS */               \
+    if (hipError_t e = allow_lds(reinterpret_cast<const void*>(f), lds, allowed); e != hipSuccess) return e;      \
     f<<<grid, RB * KW * 64, lds, a.stream>>>(a, nrb, items);                                                      \
   }
   if (a.softcap > 0.f) {

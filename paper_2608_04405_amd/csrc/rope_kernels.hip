@@ -2,21 +2,34 @@
 // rotation by its token's position, and the store to a tensor or to a page.
 //
 // A row of 128 bf16 is 16 lanes of 16 bytes, so that a wavefront works on four
-// rows (heads) of one token at once.  The mean of squares is a sum over 16
-// lanes; the partner of coordinate d in a rotation by halves (d +- R/2) lies
-// R / 16 lanes away and is fetched with one shuffle per 4 bytes of the raw row
-// (the norm's factor is the same for both), that of a rotation in adjacent
-// pairs lies in the same lane.  A lane holds the cosines and sines of its eight
-// coordinates for all heads of the token.
+// rows (heads) of one token at once, a "pass", and goes through the token's
+// heads pass by pass.  With the norm's factor r, the weights w and the token's
+// cosines and sines every coordinate becomes
+//     y_e = r (v_e C_e + u_e S_e),   C_e = w_e c,   S_e = -+ w_u s,
+// u its partner in the pair: C and S hold for all heads of the token, so a row
+// costs two multiply-adds and a product per coordinate, the mean of squares (a
+// sum over 16 lanes by DPP rotations, equal in all of them), and the partner's
+// raw values: R / 16 lanes away for pairs (i, i + R/2), where R = 128 is one
+// DPP rotation by eight lanes, or in the same 32-bit word for adjacent pairs.
+// Bound by memory: the loads of kRopeBatch passes are issued before the first is
+// used.
 #include "bpc_internal.h"
 
 namespace bpc {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWaves = kRopeThreads / 64;
-constexpr int kRowLanes = kHeadDim / 8;     // lanes per row
-constexpr int kRowsPerPass = 64 / kRowLanes;  // rows of a wavefront at once
-constexpr int kRopeBatch = 4;               // passes whose loads are issued before the first is used
+constexpr int kRowLanes = kHeadDim / 8;       // lanes per row
+constexpr int kPassRows = 64 / kRowLanes;     // rows of a pass
+constexpr int kRopeBatch = 4;                 // passes whose loads are issued before the first is used
+
+// where the partner of a coordinate lies
+enum Pairing {
+  kPairNone,     // no rotation
+  kPairEight,    // eight lanes on: halves of R = 128
+  kPairLanes,    // R / 16 lanes on: halves of a smaller R
+  kPairAdjacent  // in the same word
+};
 
 // The bf16 nearest to x, ties to even (the compiler's conversion instruction).
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -28,161 +41,214 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ float lo_f32(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f32(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// What a lane keeps for the rows of one token and one tensor: its eight norm
-// weights, its partner's, and the token's cosines and sines (of the lane's four
-// pairs in the first four entries where pairs are adjacent).
-struct RopeLane {
+// x of the lane N further on (mod 16) within the 16 lanes of a row
+template <int N>
+__device__ __forceinline__ uint32_t row_rotate(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + N, 0xF, 0xF, true);
+}
+template <int N>
+__device__ __forceinline__ float row_rotate_add(float x) {
+  return x + __uint_as_float(row_rotate<N>(__float_as_uint(x)));
+}
+
+__device__ __forceinline__ void unpack8(const uint4& x, float v[8]) {
+  v[0] = lo_f32(x.x), v[1] = hi_f32(x.x), v[2] = lo_f32(x.y), v[3] = hi_f32(x.y);
+  v[4] = lo_f32(x.z), v[5] = hi_f32(x.z), v[6] = lo_f32(x.w), v[7] = hi_f32(x.w);
+}
+
+// a lane's place in the rotation of its token: cosines and signed sines of its
+// eight coordinates (1 and 0 outside), and its partner's lane
+struct Turn {
   float c[8], s[8];
-  int partner;  // lane of the partner chunk (itself outside the rotation)
-  bool turn;    // the lane's coordinates are rotated
+  int partner;
+  uint32_t keep;  // all ones where the partner counts
 };
 
-__device__ __forceinline__ RopeLane rope_lane(const float* __restrict__ cs, int R, int inter) {
-  RopeLane r;
-  const int lane = threadIdx.x & 63, j = lane % kRowLanes;
-  r.turn = 8 * j < R;
-  r.partner = lane;
+template <Pairing PAIR>
+__device__ __forceinline__ Turn token_turn(const float* __restrict__ cs, int R) {
+  Turn r;
+  const int lane = threadIdx.x & 63, j = lane % kRowLanes, half = R / 2;
+  r.partner = lane, r.keep = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) r.c[e] = 1.f, r.s[e] = 0.f;
-  if (!r.turn) return r;
-  const int half = R / 2;
-  if (inter) {
+  if (PAIR == kPairNone || 8 * j >= R) return r;
+  r.keep = 0xFFFFFFFFu;
+  if (PAIR == kPairAdjacent) {
     const float4 c = *reinterpret_cast<const float4*>(cs + 4 * j), s = *reinterpret_cast<const float4*>(cs + half + 4 * j);
-    r.c[0] = c.x, r.c[1] = c.y, r.c[2] = c.z, r.c[3] = c.w;
-    r.s[0] = s.x, r.s[1] = s.y, r.s[2] = s.z, r.s[3] = s.w;
+    const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      r.c[2 * e] = r.c[2 * e + 1] = cc[e];
+      r.s[2 * e] = -ss[e], r.s[2 * e + 1] = ss[e];
+    }
     return r;
   }
   const int hl = R / 16;  // lanes per half
   const bool second = j >= hl;
   r.partner = second ? lane - hl : lane + hl;
-  const float4* pc = reinterpret_cast<const float4*>(cs + 8 * (second ? j - hl : j));
-  const float4* ps = reinterpret_cast<const float4*>(cs + half + 8 * (second ? j - hl : j));
+  const int f = 8 * (second ? j - hl : j);
+  const float4* pc = reinterpret_cast<const float4*>(cs + f);
+  const float4* ps = reinterpret_cast<const float4*>(cs + half + f);
   const float4 c0 = pc[0], c1 = pc[1], s0 = ps[0], s1 = ps[1];
-  const float g = second ? 1.f : -1.f;  // x1 c - x2 s, x2 c + x1 s
-  r.c[0] = c0.x, r.c[1] = c0.y, r.c[2] = c0.z, r.c[3] = c0.w;
-  r.c[4] = c1.x, r.c[5] = c1.y, r.c[6] = c1.z, r.c[7] = c1.w;
-  r.s[0] = g * s0.x, r.s[1] = g * s0.y, r.s[2] = g * s0.z, r.s[3] = g * s0.w;
-  r.s[4] = g * s1.x, r.s[5] = g * s1.y, r.s[6] = g * s1.z, r.s[7] = g * s1.w;
+  const float cc[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+  const float ss[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r.c[e] = cc[e], r.s[e] = second ? ss[e] : -ss[e];
   return r;
 }
 
-// Norm (with `w`, the row's 128 weights, else none) and rotation of the row
-// whose chunk `x` this lane holds; every lane of the wavefront calls it.
-__device__ __forceinline__ uint4 rope_row(uint4 x, const uint16_t* w, float eps, const RopeLane& rl, int R, int inter) {
-  const uint32_t xr[4] = {x.x, x.y, x.z, x.w};
-  float v[8];
+// C and S of a row with weights w (or none)
+template <Pairing PAIR>
+__device__ __forceinline__ void row_factors(const Turn& t, const uint16_t* w, float C[8], float S[8]) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[2 * e] = lo_f32(xr[e]), v[2 * e + 1] = hi_f32(xr[e]);
-  float rstd = 1.f;
-  if (w) {
+  for (int e = 0; e < 8; ++e) C[e] = t.c[e], S[e] = t.s[e];
+  if (!w) return;
+  float wv[8], wu[8];
+  unpack8(*reinterpret_cast<const uint4*>(w + 8 * (threadIdx.x % kRowLanes)), wv);
+  if (PAIR == kPairAdjacent) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) wu[e] = wv[e ^ 1];
+  } else if (PAIR != kPairNone) {
+    unpack8(*reinterpret_cast<const uint4*>(w + 8 * (t.partner % kRowLanes)), wu);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    C[e] *= wv[e];
+    if (PAIR != kPairNone) S[e] *= wu[e];
+  }
+}
+
+// the row whose chunk `x` this lane holds; every lane of the wavefront calls it
+template <Pairing PAIR>
+__device__ __forceinline__ uint4 turn_row(const uint4& x, bool norm, float eps, const Turn& t, const float C[8], const float S[8]) {
+  float v[8], y[8];
+  unpack8(x, v);
+  float r = 1.f;
+  if (norm) {
     float ss = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fmaf(v[e], v[e], ss);
-#pragma unroll
-    for (int o = 1; o < kRowLanes; o <<= 1) ss += __shfl_xor(ss, o, 64);
-    rstd = rsqrtf(ss * (1.f / kHeadDim) + eps);
+    ss = row_rotate_add<1>(row_rotate_add<2>(row_rotate_add<4>(row_rotate_add<8>(ss))));
+    r = rsqrtf(fmaf(ss, 1.f / kHeadDim, eps));
   }
-  const int j = threadIdx.x % kRowLanes;
-  if (w) {
-    const uint4 wx = *reinterpret_cast<const uint4*>(w + 8 * j);
-    const uint32_t wr[4] = {wx.x, wx.y, wx.z, wx.w};
+  if (PAIR == kPairNone) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[2 * e] *= rstd * lo_f32(wr[e]), v[2 * e + 1] *= rstd * hi_f32(wr[e]);
-  }
-  float y[8];
-  if (R == 0) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = v[e];
-  } else if (inter) {
+    for (int e = 0; e < 8; ++e) y[e] = v[e] * C[e];
+  } else {
+    const uint32_t xr[4] = {x.x, x.y, x.z, x.w};
+    float u[8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float a = v[2 * e], b = v[2 * e + 1];
-      y[2 * e] = rl.turn ? a * rl.c[e] - b * rl.s[e] : a;
-      y[2 * e + 1] = rl.turn ? b * rl.c[e] + a * rl.s[e] : b;
-    }
-  } else {
-    float u[8];
-    uint32_t pr[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) pr[e] = (uint32_t)__shfl((int)xr[e], rl.partner, 64);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) u[2 * e] = lo_f32(pr[e]), u[2 * e + 1] = hi_f32(pr[e]);
-    if (w) {
-      const uint4 wx = *reinterpret_cast<const uint4*>(w + 8 * (rl.partner % kRowLanes));
-      const uint32_t wr[4] = {wx.x, wx.y, wx.z, wx.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) u[2 * e] *= rstd * lo_f32(wr[e]), u[2 * e + 1] *= rstd * hi_f32(wr[e]);
+      uint32_t p;
+      if (PAIR == kPairAdjacent) p = __builtin_amdgcn_alignbit(xr[e], xr[e], 16);
+      if (PAIR == kPairEight) p = row_rotate<8>(xr[e]);
+      if (PAIR == kPairLanes) p = (uint32_t)__shfl((int)xr[e], t.partner, 64);
+      if (PAIR != kPairEight) p &= t.keep;  // outside the rotation: no partner, whatever its value
+      u[2 * e] = lo_f32(p), u[2 * e + 1] = hi_f32(p);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = rl.turn ? v[e] * rl.c[e] + u[e] * rl.s[e] : v[e];
+    for (int e = 0; e < 8; ++e) y[e] = fmaf(u[e], S[e], v[e] * C[e]);
   }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] *= r;
   return make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
 }
 
+// rows of `H` heads of one token, passes [p0, p1): from `src` with head stride
+// ss, to `dst` with head stride sd; PER_HEAD: weights of their own for every head
+template <Pairing PAIR, bool PER_HEAD>
+__device__ __forceinline__ void turn_heads(const uint16_t* src, int64_t ss, uint16_t* dst, int64_t sd, const uint16_t* w,
+                                           int64_t sw, float eps, const Turn& t, int H, int p0, int p1) {
+  const int lane = threadIdx.x & 63, sub = lane / kRowLanes, d0 = 8 * (lane % kRowLanes);
+  float C[8], S[8];
+  if (!PER_HEAD) row_factors<PAIR>(t, w, C, S);
+  for (int p = p0; p < p1; p += kRopeBatch) {
+    uint4 x[kRopeBatch];
+#pragma unroll
+    for (int i = 0; i < kRopeBatch; ++i) {
+      const int h = min((p + i) * kPassRows + sub, H - 1);
+      x[i] = *reinterpret_cast<const uint4*>(src + h * ss + d0);
+    }
+#pragma unroll
+    for (int i = 0; i < kRopeBatch; ++i) {
+      if (p + i >= p1) break;
+      const int h = (p + i) * kPassRows + sub;
+      if (PER_HEAD) row_factors<PAIR>(t, w ? w + min(h, H - 1) * sw : nullptr, C, S);
+      const uint4 y = turn_row<PAIR>(x[i], w != nullptr, eps, t, C, S);
+      if (h < H) *reinterpret_cast<uint4*>(dst + h * sd + d0) = y;
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------
-// qk_norm_rope: a wavefront takes one token and up to `per` of its heads, the
-// query heads before the key heads.  Bound by memory.
+// qk_norm_rope: a wavefront takes `per` of the passes of one token, those of the
+// query heads before those of the key heads
 // ---------------------------------------------------------------------------
+template <Pairing PAIR, bool PER_HEAD>
 __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, int per, int parts) {
   const int64_t wave = (int64_t)blockIdx.x * kRopeWaves + (threadIdx.x >> 6);
   const int64_t tok = wave / parts;
   if (tok >= (int64_t)a.B * a.T) return;
-  const int h0 = (int)(wave - tok * parts) * per;
   const int b = (int)(tok / a.T), t = (int)(tok - (int64_t)b * a.T);
-  const int lane = threadIdx.x & 63, sub = lane / kRowLanes, d0 = 8 * (lane % kRowLanes);
   const float* cs = nullptr;
-  if (a.R) {
+  if (PAIR != kPairNone) {
     const int p = a.pos[b * a.sp_b + t];
     if (p < 0 || p >= a.table_rows) return;  // no such position: the token's rows stay as they are
     cs = a.cos_sin + (int64_t)p * a.R;
   }
-  const RopeLane rl = rope_lane(cs, a.R, a.inter);
-  const int H = a.q.H + a.k.H, h1 = min(H, h0 + per);
-  for (int hb = h0; hb < h1; hb += kRopeBatch * kRowsPerPass) {
-    uint4 x[kRopeBatch];
-    uint16_t* dst[kRopeBatch];
-    const uint16_t* w[kRopeBatch];
-#pragma unroll
-    for (int i = 0; i < kRopeBatch; ++i) {
-      const int h = min(hb + i * kRowsPerPass + sub, h1 - 1);
-      const RopeTensor& s = h < a.q.H ? a.q : a.k;
-      const int hh = h < a.q.H ? h : h - a.q.H;
-      x[i] = *reinterpret_cast<const uint4*>(s.in + b * s.si_b + hh * s.si_h + t * s.si_t + d0);
-      dst[i] = s.out + b * s.so_b + hh * s.so_h + t * s.so_t + d0;
-      w[i] = s.w ? s.w + hh * s.sw_h : nullptr;
-    }
-#pragma unroll
-    for (int i = 0; i < kRopeBatch; ++i) {
-      if (hb + i * kRowsPerPass >= h1) break;
-      const uint4 y = rope_row(x[i], w[i], a.eps, rl, a.R, a.inter);
-      if (hb + i * kRowsPerPass + sub < h1) *reinterpret_cast<uint4*>(dst[i]) = y;
-    }
-  }
+  const Turn turn = token_turn<PAIR>(cs, a.R);
+  const int nq = (a.q.H + kPassRows - 1) / kPassRows, nk = (a.k.H + kPassRows - 1) / kPassRows;
+  const int p0 = (int)(wave - tok * parts) * per, p1 = min(nq + nk, p0 + per);
+  if (p0 < nq)
+    turn_heads<PAIR, PER_HEAD>(a.q.in + b * a.q.si_b + t * a.q.si_t, a.q.si_h, a.q.out + b * a.q.so_b + t * a.q.so_t,
+                               a.q.so_h, a.q.w, a.q.sw_h, a.eps, turn, a.q.H, p0, min(p1, nq));
+  if (p1 > nq)
+    turn_heads<PAIR, PER_HEAD>(a.k.in + b * a.k.si_b + t * a.k.si_t, a.k.si_h, a.k.out + b * a.k.so_b + t * a.k.so_t,
+                               a.k.so_h, a.k.w, a.k.sw_h, a.eps, turn, a.k.H, max(p0 - nq, 0), p1 - nq);
 }
 
-hipError_t launch_qk_norm_rope(const RopeArgs& a) {
-  const int H = a.q.H + a.k.H;
-  const int64_t tokens = (int64_t)a.B * a.T;
-  int per = H, parts = 1;
-  // few tokens: their heads are spread over wavefronts
-  while (per > kRowsPerPass && tokens * parts < 2048) {
-    per = ((per + 1) / 2 + kRowsPerPass - 1) / kRowsPerPass * kRowsPerPass;
-    parts = (H + per - 1) / per;
+// Passes per wavefront: all of a token's, or while the wavefronts are few, down
+// to one (a wavefront per SIMD and more hide each other's latency).
+static int passes_per_wave(int64_t tokens, int passes) {
+  int per = passes;
+  while (per > 1 && tokens * ((passes + per - 1) / per) < 4096) per = (per + 1) / 2;
+  return per;
+}
+
+static Pairing pairing_of(int R, int inter) {
+  return R == 0 ? kPairNone : inter ? kPairAdjacent : R == kHeadDim ? kPairEight : kPairLanes;
+}
+
+#define BPC_BY_PAIRING(KERNEL, PER_HEAD, ...)                                                          \
+  switch (pairing_of(a.R, a.inter)) {                                                                  \
+    case kPairNone: KERNEL<kPairNone, PER_HEAD><<<grid, kRopeThreads, 0, a.stream>>>(__VA_ARGS__); break;   \
+    case kPairEight: KERNEL<kPairEight, PER_HEAD><<<grid, kRopeThreads, 0, a.stream>>>(__VA_ARGS__); break; \
+    case kPairLanes: KERNEL<kPairLanes, PER_HEAD><<<grid, kRopeThreads, 0, a.stream>>>(__VA_ARGS__); break; \
+    case kPairAdjacent: KERNEL<kPairAdjacent, PER_HEAD><<<grid, kRopeThreads, 0, a.stream>>>(__VA_ARGS__); break; \
   }
-  const int64_t waves = tokens * parts;
-  qk_norm_rope_kernel<<<(unsigned)((waves + kRopeWaves - 1) / kRopeWaves), kRopeThreads, 0, a.stream>>>(a, per, parts);
+
+hipError_t launch_qk_norm_rope(const RopeArgs& a) {
+  const int passes = (a.q.H + kPassRows - 1) / kPassRows + (a.k.H + kPassRows - 1) / kPassRows;
+  const int64_t tokens = (int64_t)a.B * a.T;
+  const int per = passes_per_wave(tokens, passes), parts = (passes + per - 1) / per;
+  const unsigned grid = (unsigned)((tokens * parts + kRopeWaves - 1) / kRopeWaves);
+  if ((a.q.w && a.q.sw_h) || (a.k.w && a.k.sw_h)) {
+    BPC_BY_PAIRING(qk_norm_rope_kernel, true, a, per, parts)
+  } else {
+    BPC_BY_PAIRING(qk_norm_rope_kernel, false, a, per, parts)
+  }
   return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------
 // append_kv_paged: as above, the key heads (normed and rotated) before the
-// value heads (copied), stored at the token's row of its page.
+// value heads (copied), stored at the token's row of its page
 // ---------------------------------------------------------------------------
+template <Pairing PAIR, bool PER_HEAD>
 __global__ __launch_bounds__(kRopeThreads) void append_paged_kernel(AppendPagedArgs a, int per, int parts) {
   const int64_t wave = (int64_t)blockIdx.x * kRopeWaves + (threadIdx.x >> 6);
   const int64_t tok = wave / parts;
   if (tok >= (int64_t)a.B * a.T) return;
-  const int h0 = (int)(wave - tok * parts) * per;
   const int b = (int)(tok / a.T), t = (int)(tok - (int64_t)b * a.T);
   if (a.count && t >= a.count[b]) return;
   const int64_t slot = (int64_t)a.pos[b] + t;
@@ -191,53 +257,46 @@ __global__ __launch_bounds__(kRopeThreads) void append_paged_kernel(AppendPagedA
   if (page < 0 || page >= a.num_pages) return;
   const int64_t row = slot & ((1 << a.page_shift) - 1);
   const float* cs = nullptr;
-  if (a.R) {
+  if (PAIR != kPairNone) {
     const int64_t p = a.rope_pos ? a.rope_pos[b * a.sr_b + t] : slot;
     if (p < 0 || p >= a.table_rows) return;
     cs = a.cos_sin + p * a.R;
   }
-  const int lane = threadIdx.x & 63, sub = lane / kRowLanes, d0 = 8 * (lane % kRowLanes);
-  const RopeLane rl = rope_lane(cs, a.R, a.inter);
-  const int H = 2 * a.Hkv, h1 = min(H, h0 + per);
-  for (int hb = h0; hb < h1; hb += kRopeBatch * kRowsPerPass) {
-    uint4 x[kRopeBatch];
+  const int n = (a.Hkv + kPassRows - 1) / kPassRows;
+  const int p0 = (int)(wave - tok * parts) * per, p1 = min(2 * n, p0 + per);
+  if (p0 < n)
+    turn_heads<PAIR, PER_HEAD>(a.kn + b * a.skn_b + t * a.skn_t, a.skn_h, a.K + page * a.sK_p + row * a.sK_n, a.sK_h,
+                               a.wk, a.sw_h, a.eps, token_turn<PAIR>(cs, a.R), a.Hkv, p0, min(p1, n));
+  if (p1 > n) {
+    const int lane = threadIdx.x & 63, sub = lane / kRowLanes, d0 = 8 * (lane % kRowLanes);
+    const uint16_t* src = a.vn + b * a.svn_b + t * a.svn_t + d0;
+    uint16_t* dst = a.V + page * a.sV_p + row * a.sV_n + d0;
+    for (int p = max(p0 - n, 0); p < p1 - n; p += kRopeBatch) {
+      uint4 x[kRopeBatch];
 #pragma unroll
-    for (int i = 0; i < kRopeBatch; ++i) {
-      const int h = min(hb + i * kRowsPerPass + sub, h1 - 1);
-      const uint16_t* src = h < a.Hkv ? a.kn + b * a.skn_b + h * a.skn_h + t * a.skn_t
-                                      : a.vn + b * a.svn_b + (h - a.Hkv) * a.svn_h + t * a.svn_t;
-      x[i] = *reinterpret_cast<const uint4*>(src + d0);
-    }
+      for (int i = 0; i < kRopeBatch; ++i)
+        x[i] = *reinterpret_cast<const uint4*>(src + min((p + i) * kPassRows + sub, a.Hkv - 1) * a.svn_h);
 #pragma unroll
-    for (int i = 0; i < kRopeBatch; ++i) {
-      if (hb + i * kRowsPerPass >= h1) break;
-      const int h = hb + i * kRowsPerPass + sub;
-      uint4 y = x[i];
-      if (hb + i * kRowsPerPass < a.Hkv && (a.R || a.wk)) {  // some of the wavefront's rows are keys
-        const int hk = min(h, a.Hkv - 1);
-        const uint4 turned = rope_row(x[i], a.wk ? a.wk + hk * a.sw_h : nullptr, a.eps, rl, a.R, a.inter);
-        if (h < a.Hkv) y = turned;
-      }
-      if (h < h1) {
-        uint16_t* dst = h < a.Hkv ? a.K + page * a.sK_p + h * a.sK_h + row * a.sK_n
-                                  : a.V + page * a.sV_p + (h - a.Hkv) * a.sV_h + row * a.sV_n;
-        *reinterpret_cast<uint4*>(dst + d0) = y;
+      for (int i = 0; i < kRopeBatch; ++i) {
+        const int h = (p + i) * kPassRows + sub;
+        if (p + i < p1 - n && h < a.Hkv) *reinterpret_cast<uint4*>(dst + h * a.sV_h) = x[i];
       }
     }
   }
 }
 
 hipError_t launch_append_paged(const AppendPagedArgs& a) {
-  const int H = 2 * a.Hkv;
+  const int passes = 2 * ((a.Hkv + kPassRows - 1) / kPassRows);
   const int64_t tokens = (int64_t)a.B * a.T;
-  int per = H, parts = 1;
-  while (per > kRowsPerPass && tokens * parts < 2048) {
-    per = ((per + 1) / 2 + kRowsPerPass - 1) / kRowsPerPass * kRowsPerPass;
-    parts = (H + per - 1) / per;
+  const int per = passes_per_wave(tokens, passes), parts = (passes + per - 1) / per;
+  const unsigned grid = (unsigned)((tokens * parts + kRopeWaves - 1) / kRopeWaves);
+  if (a.wk && a.sw_h) {
+    BPC_BY_PAIRING(append_paged_kernel, true, a, per, parts)
+  } else {
+    BPC_BY_PAIRING(append_paged_kernel, false, a, per, parts)
   }
-  const int64_t waves = tokens * parts;
-  append_paged_kernel<<<(unsigned)((waves + kRopeWaves - 1) / kRopeWaves), kRopeThreads, 0, a.stream>>>(a, per, parts);
   return hipGetLastError();
 }
+#undef BPC_BY_PAIRING
 
 }  // namespace bpc

@@ -74,7 +74,7 @@ def test_good_shapes_reach_the_device_check(bpc):
     (dict(q=z(2, 8, 5, 128, dtype=torch.float16)), "q"),
     (dict(k=z(3, 2, 5, 128)), "k"),
     (dict(k=z(2, 2, 4, 128)), "k"),
-    (dict(q=z(2, 8, 0, 128), k=None, pos=z(2, 0, dtype=i32)), "row"),
+    (dict(q=z(2, 8, 0, 128), k=None, pos=z(2, 0, dtype=i32)), "q"),
     (dict(pos=None), "pos"),
     (dict(pos=z(2, 4, dtype=i32)), "pos"),
     (dict(pos=z(2, 5, dtype=i64)), "pos"),
