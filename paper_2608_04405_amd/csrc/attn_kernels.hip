@@ -19,6 +19,7 @@
 // four consecutive rows' neighbouring chunk pairs (the transposing reads that
 // make the V operand) then lie in different banks.
 #include <atomic>
+#include <type_traits>
 
 #include "bpc_internal.h"
 
@@ -27,6 +28,7 @@ namespace bpc {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -75,9 +77,25 @@ __device__ __forceinline__ void dma_wait() {  // until at most N copies of this 
 }
 __device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
 
+// LDS at `at` + a constant, which goes into the instruction
 template <typename T>
-__device__ __forceinline__ T lds_read(uint32_t at) {
-  return *(__attribute__((address_space(3))) T*)at;
+__device__ __forceinline__ T lds_read(uint32_t at, int offset) {
+  return *(__attribute__((address_space(3))) T*)((lds_char*)at + offset);
+}
+// four rows' columns: lane i of each 16 gets column i of the 4 x 16 block whose
+// row i / 4, columns 4 (i % 4) .. + 3 it addresses
+__device__ __forceinline__ s16x4 lds_read_tr(uint32_t at, int offset) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)((lds_char*)at + offset));
+}
+// a value equal in all lanes, in scalar registers
+__device__ __forceinline__ uint64_t uniform64(uint64_t x) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) |
+         (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
+}
+// x, as a value that the compiler does not take apart again
+__device__ __forceinline__ uint32_t opaque(uint32_t x) {
+  asm("" : "+v"(x));
+  return x;
 }
 
 // a value that every lane reads at the same address, through the scalar cache
@@ -102,6 +120,7 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
   constexpr int RPW = KT / RB;  // rows of a tile's K (and V) that a wavefront copies
   static_assert(RPW % 4 == 0, "a copy moves four rows");
   extern __shared__ char smem[];
+  __shared__ uint64_t odd_rows[2][RB * KW];
   __shared__ int draft_place[TREE && BIAS ? 64 : 1];
   // consecutive workgroups go to different XCDs; give each XCD a run of
   // consecutive items, which share their keys in its L2
@@ -119,19 +138,23 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
 
   // ---- the keys that any row of the workgroup sees -------------------------
   int klo = 0, khi = 0, len = 0;
+  int wg_all_lo = 0, wg_all_hi = 0;  // and those that every row sees
   if (TREE) {
     len = a.lens[b];
     if (len < 0 || len > a.N - a.T) return;  // no such sequence: its rows stay as they are
     khi = len + a.T;
+    wg_all_hi = len;
   } else {
     const int t0 = wg_row0 / G, t1 = min(rows - 1, wg_row0 + RB * kBlockRows - 1) / G;
-    int lo = INT32_MAX, hi = 0;
+    int lo = INT32_MAX, hi = 0, all_lo = 0, all_hi = INT32_MAX;
     for (int t = t0 + lane; t <= t1; t += 64) {
       const int f = a.key_begin ? max(a.key_begin[b * a.s_begin + t], 0) : 0;
       const int e = a.key_end ? min(a.key_end[b * a.s_end + t], a.N) : (int)min((int64_t)a.N, (int64_t)a.pos0 + t + 1);
       if (f < e) lo = min(lo, f), hi = max(hi, e);
+      all_lo = max(all_lo, f), all_hi = min(all_hi, e);
     }
     klo = wave_min(lo), khi = wave_max(hi);
+    wg_all_lo = wave_max(all_lo), wg_all_hi = wave_min(all_hi);
     if (klo >= khi) klo = khi = 0;
   }
 
@@ -257,20 +280,23 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
   const float c1 = a.sm_scale * kLog2e;
   const float cap2 = a.softcap * kLog2e, capk = CAP ? 2.f * kLog2e * a.sm_scale / a.softcap : 0.f;
 
-  auto compute = [&](int it, int buf) {
+  auto compute = [&](int it, int buf, uint64_t odd) {
     const int n0 = base0 + (it * KW + grp) * KT;
     if (n0 >= any_hi || n0 + KT <= any_lo) return;
-    const bool full = n0 >= all_lo && n0 + KT <= all_hi && !bad_pages;
+    const bool full = n0 >= all_lo && n0 + KT <= all_hi && !bad_pages;  // every row sees every key
     const uint32_t bo = buf * S::kTileBytes;
+    uint32_t ka[8], va[4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ka[i] = opaque(kaddr[i] + bo);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) va[i] = opaque(vaddr[i] + bo);
     f32x16 acc[NB];
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[k][e] = 0.f;
-#pragma unroll
       for (int s = 0; s < 8; ++s) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, lds_read<u32x4>(kaddr[s] + bo + k * 32 * kRowBytes));
-        acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], acc[k], 0, 0, 0);
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, lds_read<u32x4>(ka[s], k * 32 * kRowBytes));
+        acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], s ? acc[k] : f32x16{}, 0, 0, 0);
       }
     }
     // key of score e of block k: n0 + 32 k + 8 (e / 4) + 4 half + e % 4
@@ -341,69 +367,93 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
       }
     }
     const float mu = mrun == -INFINITY ? 0.f : mrun;
+    u32x4 pw[NB][2];
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float p = __builtin_amdgcn_exp2f((CAP || BIAS) ? acc[k][e] - mu : fmaf(acc[k][e], c1, -mu));
-        acc[k][e] = p;
-        lsum += p;
+      for (int e = 0; e < 16; e += 2) {
+        float p[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          p[i] = __builtin_amdgcn_exp2f((CAP || BIAS) ? acc[k][e + i] - mu : fmaf(acc[k][e + i], c1, -mu));
+        const bf16x2 pp = {(__bf16)p[0], (__bf16)p[1]};
+        lsum = __builtin_amdgcn_fdot2_f32_bf16(pp, bf16x2{(__bf16)1.f, (__bf16)1.f}, lsum, false);
+        pw[k][e / 8][e % 8 / 2] = __builtin_bit_cast(uint32_t, pp);
       }
     }
-    // a key that a row does not see must not reach it through 0 * V either:
-    // values that are not finite are left out of the product and added below
-    bool odd = false;
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        u32x4 pw;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) pw[e] = cvt_pk_bf16(acc[k][8 * s + 2 * e], acc[k][8 * s + 2 * e + 1]);
-        const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, pw[k][s]);
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
           // keys 16 s + 4 half + j and 16 s + 8 + 4 half + j: the second lies eight
           // rows on, whose swizzle differs in bit 3
-          const uint32_t at = bo + (32 * k + 16 * s) * kRowBytes;
-          s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vaddr[d] + at));
-          s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4*)(vaddr[d ^ 2] + at + 8 * kRowBytes));
-          if (!full) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const bool n0f = (v0[e] & 0x7F80) == 0x7F80, n1f = (v1[e] & 0x7F80) == 0x7F80;
-              odd |= n0f | n1f;
-              v0[e] = n0f ? (short)0 : v0[e], v1[e] = n1f ? (short)0 : v1[e];
-            }
-          }
-          bf16x8 vf;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            vf[e] = __builtin_bit_cast(__bf16, (short)v0[e]);
-            vf[4 + e] = __builtin_bit_cast(__bf16, (short)v1[e]);
-          }
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[d], 0, 0, 0);
+          const uint32_t at = (32 * k + 16 * s) * kRowBytes;
+          const s16x8 vf = __builtin_shufflevector(lds_read_tr(va[d], at), lds_read_tr(va[d ^ 2], at + 8 * kRowBytes), 0, 1,
+                                                   2, 3, 4, 5, 6, 7);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), pf, o[d], 0, 0, 0);
         }
       }
     }
-    if (!full && __any(odd)) {
-#pragma unroll 1
-      for (int i = 0; i < KT; ++i) {
-        const int n = n0 + i;
-        const bool hidden = bad_pages && n < khi && (uint32_t)uniform_load(table + (n >> a.page_shift)) >= (uint32_t)a.num_pages;
-        const bool see = visible(n) && n < khi && !hidden;
-        const uint32_t rowat = ldsV + bo + i * kRowBytes + 8 * half;
+    if (!full && RB > 1) {
+      odd = 0;
 #pragma unroll
-        for (int c = 0; c < 16; ++c) {  // coordinates 8 c + 4 half + 0..3
-          const u32x2 x = lds_read<u32x2>(rowat + ((uint32_t)c ^ swz(i & 15)) * 16);
-          const uint32_t w[4] = {x.x << 16, x.x & 0xFFFF0000u, x.y << 16, x.y & 0xFFFF0000u};
+      for (int w = 0; w < RB; ++w) odd |= odd_rows[buf][grp * RB + w];
+      odd = uniform64(odd);
+    }
+    while (odd) {  // values of V that clear_odd() took out of the tile
+      const int i = __ffsll((long long)odd) - 1, n = n0 + i;
+      odd &= odd - 1;
+      if (n >= khi) continue;
+      const char* vr = Vb + n * vstep;
+      if (paged) {
+        const uint32_t pg = (uint32_t)uniform_load(table + (n >> a.page_shift));
+        if (pg >= (uint32_t)a.num_pages) continue;
+        vr = Vb + pg * a.sV_b * 2 + (n & pmask) * vstep;
+      }
+      const bool see = visible(n);
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (see && (w[e] & 0x7F800000u) == 0x7F800000u) o[c / 4][4 * (c % 4) + e] += __uint_as_float(w[e]);
-        }
+      for (int c = 0; c < 16; ++c) {  // coordinates 8 c + 4 half + 0..3
+        const u32x2 x = *reinterpret_cast<const u32x2*>(vr + 16 * c + 8 * half);
+        const uint32_t w[4] = {x[0] << 16, x[0] & 0xFFFF0000u, x[1] << 16, x[1] & 0xFFFF0000u};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (see && (w[e] & 0x7F800000u) == 0x7F800000u) o[c / 4][4 * (c % 4) + e] += __uint_as_float(w[e]);
       }
     }
+  };
+
+  // A key that a row does not see must not reach it through 0 * V either: where
+  // some row sees only part of a tile, values of V that are not finite are
+  // cleared, and added afterwards (from memory) to the rows that see them.  A
+  // wavefront does this for the rows that it copied; the result has a bit for
+  // each row of the tile that held such a value.
+  auto clear_odd = [&](int buf) {
+    uint64_t rows_odd = 0;
+#pragma unroll
+    for (int i = 0; i < RPW / 4; ++i) {
+      const uint32_t at = ldsV + buf * S::kTileBytes + (rbw * RPW + 4 * i) * kRowBytes + 16 * lane;
+      u32x4 x = lds_read<u32x4>(at, 0);
+      uint32_t seen = 0;  // an exponent of all ones carries into bits 15 and 31
+#pragma unroll
+      for (int e = 0; e < 4; ++e) seen |= (x[e] & 0x7F807F80u) + 0x00800080u;
+      seen &= 0x80008000u;
+      const uint64_t lanes = __ballot(seen != 0);
+      if (lanes) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if ((x[e] & 0x7F80u) == 0x7F80u) x[e] &= 0xFFFF0000u;
+          if ((x[e] & 0x7F800000u) == 0x7F800000u) x[e] &= 0x0000FFFFu;
+        }
+        *(__attribute__((address_space(3))) u32x4*)(lds_char*)at = x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if ((lanes >> (16 * r)) & 0xFFFFu) rows_odd |= 1ull << (rbw * RPW + 4 * i + r);
+      }
+    }
+    return rows_odd;
   };
 
   if (it0 < it1) issue(it0, 0);
@@ -415,9 +465,16 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
     } else {
       dma_wait<0>();
     }
+    const int n0 = base0 + (it * KW + grp) * KT;
+    uint64_t odd = 0;
+    if (n0 + KT > wg_all_hi || n0 < wg_all_lo || bad_pages) {
+      odd = clear_odd(buf);
+      if (RB > 1 && lane == 0) odd_rows[buf][wid] = odd;
+      lds_done();
+    }
     if (RB > 1) __builtin_amdgcn_s_barrier();
     asm volatile("" : : : "memory");
-    compute(it, buf);
+    compute(it, buf, odd);
     lds_done();  // the reads of this buffer, before it is filled again
     if (RB > 1) __builtin_amdgcn_s_barrier();
   }
