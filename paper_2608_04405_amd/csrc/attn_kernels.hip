@@ -35,6 +35,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
 
 constexpr float kLog2e = 1.4426950408889634f;
+// instruction kinds of __builtin_amdgcn_sched_group_barrier
+constexpr int kSchedValu = 0x2, kSchedMfma = 0x8, kSchedLds = 0x100;
 constexpr int kRowBytes = kHeadDim * 2;
 constexpr int kBlockRows = 32;  // query rows of a wavefront
 
@@ -202,6 +204,9 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
       u32x4 x = live ? *reinterpret_cast<const u32x4*>(qp + 16 * s) : u32x4{0, 0, 0, 0};
       qf[s] = __builtin_bit_cast(bf16x8, x);
     }
+    // loaded here, not at their first use: a wait there would be one for the copies
+#pragma unroll
+    for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
   }
 
   // ---- tiles of this workgroup ---------------------------------------------
@@ -299,6 +304,14 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
         acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], s ? acc[k] : f32x16{}, 0, 0, 0);
       }
     }
+    // the operand of a product is read four products ahead
+    __builtin_amdgcn_sched_group_barrier(kSchedLds, 4, 0);
+#pragma unroll
+    for (int i = 0; i < 8 * NB - 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 0);
     // key of score e of block k: n0 + 32 k + 8 (e / 4) + 4 half + e % 4
     const int nl = n0 + 4 * half;
     if (CAP || BIAS) {
@@ -397,6 +410,16 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
         }
       }
     }
+    // V is read, and the next 16 keys' probabilities are computed, in the shadow
+    // of the products
+    __builtin_amdgcn_sched_group_barrier(kSchedLds, 8, 1);
+    __builtin_amdgcn_sched_group_barrier(kSchedValu, 24, 1);
+#pragma unroll
+    for (int i = 0; i < 8 * NB; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 1);
+      __builtin_amdgcn_sched_group_barrier(kSchedLds, 2, 1);
+      __builtin_amdgcn_sched_group_barrier(kSchedValu, 5, 1);
+    }
     if (!full && RB > 1) {
       odd = 0;
 #pragma unroll
@@ -459,7 +482,9 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
   if (it0 < it1) issue(it0, 0);
   for (int it = it0; it < it1; ++it) {
     const int buf = (it - it0) & 1;
-    if (it + 1 < it1) {
+    if (RB > 1) {
+      dma_wait<0>();
+    } else if (it + 1 < it1) {  // the other buffer is this wavefront's own: its next tile can be under way already
       issue(it + 1, buf ^ 1);
       dma_wait<kCopies>();
     } else {
@@ -472,11 +497,16 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
       if (RB > 1 && lane == 0) odd_rows[buf][wid] = odd;
       lds_done();
     }
-    if (RB > 1) __builtin_amdgcn_s_barrier();
+    if (RB > 1) {
+      // past this point every wavefront's part of this tile is there, and no one
+      // reads the other buffer any more
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" : : : "memory");
+      if (it + 1 < it1) issue(it + 1, buf ^ 1);
+    }
     asm volatile("" : : : "memory");
     compute(it, buf, odd);
     lds_done();  // the reads of this buffer, before it is filled again
-    if (RB > 1) __builtin_amdgcn_s_barrier();
   }
 
   // ---- results ---------------------------------------------------------------
