@@ -232,15 +232,21 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
     bad_pages = __any(bad);
   }
 
-  const int r4 = lane >> 4;  // row within a copy's four
+  constexpr int RU = RPW < 16 ? RPW : 16;  // a wavefront copies rows in runs of RU, which no page border cuts
+  const int r4 = lane >> 4;                // row within a copy's four
+  uint32_t chunk[RU / 4], koff[RU / 4], voff[RU / 4];
+#pragma unroll
+  for (int i = 0; i < RU / 4; ++i) {
+    chunk[i] = (((uint32_t)lane & 15u) ^ swz((uint32_t)(rbw * RPW + 4 * i + r4))) * 16;
+    koff[i] = (4 * i + r4) * (uint32_t)kstep + chunk[i];
+    voff[i] = (4 * i + r4) * (uint32_t)vstep + chunk[i];
+  }
   auto issue = [&](int it, int buf) {
     const int n0 = base0 + (it * KW + grp) * KT + rbw * RPW;
 #pragma unroll
-    for (int u = 0; u < (RPW + 15) / 16; ++u) {
-      constexpr int RU = RPW < 16 ? RPW : 16;  // rows of one page at least
-      const int nu = min(n0 + 16 * u, khi - 1);
+    for (int u = 0; u < RPW / RU; ++u) {
+      const int nu = min(n0 + RU * u, khi - 1);
       const char *kt, *vt;
-      int last;  // last row that may be read, from kt and vt on
       if (paged) {
         const uint32_t pg = (uint32_t)uniform_load(table + (nu >> a.page_shift));
         const int64_t page = pg < (uint32_t)a.num_pages ? pg : 0;
@@ -249,15 +255,21 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
       } else {
         kt = Kb + nu * kstep, vt = Vb + nu * vstep;
       }
-      last = khi - 1 - nu;
+      const uint32_t dst = (uint32_t)buf * S::kTileBytes + (rbw * RPW + RU * u) * kRowBytes;
+      const int last = khi - 1 - nu;  // last row that may be read, from kt and vt on
+      if (last >= RU - 1) {
 #pragma unroll
-      for (int i = 0; i < RU / 4; ++i) {
-        const int rt = 16 * u + 4 * i;  // row within this wavefront's share
-        const uint32_t r = min(4 * i + r4, last);
-        const uint32_t chunk = ((uint32_t)lane & 15u) ^ swz((uint32_t)(rbw * RPW + rt + r4));
-        const uint32_t dst = (uint32_t)buf * S::kTileBytes + (rbw * RPW + rt) * kRowBytes;
-        dma16(kt, r * (uint32_t)kstep + chunk * 16, ldsK + dst);
-        dma16(vt, r * (uint32_t)vstep + chunk * 16, ldsV + dst);
+        for (int i = 0; i < RU / 4; ++i) {
+          dma16(kt, koff[i], ldsK + dst + 4 * i * kRowBytes);
+          dma16(vt, voff[i], ldsV + dst + 4 * i * kRowBytes);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < RU / 4; ++i) {
+          const uint32_t r = min(4 * i + r4, last);
+          dma16(kt, r * (uint32_t)kstep + chunk[i], ldsK + dst + 4 * i * kRowBytes);
+          dma16(vt, r * (uint32_t)vstep + chunk[i], ldsV + dst + 4 * i * kRowBytes);
+        }
       }
     }
   };
@@ -314,21 +326,27 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
     __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 0);
     // key of score e of block k: n0 + 32 k + 8 (e / 4) + 4 half + e % 4
     const int nl = n0 + 4 * half;
+    // in units of log2: cap tanh(x) = cap - 2 cap / (1 + e^2x)
+    auto scored = [&](float z) {
+      return CAP ? fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * capk)), cap2) : z * c1;
+    };
     if (CAP || BIAS) {
+      // (a distance beyond 2^24 is rounded to fp32 before it is weighed)
+      const float ahead = (float)(place - nl);
+      const bool drafts = TREE && BIAS && n0 + KT > len;
 #pragma unroll
       for (int k = 0; k < NB; ++k) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          float z = acc[k][e];
-          // cap tanh(x) = cap - 2 cap / (1 + e^2x)
-          if (CAP)
-            z = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * capk)), cap2);
-          else
-            z *= c1;
+          const int at = 32 * k + 8 * (e / 4) + e % 4;
+          float z = scored(acc[k][e]);
           if (BIAS) {
-            int n = nl + 32 * k + 8 * (e / 4) + e % 4;
-            if (TREE && n0 + KT > len) n = (uint32_t)(n - len) < (uint32_t)a.T ? draft_place[n - len] : n;
-            z = fmaf(-slope, (float)abs(place - n), z);
+            float dist = ahead - (float)at;
+            if (TREE && drafts) {
+              const uint32_t j = (uint32_t)(nl + at - len);
+              if (j < (uint32_t)a.T) dist = (float)(place - draft_place[j]);
+            }
+            z = fmaf(-slope, fabsf(dist), z);
           }
           acc[k][e] = z;
         }
