@@ -124,13 +124,21 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
   extern __shared__ char smem[];
   __shared__ uint64_t odd_rows[2][RB * KW];
   __shared__ int draft_place[TREE && BIAS ? 64 : 1];
-  // consecutive workgroups go to different XCDs; give each XCD a run of
-  // consecutive items, which share their keys in its L2
-  const int per_xcd = (items + 7) / 8;
-  const int item = (blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-  if (item >= items || (int)(blockIdx.x >> 3) >= per_xcd) return;
-  const int rb = nrb - 1 - item % nrb;  // later rows see more keys: longest first
-  const int split = item / nrb % a.splits, bh = item / nrb / a.splits;
+  // Consecutive workgroups go to different XCDs.  A prefill gives each XCD a run
+  // of consecutive items, whose row blocks share their keys in its L2 (later row
+  // blocks first: they see more keys).  In a tree only the row blocks of one
+  // piece share keys, and the sequences' lengths differ: pieces go round the XCDs.
+  const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3;
+  int rb, piece;
+  if (TREE) {
+    rb = turn % nrb, piece = turn / nrb * 8 + xcd;
+    if (piece >= items / nrb) return;
+  } else {
+    const int item = xcd * ((items + 7) / 8) + turn;
+    if (item >= items || turn >= (items + 7) / 8) return;
+    rb = nrb - 1 - item % nrb, piece = item / nrb;
+  }
+  const int split = piece % a.splits, bh = piece / a.splits;
   const int b = bh / a.Hkv, h = bh - b * a.Hkv;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = wid / RB, rbw = wid % RB;
@@ -636,7 +644,7 @@ template <int RB, int KW, int KT, bool TREE>
 static hipError_t launch_attn_shape(const AttnArgs& a) {
   const int rows = a.T * a.G, nrb = (rows + RB * kBlockRows - 1) / (RB * kBlockRows);
   const int items = a.B * a.Hkv * nrb * a.splits;
-  const int grid = (items + 7) / 8 * 8;
+  const int grid = TREE ? (items / nrb + 7) / 8 * 8 * nrb : (items + 7) / 8 * 8;
 #define BPC_ATTN(CAP, BIAS)                                                                                       \
   {                                                                                                               \
     auto* f = attn_kernel<RB, KW, KT, TREE, CAP, BIAS>;                                                           \
