@@ -154,30 +154,41 @@ __device__ __forceinline__ uint4 turn_row(const uint4& x, bool norm, float eps, 
   return make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
 }
 
-// rows of `H` heads of one token, passes [p0, p1): from `src` with head stride
-// ss, to `dst` with head stride sd; PER_HEAD: weights of their own for every head
+// Passes [p0, p1) of a token's heads through `row(chunk, head)`, from `src` with
+// head stride ss to `dst` with head stride sd: up to kRopeBatch passes' loads
+// before the first is used.
+template <int N, class Row>
+__device__ __forceinline__ void move_passes(const uint16_t* src, int64_t ss, uint16_t* dst, int64_t sd, int H, int p, Row row) {
+  const int sub = (threadIdx.x & 63) / kRowLanes, d0 = 8 * (threadIdx.x % kRowLanes);
+  uint4 x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    x[i] = *reinterpret_cast<const uint4*>(src + min((p + i) * kPassRows + sub, H - 1) * ss + d0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int h = (p + i) * kPassRows + sub;
+    const uint4 y = row(x[i], min(h, H - 1));
+    if (h < H) *reinterpret_cast<uint4*>(dst + h * sd + d0) = y;
+  }
+}
+template <class Row>
+__device__ __forceinline__ void move_heads(const uint16_t* src, int64_t ss, uint16_t* dst, int64_t sd, int H, int p0, int p1, Row row) {
+  int p = p0;
+  for (; p + kRopeBatch <= p1; p += kRopeBatch) move_passes<kRopeBatch>(src, ss, dst, sd, H, p, row);
+  if (p + 2 <= p1) move_passes<2>(src, ss, dst, sd, H, p, row), p += 2;
+  if (p < p1) move_passes<1>(src, ss, dst, sd, H, p, row);
+}
+
+// rows of H heads of one token; PER_HEAD: weights of their own for every head
 template <Pairing PAIR, bool PER_HEAD>
 __device__ __forceinline__ void turn_heads(const uint16_t* src, int64_t ss, uint16_t* dst, int64_t sd, const uint16_t* w,
                                            int64_t sw, float eps, const Turn& t, int H, int p0, int p1) {
-  const int lane = threadIdx.x & 63, sub = lane / kRowLanes, d0 = 8 * (lane % kRowLanes);
   float C[8], S[8];
   if (!PER_HEAD) row_factors<PAIR>(t, w, C, S);
-  for (int p = p0; p < p1; p += kRopeBatch) {
-    uint4 x[kRopeBatch];
-#pragma unroll
-    for (int i = 0; i < kRopeBatch; ++i) {
-      const int h = min((p + i) * kPassRows + sub, H - 1);
-      x[i] = *reinterpret_cast<const uint4*>(src + h * ss + d0);
-    }
-#pragma unroll
-    for (int i = 0; i < kRopeBatch; ++i) {
-      if (p + i >= p1) break;
-      const int h = (p + i) * kPassRows + sub;
-      if (PER_HEAD) row_factors<PAIR>(t, w ? w + min(h, H - 1) * sw : nullptr, C, S);
-      const uint4 y = turn_row<PAIR>(x[i], w != nullptr, eps, t, C, S);
-      if (h < H) *reinterpret_cast<uint4*>(dst + h * sd + d0) = y;
-    }
-  }
+  move_heads(src, ss, dst, sd, H, p0, p1, [&](const uint4& x, int h) {
+    if (PER_HEAD) row_factors<PAIR>(t, w ? w + h * sw : nullptr, C, S);
+    return turn_row<PAIR>(x, w != nullptr, eps, t, C, S);
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -186,10 +197,11 @@ __device__ __forceinline__ void turn_heads(const uint16_t* src, int64_t ss, uint
 // ---------------------------------------------------------------------------
 template <Pairing PAIR, bool PER_HEAD>
 __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, int per, int parts) {
-  const int64_t wave = (int64_t)blockIdx.x * kRopeWaves + (threadIdx.x >> 6);
-  const int64_t tok = wave / parts;
-  if (tok >= (int64_t)a.B * a.T) return;
-  const int b = (int)(tok / a.T), t = (int)(tok - (int64_t)b * a.T);
+  // (fewer than 2^32 wavefronts: 2^30 tokens, or few of them in parts)
+  const uint32_t wave = blockIdx.x * kRopeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t tok = wave / (uint32_t)parts;
+  if (tok >= (uint32_t)a.B * (uint32_t)a.T) return;
+  const int b = (int)(tok / (uint32_t)a.T), t = (int)(tok - (uint32_t)b * (uint32_t)a.T);
   const float* cs = nullptr;
   if (PAIR != kPairNone) {
     const int p = a.pos[b * a.sp_b + t];
@@ -198,7 +210,7 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, 
   }
   const Turn turn = token_turn<PAIR>(cs, a.R);
   const int nq = (a.q.H + kPassRows - 1) / kPassRows, nk = (a.k.H + kPassRows - 1) / kPassRows;
-  const int p0 = (int)(wave - tok * parts) * per, p1 = min(nq + nk, p0 + per);
+  const int p0 = (int)(wave - tok * (uint32_t)parts) * per, p1 = min(nq + nk, p0 + per);
   if (p0 < nq)
     turn_heads<PAIR, PER_HEAD>(a.q.in + b * a.q.si_b + t * a.q.si_t, a.q.si_h, a.q.out + b * a.q.so_b + t * a.q.so_t,
                                a.q.so_h, a.q.w, a.q.sw_h, a.eps, turn, a.q.H, p0, min(p1, nq));
@@ -246,10 +258,11 @@ hipError_t launch_qk_norm_rope(const RopeArgs& a) {
 // ---------------------------------------------------------------------------
 template <Pairing PAIR, bool PER_HEAD>
 __global__ __launch_bounds__(kRopeThreads) void append_paged_kernel(AppendPagedArgs a, int per, int parts) {
-  const int64_t wave = (int64_t)blockIdx.x * kRopeWaves + (threadIdx.x >> 6);
-  const int64_t tok = wave / parts;
-  if (tok >= (int64_t)a.B * a.T) return;
-  const int b = (int)(tok / a.T), t = (int)(tok - (int64_t)b * a.T);
+  // (fewer than 2^32 wavefronts: 2^30 tokens, or few of them in parts)
+  const uint32_t wave = blockIdx.x * kRopeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t tok = wave / (uint32_t)parts;
+  if (tok >= (uint32_t)a.B * (uint32_t)a.T) return;
+  const int b = (int)(tok / (uint32_t)a.T), t = (int)(tok - (uint32_t)b * (uint32_t)a.T);
   if (a.count && t >= a.count[b]) return;
   const int64_t slot = (int64_t)a.pos[b] + t;
   if (slot < 0 || (slot >> a.page_shift) >= a.max_pages) return;
@@ -263,26 +276,13 @@ __global__ __launch_bounds__(kRopeThreads) void append_paged_kernel(AppendPagedA
     cs = a.cos_sin + p * a.R;
   }
   const int n = (a.Hkv + kPassRows - 1) / kPassRows;
-  const int p0 = (int)(wave - tok * parts) * per, p1 = min(2 * n, p0 + per);
+  const int p0 = (int)(wave - tok * (uint32_t)parts) * per, p1 = min(2 * n, p0 + per);
   if (p0 < n)
     turn_heads<PAIR, PER_HEAD>(a.kn + b * a.skn_b + t * a.skn_t, a.skn_h, a.K + page * a.sK_p + row * a.sK_n, a.sK_h,
                                a.wk, a.sw_h, a.eps, token_turn<PAIR>(cs, a.R), a.Hkv, p0, min(p1, n));
-  if (p1 > n) {
-    const int lane = threadIdx.x & 63, sub = lane / kRowLanes, d0 = 8 * (lane % kRowLanes);
-    const uint16_t* src = a.vn + b * a.svn_b + t * a.svn_t + d0;
-    uint16_t* dst = a.V + page * a.sV_p + row * a.sV_n + d0;
-    for (int p = max(p0 - n, 0); p < p1 - n; p += kRopeBatch) {
-      uint4 x[kRopeBatch];
-#pragma unroll
-      for (int i = 0; i < kRopeBatch; ++i)
-        x[i] = *reinterpret_cast<const uint4*>(src + min((p + i) * kPassRows + sub, a.Hkv - 1) * a.svn_h);
-#pragma unroll
-      for (int i = 0; i < kRopeBatch; ++i) {
-        const int h = (p + i) * kPassRows + sub;
-        if (p + i < p1 - n && h < a.Hkv) *reinterpret_cast<uint4*>(dst + h * a.sV_h) = x[i];
-      }
-    }
-  }
+  if (p1 > n)
+    move_heads(a.vn + b * a.svn_b + t * a.svn_t, a.svn_h, a.V + page * a.sV_p + row * a.sV_n, a.sV_h, a.Hkv, max(p0 - n, 0),
+               p1 - n, [](const uint4& x, int) { return x; });
 }
 
 hipError_t launch_append_paged(const AppendPagedArgs& a) {
