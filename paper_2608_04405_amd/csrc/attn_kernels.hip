@@ -39,6 +39,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSchedValu = 0x2, kSchedMfma = 0x8, kSchedLds = 0x100;
 constexpr int kRowBytes = kHeadDim * 2;
 constexpr int kBlockRows = 32;  // query rows of a wavefront
+constexpr int kMaxSplits = 64;  // pieces of the key axis
 
 __device__ __forceinline__ uint32_t swz(uint32_t row) {
   return (row & 8u) | ((row & 3u) << 1) | ((row >> 2) & 1u);
@@ -62,6 +63,11 @@ __device__ __forceinline__ float sum_halves(float x) {
 __device__ __forceinline__ int wave_min(int x) { return wave_reduce_maxmin<false>(x); }
 __device__ __forceinline__ int wave_max(int x) { return wave_reduce_maxmin<true>(x); }
 
+// a value equal in all lanes, in scalar registers
+__device__ __forceinline__ uint64_t uniform64(uint64_t x) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) |
+         (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
+}
 // 64 lanes' 16 bytes each, from `base` + their own offset to LDS at `dst` +
 // 16 lane.  Written out because the compiler would otherwise wait for every
 // such copy in flight before any LDS read; the kernel waits by itself (dma_wait).
@@ -88,11 +94,6 @@ __device__ __forceinline__ T lds_read(uint32_t at, int offset) {
 // row i / 4, columns 4 (i % 4) .. + 3 it addresses
 __device__ __forceinline__ s16x4 lds_read_tr(uint32_t at, int offset) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)((lds_char*)at + offset));
-}
-// a value equal in all lanes, in scalar registers
-__device__ __forceinline__ uint64_t uniform64(uint64_t x) {
-  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) |
-         (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
 }
 // x, as a value that the compiler does not take apart again
 __device__ __forceinline__ uint32_t opaque(uint32_t x) {
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
   int klo = 0, khi = 0, len = 0;
   int wg_all_lo = 0, wg_all_hi = 0;  // and those that every row sees
   if (TREE) {
-    len = a.lens[b];
+    len = uniform_load(a.lens + b);
     if (len < 0 || len > a.N - a.T) return;  // no such sequence: its rows stay as they are
     khi = len + a.T;
     wg_all_hi = len;
@@ -167,6 +168,78 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
     wg_all_lo = wave_max(all_lo), wg_all_hi = wave_min(all_hi);
     if (klo >= khi) klo = khi = 0;
   }
+
+  // ---- tiles of this workgroup ---------------------------------------------
+  const int base0 = klo / KT * KT;
+  const int total = (khi - base0 + KT * KW - 1) / (KT * KW);
+  const int per = (total + a.splits - 1) / a.splits;
+  const int it0 = split * per, it1 = min(total, it0 + per);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
+  const uint32_t ldsK = lds0 + grp * 4 * S::kTileBytes, ldsV = ldsK + 2 * S::kTileBytes;
+
+  const bool paged = TREE && a.table;
+  const int32_t* table = paged ? a.table + b * a.st_b : nullptr;
+  const char* Kb = reinterpret_cast<const char*>(a.K + (paged ? 0 : b * a.sK_b) + h * a.sK_h);
+  const char* Vb = reinterpret_cast<const char*>(a.V + (paged ? 0 : b * a.sV_b) + h * a.sV_h);
+  const int64_t kstep = a.sK_n * 2, vstep = a.sV_n * 2;
+  const int pmask = (1 << a.page_shift) - 1;
+  constexpr int RU = RPW < 16 ? RPW : 16;  // a wavefront copies rows in runs of RU, which no page border cuts
+  const int r4 = lane >> 4;                // row within a copy's four
+  uint32_t chunk[RU / 4], koff[RU / 4], voff[RU / 4];
+#pragma unroll
+  for (int i = 0; i < RU / 4; ++i) {
+    chunk[i] = (((uint32_t)lane & 15u) ^ swz((uint32_t)(rbw * RPW + 4 * i + r4))) * 16;
+    koff[i] = (4 * i + r4) * (uint32_t)kstep + chunk[i];
+    voff[i] = (4 * i + r4) * (uint32_t)vstep + chunk[i];
+  }
+  auto issue = [&](int it, int buf) {
+    const int n0 = base0 + (it * KW + grp) * KT + rbw * RPW;
+#pragma unroll
+    for (int u = 0; u < RPW / RU; ++u) {
+      const int nu = min(n0 + RU * u, khi - 1);
+      const char *kt, *vt;
+      if (paged) {
+        const uint32_t pg = (uint32_t)uniform_load(table + (nu >> a.page_shift));
+        const int64_t page = pg < (uint32_t)a.num_pages ? pg : 0;
+        kt = Kb + page * a.sK_b * 2 + (nu & pmask) * kstep;
+        vt = Vb + page * a.sV_b * 2 + (nu & pmask) * vstep;
+      } else {
+        kt = Kb + nu * kstep, vt = Vb + nu * vstep;
+      }
+      kt = reinterpret_cast<const char*>(uniform64(reinterpret_cast<uint64_t>(kt)));
+      vt = reinterpret_cast<const char*>(uniform64(reinterpret_cast<uint64_t>(vt)));
+      const uint32_t dst = (uint32_t)buf * S::kTileBytes + (rbw * RPW + RU * u) * kRowBytes;
+      const int last = khi - 1 - nu;  // last row that may be read, from kt and vt on
+      if (last >= RU - 1) {
+#pragma unroll
+        for (int i = 0; i < RU / 4; ++i) {
+          dma16(kt, koff[i], ldsK + dst + 4 * i * kRowBytes);
+          dma16(vt, voff[i], ldsV + dst + 4 * i * kRowBytes);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < RU / 4; ++i) {
+          const uint32_t r = min(4 * i + r4, last);
+          dma16(kt, r * (uint32_t)kstep + chunk[i], ldsK + dst + 4 * i * kRowBytes);
+          dma16(vt, r * (uint32_t)vstep + chunk[i], ldsV + dst + 4 * i * kRowBytes);
+        }
+      }
+    }
+  };
+  constexpr int kCopies = 2 * (RPW / 4);  // copies a wavefront issues per tile
+
+  // the first tile is under way before anything else is looked up
+  if (it0 < it1) issue(it0, 0);
+
+  // a page that the table does not name hides its keys; rare enough to look only once
+  bool bad_pages = false;
+  if (paged && it0 < it1) {
+    const int p0 = (base0 + it0 * KT * KW) >> a.page_shift, p1 = (min(khi, base0 + it1 * KT * KW) - 1) >> a.page_shift;
+    bool bad = false;
+    for (int p = p0 + lane; p <= p1; p += 64) bad |= (uint32_t)table[p] >= (uint32_t)a.num_pages;
+    bad_pages = __any(bad);
+  }
+
 
   // ---- this lane's row ------------------------------------------------------
   const int row = wg_row0 + rbw * kBlockRows + col;
@@ -216,72 +289,6 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
 #pragma unroll
     for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
   }
-
-  // ---- tiles of this workgroup ---------------------------------------------
-  const int base0 = klo / KT * KT;
-  const int total = (khi - base0 + KT * KW - 1) / (KT * KW);
-  const int per = (total + a.splits - 1) / a.splits;
-  const int it0 = split * per, it1 = min(total, it0 + per);
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
-  const uint32_t ldsK = lds0 + grp * 4 * S::kTileBytes, ldsV = ldsK + 2 * S::kTileBytes;
-
-  const bool paged = TREE && a.table;
-  const int32_t* table = paged ? a.table + b * a.st_b : nullptr;
-  const char* Kb = reinterpret_cast<const char*>(a.K + (paged ? 0 : b * a.sK_b) + h * a.sK_h);
-  const char* Vb = reinterpret_cast<const char*>(a.V + (paged ? 0 : b * a.sV_b) + h * a.sV_h);
-  const int64_t kstep = a.sK_n * 2, vstep = a.sV_n * 2;
-  const int pmask = (1 << a.page_shift) - 1;
-  // a page that the table does not name hides its keys; rare enough to look only once
-  bool bad_pages = false;
-  if (paged && it0 < it1) {
-    const int p0 = (base0 + it0 * KT * KW) >> a.page_shift, p1 = (min(khi, base0 + it1 * KT * KW) - 1) >> a.page_shift;
-    bool bad = false;
-    for (int p = p0 + lane; p <= p1; p += 64) bad |= (uint32_t)table[p] >= (uint32_t)a.num_pages;
-    bad_pages = __any(bad);
-  }
-
-  constexpr int RU = RPW < 16 ? RPW : 16;  // a wavefront copies rows in runs of RU, which no page border cuts
-  const int r4 = lane >> 4;                // row within a copy's four
-  uint32_t chunk[RU / 4], koff[RU / 4], voff[RU / 4];
-#pragma unroll
-  for (int i = 0; i < RU / 4; ++i) {
-    chunk[i] = (((uint32_t)lane & 15u) ^ swz((uint32_t)(rbw * RPW + 4 * i + r4))) * 16;
-    koff[i] = (4 * i + r4) * (uint32_t)kstep + chunk[i];
-    voff[i] = (4 * i + r4) * (uint32_t)vstep + chunk[i];
-  }
-  auto issue = [&](int it, int buf) {
-    const int n0 = base0 + (it * KW + grp) * KT + rbw * RPW;
-#pragma unroll
-    for (int u = 0; u < RPW / RU; ++u) {
-      const int nu = min(n0 + RU * u, khi - 1);
-      const char *kt, *vt;
-      if (paged) {
-        const uint32_t pg = (uint32_t)uniform_load(table + (nu >> a.page_shift));
-        const int64_t page = pg < (uint32_t)a.num_pages ? pg : 0;
-        kt = Kb + page * a.sK_b * 2 + (nu & pmask) * kstep;
-        vt = Vb + page * a.sV_b * 2 + (nu & pmask) * vstep;
-      } else {
-        kt = Kb + nu * kstep, vt = Vb + nu * vstep;
-      }
-      const uint32_t dst = (uint32_t)buf * S::kTileBytes + (rbw * RPW + RU * u) * kRowBytes;
-      const int last = khi - 1 - nu;  // last row that may be read, from kt and vt on
-      if (last >= RU - 1) {
-#pragma unroll
-        for (int i = 0; i < RU / 4; ++i) {
-          dma16(kt, koff[i], ldsK + dst + 4 * i * kRowBytes);
-          dma16(vt, voff[i], ldsV + dst + 4 * i * kRowBytes);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < RU / 4; ++i) {
-          const uint32_t r = min(4 * i + r4, last);
-          dma16(kt, r * (uint32_t)kstep + chunk[i], ldsK + dst + 4 * i * kRowBytes);
-          dma16(vt, r * (uint32_t)vstep + chunk[i], ldsV + dst + 4 * i * kRowBytes);
-        }
-      }
-    }
-  };
-  constexpr int kCopies = 2 * (RPW / 4);  // copies a wavefront issues per tile
 
   f32x16 o[4];
 #pragma unroll
@@ -505,7 +512,6 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
     return rows_odd;
   };
 
-  if (it0 < it1) issue(it0, 0);
   for (int it = it0; it < it1; ++it) {
     const int buf = (it - it0) & 1;
     if (RB > 1) {
@@ -600,33 +606,52 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
   }
 }
 
-// The splits of a row joined: a wavefront per row, two coordinates per lane.
+// The splits of a row joined: a wavefront per row.  Lane s holds split s's
+// (max, sum) and so its weight; then each half of the wavefront adds every other
+// split's 128 sums, four coordinates per lane, four loads in flight.
+static_assert(kMaxSplits <= 64, "a lane per split");
 template <bool TREE>
 __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (bh, t, g)
-  const int rows = a.T * a.G, lane = threadIdx.x & 63;
-  const int64_t bh = r / rows;
-  if (bh >= (int64_t)a.B * a.Hkv) return;
+  const int rows = a.T * a.G, lane = threadIdx.x & 63, half = lane >> 5, d = 4 * (lane & 31);
+  const uint32_t r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (bh, t, g)
+  const uint32_t bh = r / (uint32_t)rows;
+  if (bh >= (uint32_t)(a.B * a.Hkv)) return;
   const int row = (int)(r - bh * rows), t = row / a.G, g = row - t * a.G;
-  const int b = (int)(bh / a.Hkv), h = (int)(bh - (int64_t)b * a.Hkv);
+  const int b = (int)(bh / a.Hkv), h = (int)(bh - b * a.Hkv);
   if (TREE) {
-    const int len = a.lens[b];
+    const int len = uniform_load(a.lens + b);
     if (len < 0 || len > a.N - a.T) return;
   }
-  const float2* ml = a.part_ml + r * a.splits;
-  const float* po = a.part_o + r * a.splits * kHeadDim + 2 * lane;
-  float mx = -INFINITY, tot = 0.f, x0 = 0.f, x1 = 0.f;
-  for (int s = 0; s < a.splits; ++s) mx = fmaxf(mx, ml[s].x);
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 p = ml[s];
-    if (p.y == 0.f) continue;  // the split saw no key of this row: its sum was not written
-    const float f = __builtin_amdgcn_exp2f(p.x - mx);
-    const float2 v = *reinterpret_cast<const float2*>(po + (int64_t)s * kHeadDim);
-    tot = fmaf(p.y, f, tot), x0 = fmaf(v.x, f, x0), x1 = fmaf(v.y, f, x1);
+  const float2* ml = a.part_ml + (int64_t)r * a.splits;
+  const float* po = a.part_o + (int64_t)r * a.splits * kHeadDim + d;
+  float2 mine = make_float2(-INFINITY, 0.f);
+  if (lane < a.splits) mine = ml[lane];
+  // a split that saw no key of this row has the sum 0, and its o was not written
+  float mx = mine.y == 0.f ? -INFINITY : mine.x;
+#pragma unroll
+  for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+  const float w = mine.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(mine.x - mx);
+  float tot = mine.y * w;
+#pragma unroll
+  for (int o = 32; o; o >>= 1) tot += __shfl_xor(tot, o, 64);
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s0 = 0; s0 < a.splits; s0 += 8) {
+    float4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      v[i] = *reinterpret_cast<const float4*>(po + (int64_t)min(s0 + 2 * i + half, a.splits - 1) * kHeadDim);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = __shfl(w, (s0 + 2 * i + half) & 63, 64);
+      const bool on = f != 0.f && s0 + 2 * i + half < a.splits;
+      x.x = on ? fmaf(v[i].x, f, x.x) : x.x, x.y = on ? fmaf(v[i].y, f, x.y) : x.y;
+      x.z = on ? fmaf(v[i].z, f, x.z) : x.z, x.w = on ? fmaf(v[i].w, f, x.w) : x.w;
+    }
   }
   const float inv = tot == 0.f ? 0.f : 1.f / tot;
+  x.x = sum_halves(x.x) * inv, x.y = sum_halves(x.y) * inv, x.z = sum_halves(x.z) * inv, x.w = sum_halves(x.w) * inv;
   uint16_t* op = a.out + b * a.so_b + (int64_t)(h * a.G + g) * a.so_h + (int64_t)t * a.so_t;
-  *reinterpret_cast<uint32_t*>(op + 2 * lane) = cvt_pk_bf16(x0 * inv, x1 * inv);
+  if (half == 0) *reinterpret_cast<uint2*>(op + d) = make_uint2(cvt_pk_bf16(x.x, x.y), cvt_pk_bf16(x.z, x.w));
 }
 
 static hipError_t allow_lds(const void* f, int bytes, std::atomic<uint64_t>& allowed) {
@@ -671,7 +696,7 @@ AttnPlan attn_plan(int B, int Hkv, int G, int T, int N) {
   const int64_t most = ((int64_t)N + 2 * unit - 1) / (2 * unit);
   int64_t s = 1024 / blocks;
   s = s > most ? most : s;
-  s = s > 64 ? 64 : s;
+  s = s > kMaxSplits ? kMaxSplits : s;
   p.splits = s < 1 ? 1 : (int)s;
   size_t o = 0;
   auto take = [&](size_t bytes) {
