@@ -107,18 +107,30 @@ __device__ __forceinline__ int32_t uniform_load(const int32_t* p) {
   return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;
 }
 
+// The kernel's arguments, read again: what only the end of a kernel or a rare
+// path needs would otherwise hold scalar registers through the loop.
+typedef const __attribute__((address_space(4))) AttnArgs* LateArgs;
+__device__ __forceinline__ LateArgs late_args() {
+  LateArgs p = (LateArgs)__builtin_amdgcn_kernarg_segment_ptr();  // (the kernel's first argument)
+  asm volatile("" : "+s"(p));
+  return p;
+}
+
 // RB row blocks of 32 rows by KW groups of wavefronts that take alternate key
 // tiles of KT keys; RB KW wavefronts.
-template <int RB, int KW, int KT, bool TREE, bool CAP, bool BIAS>
+enum AttnKind { kPrefill, kTree, kPagedTree };
+
+template <int RB, int KW, int KT, AttnKind KIND, bool CAP, bool BIAS>
 struct AttnShape {
   static constexpr int kThreads = RB * KW * 64;
   static constexpr int kTileBytes = KT * kRowBytes;    // K or V of a tile
   static constexpr int kLds = KW * 2 * 2 * kTileBytes;  // K and V, two buffers, per group
 };
 
-template <int RB, int KW, int KT, bool TREE, bool CAP, bool BIAS>
-__global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nrb, int items) {
-  using S = AttnShape<RB, KW, KT, TREE, CAP, BIAS>;
+template <int RB, int KW, int KT, AttnKind KIND, bool CAP, bool BIAS>
+__global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnArgs a) {
+  using S = AttnShape<RB, KW, KT, KIND, CAP, BIAS>;
+  constexpr bool TREE = KIND != kPrefill, paged = KIND == kPagedTree;
   constexpr int NB = KT / 32;   // 32-key blocks of a tile
   constexpr int RPW = KT / RB;  // rows of a tile's K (and V) that a wavefront copies
   static_assert(RPW % 4 == 0, "a copy moves four rows");
@@ -132,15 +144,16 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
   const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3;
   int rb, piece;
   if (TREE) {
-    rb = turn % nrb, piece = turn / nrb * 8 + xcd;
-    if (piece >= items / nrb) return;
+    const int round = a.div_nrb.quotient(turn);
+    rb = turn - round * a.nrb, piece = round * 8 + xcd;
+    if (piece * a.nrb >= a.items) return;
   } else {
-    const int item = xcd * ((items + 7) / 8) + turn;
-    if (item >= items || turn >= (items + 7) / 8) return;
-    rb = nrb - 1 - item % nrb, piece = item / nrb;
+    const int item = xcd * ((a.items + 7) >> 3) + turn;
+    if (item >= a.items || turn >= (a.items + 7) >> 3) return;
+    piece = a.div_nrb.quotient(item), rb = a.nrb - 1 - (item - piece * a.nrb);
   }
-  const int split = piece % a.splits, bh = piece / a.splits;
-  const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const int bh = a.div_splits.quotient(piece), split = piece - bh * a.splits;
+  const int b = a.div_Hkv.quotient(bh), h = bh - b * a.Hkv;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = wid / RB, rbw = wid % RB;
   const int half = lane >> 5, col = lane & 31;
@@ -156,7 +169,7 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
     khi = len + a.T;
     wg_all_hi = len;
   } else {
-    const int t0 = wg_row0 / G, t1 = min(rows - 1, wg_row0 + RB * kBlockRows - 1) / G;
+    const int t0 = a.div_G.quotient(wg_row0), t1 = a.div_G.quotient(min(rows - 1, wg_row0 + RB * kBlockRows - 1));
     int lo = INT32_MAX, hi = 0, all_lo = 0, all_hi = INT32_MAX;
     for (int t = t0 + lane; t <= t1; t += 64) {
       const int f = a.key_begin ? max(a.key_begin[b * a.s_begin + t], 0) : 0;
@@ -172,12 +185,11 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
   // ---- tiles of this workgroup ---------------------------------------------
   const int base0 = klo / KT * KT;
   const int total = (khi - base0 + KT * KW - 1) / (KT * KW);
-  const int per = (total + a.splits - 1) / a.splits;
+  const int per = a.div_splits.quotient(total + a.splits - 1);
   const int it0 = split * per, it1 = min(total, it0 + per);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
   const uint32_t ldsK = lds0 + grp * 4 * S::kTileBytes, ldsV = ldsK + 2 * S::kTileBytes;
 
-  const bool paged = TREE && a.table;
   const int32_t* table = paged ? a.table + b * a.st_b : nullptr;
   const char* Kb = reinterpret_cast<const char*>(a.K + (paged ? 0 : b * a.sK_b) + h * a.sK_h);
   const char* Vb = reinterpret_cast<const char*>(a.V + (paged ? 0 : b * a.sV_b) + h * a.sV_h);
@@ -192,15 +204,34 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
     koff[i] = (4 * i + r4) * (uint32_t)kstep + chunk[i];
     voff[i] = (4 * i + r4) * (uint32_t)vstep + chunk[i];
   }
+  // Pages of the next tile to be copied, one per 16 keys.
+  // A page that is not in the pool hides its keys: pages_bad has a bit for each
+  // such 16 keys of the tile copied last (page 0 is read in its place).
+  constexpr int NP = KT / 16;
+  uint32_t pages[NP], pages_bad = 0;
+  auto look_up = [&](int it) {
+    const int n0 = base0 + (it * KW + grp) * KT;
+#pragma unroll
+    for (int u = 0; u < NP; ++u) pages[u] = (uint32_t)uniform_load(table + (min(n0 + 16 * u, khi - 1) >> a.page_shift));
+  };
   auto issue = [&](int it, int buf) {
     const int n0 = base0 + (it * KW + grp) * KT + rbw * RPW;
+    if (paged) {
+      pages_bad = 0;
+#pragma unroll
+      for (int u = 0; u < NP; ++u) {
+        if (pages[u] >= (uint32_t)a.num_pages) pages_bad |= 1u << u, pages[u] = 0;
+      }
+    }
 #pragma unroll
     for (int u = 0; u < RPW / RU; ++u) {
       const int nu = min(n0 + RU * u, khi - 1);
       const char *kt, *vt;
       if (paged) {
-        const uint32_t pg = (uint32_t)uniform_load(table + (nu >> a.page_shift));
-        const int64_t page = pg < (uint32_t)a.num_pages ? pg : 0;
+        static_assert(RPW >= 16, "a wavefront's share of a tile begins with a page entry");
+        int64_t page = pages[u];
+#pragma unroll
+        for (int w = 1; w < RB; ++w) page = rbw == w ? pages[(w * RPW) / 16 + u] : page;
         kt = Kb + page * a.sK_b * 2 + (nu & pmask) * kstep;
         vt = Vb + page * a.sV_b * 2 + (nu & pmask) * vstep;
       } else {
@@ -228,23 +259,12 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
   };
   constexpr int kCopies = 2 * (RPW / 4);  // copies a wavefront issues per tile
 
-  // the first tile is under way before anything else is looked up
-  if (it0 < it1) issue(it0, 0);
-
-  // a page that the table does not name hides its keys; rare enough to look only once
-  bool bad_pages = false;
-  if (paged && it0 < it1) {
-    const int p0 = (base0 + it0 * KT * KW) >> a.page_shift, p1 = (min(khi, base0 + it1 * KT * KW) - 1) >> a.page_shift;
-    bool bad = false;
-    for (int p = p0 + lane; p <= p1; p += 64) bad |= (uint32_t)table[p] >= (uint32_t)a.num_pages;
-    bad_pages = __any(bad);
-  }
-
+  if (paged && it0 < it1) look_up(it0);
 
   // ---- this lane's row ------------------------------------------------------
   const int row = wg_row0 + rbw * kBlockRows + col;
   const bool live = row < rows;
-  const int t = live ? row / G : 0, g = live ? row - t * G : 0;
+  const int t = live ? a.div_G.quotient(row) : 0, g = live ? row - t * G : 0;
   int lo = INT32_MIN, hi = INT32_MAX;  // rows past the last see everything: they never make a tile partial
   uint64_t sees = ~0ull;
   int place = 0;  // position, for the distance
@@ -285,10 +305,13 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
       u32x4 x = live ? *reinterpret_cast<const u32x4*>(qp + 16 * s) : u32x4{0, 0, 0, 0};
       qf[s] = __builtin_bit_cast(bf16x8, x);
     }
-    // loaded here, not at their first use: a wait there would be one for the copies
-#pragma unroll
-    for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
   }
+  // the first tile is under way while the queries arrive
+  if (it0 < it1) issue(it0, 0);
+  if (RB == 1 && paged && it0 + 1 < it1) look_up(it0 + 1);
+  // waited for here, not at their first use: a wait there would be one for the copies
+#pragma unroll
+  for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
 
   f32x16 o[4];
 #pragma unroll
@@ -312,10 +335,10 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
   const float c1 = a.sm_scale * kLog2e;
   const float cap2 = a.softcap * kLog2e, capk = CAP ? 2.f * kLog2e * a.sm_scale / a.softcap : 0.f;
 
-  auto compute = [&](int it, int buf, uint64_t odd) {
+  auto compute = [&](int it, int buf, uint32_t bad, bool cleared, uint64_t odd) {
     const int n0 = base0 + (it * KW + grp) * KT;
     if (n0 >= any_hi || n0 + KT <= any_lo) return;
-    const bool full = n0 >= all_lo && n0 + KT <= all_hi && !bad_pages;  // every row sees every key
+    const bool full = n0 >= all_lo && n0 + KT <= all_hi && !bad;  // every row sees every key
     const uint32_t bo = buf * S::kTileBytes;
     uint32_t ka[8], va[4];
 #pragma unroll
@@ -375,18 +398,10 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
     if (!full) {
 #pragma unroll
       for (int k = 0; k < NB; ++k) {
-        bool hidden[2] = {false, false};
-        if (bad_pages) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const int n = n0 + 32 * k + 16 * u;
-            hidden[u] = n < khi && (uint32_t)uniform_load(table + (n >> a.page_shift)) >= (uint32_t)a.num_pages;
-          }
-        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int n = nl + 32 * k + 8 * (e / 4) + e % 4;
-          acc[k][e] = visible(n) && n < khi && !hidden[e / 8] ? acc[k][e] : -INFINITY;
+          acc[k][e] = visible(n) && n < khi && !(paged && (bad >> (2 * k + e / 8) & 1)) ? acc[k][e] : -INFINITY;
         }
       }
     }
@@ -453,7 +468,7 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
       __builtin_amdgcn_sched_group_barrier(kSchedLds, 2, 1);
       __builtin_amdgcn_sched_group_barrier(kSchedValu, 5, 1);
     }
-    if (!full && RB > 1) {
+    if (cleared && RB > 1) {
       odd = 0;
 #pragma unroll
       for (int w = 0; w < RB; ++w) odd |= odd_rows[buf][grp * RB + w];
@@ -463,11 +478,12 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
       const int i = __ffsll((long long)odd) - 1, n = n0 + i;
       odd &= odd - 1;
       if (n >= khi) continue;
-      const char* vr = Vb + n * vstep;
+      const LateArgs la = late_args();
+      const char* vr = Vb + n * la->sV_n * 2;
       if (paged) {
-        const uint32_t pg = (uint32_t)uniform_load(table + (n >> a.page_shift));
-        if (pg >= (uint32_t)a.num_pages) continue;
-        vr = Vb + pg * a.sV_b * 2 + (n & pmask) * vstep;
+        const uint32_t pg = (uint32_t)uniform_load(table + (n >> la->page_shift));
+        if (pg >= (uint32_t)la->num_pages) continue;
+        vr = Vb + (pg * la->sV_b + (n & ((1 << la->page_shift) - 1)) * la->sV_n) * 2;
       }
       const bool see = visible(n);
 #pragma unroll
@@ -514,17 +530,23 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
 
   for (int it = it0; it < it1; ++it) {
     const int buf = (it - it0) & 1;
+    const uint32_t bad = pages_bad;  // of this tile: issue() turns to the next
+    // (pages are looked up where copies are waited for: a scalar load in flight
+    // would make every read of LDS wait for it)
     if (RB > 1) {
+      if (paged && it + 1 < it1) look_up(it + 1);
       dma_wait<0>();
     } else if (it + 1 < it1) {  // the other buffer is this wavefront's own: its next tile can be under way already
       issue(it + 1, buf ^ 1);
+      if (paged && it + 2 < it1) look_up(it + 2);
       dma_wait<kCopies>();
     } else {
       dma_wait<0>();
     }
     const int n0 = base0 + (it * KW + grp) * KT;
+    const bool partial = n0 + KT > wg_all_hi || n0 < wg_all_lo || bad;
     uint64_t odd = 0;
-    if (n0 + KT > wg_all_hi || n0 < wg_all_lo || bad_pages) {
+    if (partial) {
       odd = clear_odd(buf);
       if (RB > 1 && lane == 0) odd_rows[buf][wid] = odd;
       lds_done();
@@ -537,7 +559,7 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
       if (it + 1 < it1) issue(it + 1, buf ^ 1);
     }
     asm volatile("" : : : "memory");
-    compute(it, buf, odd);
+    compute(it, buf, bad, partial, odd);
     lds_done();  // the reads of this buffer, before it is filled again
   }
 
@@ -584,12 +606,14 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
     }
     mrun = mx, lsum = tot;
   }
-  if (!live) return;
-  if (a.splits > 1) {
-    const int64_t at = ((int64_t)bh * rows + row) * a.splits + split;
-    if (half == 0) a.part_ml[at] = make_float2(mrun, lsum);
+  const LateArgs la = late_args();
+  const int end_row = (rb * RB + rbw) * kBlockRows + col, end_rows = la->T * la->G;
+  if (end_row >= end_rows) return;
+  if (la->splits > 1) {
+    const int64_t at = ((int64_t)bh * end_rows + end_row) * la->splits + split;
+    if (half == 0) la->part_ml[at] = make_float2(mrun, lsum);
     if (lsum == 0.f) return;
-    float* po = a.part_o + at * kHeadDim + 4 * half;
+    float* po = la->part_o + at * kHeadDim + 4 * half;
 #pragma unroll
     for (int c = 0; c < 16; ++c)
       *reinterpret_cast<float4*>(po + 8 * c) =
@@ -597,13 +621,15 @@ __global__ __launch_bounds__(RB* KW * 64, 2) void attn_kernel(AttnArgs a, int nr
     return;
   }
   const float inv = lsum == 0.f ? 0.f : 1.f / lsum;  // a row that sees no key: zeros
-  uint16_t* op = a.out + b * a.so_b + (int64_t)(h * G + g) * a.so_h + (int64_t)t * a.so_t + 4 * half;
+  const FastDiv by_G{la->div_G.mul, la->div_G.shift}, by_Hkv{la->div_Hkv.mul, la->div_Hkv.shift};
+  const int end_t = by_G.quotient(end_row), end_b = by_Hkv.quotient(bh);
+  const int head = (bh - end_b * la->Hkv) * la->G + end_row - end_t * la->G;
+  uint16_t* op = la->out + end_b * la->so_b + head * la->so_h + end_t * la->so_t + 4 * half;
 #pragma unroll
-  for (int c = 0; c < 16; ++c) {
+  for (int c = 0; c < 16; ++c)
     *reinterpret_cast<uint2*>(op + 8 * c) =
         make_uint2(cvt_pk_bf16(o[c / 4][4 * (c % 4)] * inv, o[c / 4][4 * (c % 4) + 1] * inv),
                    cvt_pk_bf16(o[c / 4][4 * (c % 4) + 2] * inv, o[c / 4][4 * (c % 4) + 3] * inv));
-  }
 }
 
 // The splits of a row joined: a wavefront per row.  Lane s holds split s's
@@ -614,10 +640,10 @@ template <bool TREE>
 __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
   const int rows = a.T * a.G, lane = threadIdx.x & 63, half = lane >> 5, d = 4 * (lane & 31);
   const uint32_t r = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // (bh, t, g)
-  const uint32_t bh = r / (uint32_t)rows;
-  if (bh >= (uint32_t)(a.B * a.Hkv)) return;
-  const int row = (int)(r - bh * rows), t = row / a.G, g = row - t * a.G;
-  const int b = (int)(bh / a.Hkv), h = (int)(bh - b * a.Hkv);
+  const int bh = (int)(r / (uint32_t)rows);
+  if (bh >= a.B * a.Hkv) return;
+  const int row = (int)r - bh * rows, t = a.div_G.quotient(row), g = row - t * a.G;
+  const int b = a.div_Hkv.quotient(bh), h = bh - b * a.Hkv;
   if (TREE) {
     const int len = uniform_load(a.lens + b);
     if (len < 0 || len > a.N - a.T) return;
@@ -665,18 +691,19 @@ static hipError_t allow_lds(const void* f, int bytes, std::atomic<uint64_t>& all
   return e;
 }
 
-template <int RB, int KW, int KT, bool TREE>
-static hipError_t launch_attn_shape(const AttnArgs& a) {
+template <int RB, int KW, int KT, AttnKind KIND>
+static hipError_t launch_attn_shape(AttnArgs a) {
   const int rows = a.T * a.G, nrb = (rows + RB * kBlockRows - 1) / (RB * kBlockRows);
   const int items = a.B * a.Hkv * nrb * a.splits;
-  const int grid = TREE ? (items / nrb + 7) / 8 * 8 * nrb : (items + 7) / 8 * 8;
+  a.nrb = nrb, a.items = items, a.div_nrb = FastDiv::by(nrb);
+  const int grid = KIND != kPrefill ? (items / nrb + 7) / 8 * 8 * nrb : (items + 7) / 8 * 8;
 #define BPC_ATTN(CAP, BIAS)                                                                                       \
   {                                                                                                               \
-    auto* f = attn_kernel<RB, KW, KT, TREE, CAP, BIAS>;                                                           \
-    constexpr int lds = AttnShape<RB, KW, KT, TREE, CAP, BIAS>::kLds;                                             \
+    auto* f = attn_kernel<RB, KW, KT, KIND, CAP, BIAS>;                                                           \
+    constexpr int lds = AttnShape<RB, KW, KT, KIND, CAP, BIAS>::kLds;                                             \
     static std::atomic<uint64_t> allowed{0}; /* devices on which the kernel may use that much LDS */               \
     if (hipError_t e = allow_lds(reinterpret_cast<const void*>(f), lds, allowed); e != hipSuccess) return e;      \
-    f<<<grid, RB * KW * 64, lds, a.stream>>>(a, nrb, items);                                                      \
+    f<<<grid, RB * KW * 64, lds, a.stream>>>(a);                                                      \
   }
   if (a.softcap > 0.f) {
     if (a.slopes) BPC_ATTN(true, true) else BPC_ATTN(true, false)
@@ -713,19 +740,20 @@ AttnPlan attn_plan(int B, int Hkv, int G, int T, int N) {
   return p;
 }
 
-template <bool TREE>
+template <AttnKind KIND>
 static hipError_t launch_attn_as(const AttnArgs& a, const AttnPlan& p) {
-  hipError_t e = p.rb == 1   ? launch_attn_shape<1, 4, 32, TREE>(a)
-                 : p.rb == 2 ? launch_attn_shape<2, 2, 32, TREE>(a)
-                             : launch_attn_shape<4, 1, 64, TREE>(a);
+  hipError_t e = p.rb == 1   ? launch_attn_shape<1, 4, 32, KIND>(a)
+                 : p.rb == 2 ? launch_attn_shape<2, 2, 32, KIND>(a)
+                             : launch_attn_shape<4, 1, 64, KIND>(a);
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.T * a.G;
-  attn_merge_kernel<TREE><<<(unsigned)((rows + 3) / 4), 256, 0, a.stream>>>(a);
+  attn_merge_kernel<KIND != kPrefill><<<(unsigned)((rows + 3) / 4), 256, 0, a.stream>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_attn(const AttnArgs& a, const AttnPlan& p) {
-  return a.lens ? launch_attn_as<true>(a, p) : launch_attn_as<false>(a, p);
+hipError_t launch_attn(AttnArgs a, const AttnPlan& p) {
+  a.div_G = FastDiv::by(a.G), a.div_Hkv = FastDiv::by(a.Hkv), a.div_splits = FastDiv::by(a.splits);
+  return !a.lens ? launch_attn_as<kPrefill>(a, p) : a.table ? launch_attn_as<kPagedTree>(a, p) : launch_attn_as<kTree>(a, p);
 }
 
 }  // namespace bpc

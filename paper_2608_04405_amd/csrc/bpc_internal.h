@@ -271,6 +271,19 @@ struct AppendPagedArgs {
 hipError_t launch_append_paged(const AppendPagedArgs& a);
 
 // ---- attention of many query rows -----------------------------------------
+// n / d of 0 <= n < 2^31 by a product (mul = 2^32 (2^shift - d) / d + 1, shift the
+// bits of d - 1): a division in a kernel costs it some 40 instructions.
+struct FastDiv {
+  uint32_t mul, shift;
+  static FastDiv by(int d) {
+    FastDiv f{0, 0};
+    while (f.shift < 31 && (1ull << f.shift) < (uint64_t)d) ++f.shift;
+    if (d > 1) f.mul = (uint32_t)(((1ull << 32) * ((1ull << f.shift) - (uint64_t)d)) / (uint64_t)d + 1);
+    return f;
+  }
+  __device__ __forceinline__ int quotient(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+};
+
 struct AttnArgs {
   const uint16_t* q;
   int64_t sq_b, sq_h, sq_t;
@@ -295,6 +308,8 @@ struct AttnArgs {
   uint16_t* out;
   int64_t so_b, so_h, so_t;
   int splits;
+  FastDiv div_G, div_Hkv, div_nrb, div_splits;
+  int nrb, items;  // row blocks of a (b, h), workgroups
   float2* part_ml;  // [B, Hkv, T G][splits] (max, sum), and o[128]
   float* part_o;
   hipStream_t stream;
@@ -305,7 +320,7 @@ struct AttnPlan {
   size_t off_ml, off_o, total;
 };
 AttnPlan attn_plan(int B, int Hkv, int G, int T, int N);
-hipError_t launch_attn(const AttnArgs& a, const AttnPlan& p);
+hipError_t launch_attn(AttnArgs a, const AttnPlan& p);
 
 struct BuildArgs {
   const uint16_t* K;

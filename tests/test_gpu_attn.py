@@ -237,3 +237,24 @@ def test_tree_hidden_drafts_do_not_reach():
     visible, dist = tree_view([50], tree, T, N)
     got = bpc.tree_attention(q.to(DEV), K.to(DEV), V.to(DEV), torch.tensor([50], dtype=torch.int32, device=DEV), as_int64(tree).to(DEV))
     check_attend(got, attend(q, K, V, visible, dist, SM))
+
+
+@pytest.mark.parametrize("Hq,Hkv,T", [(1, 1, 150), (4, 1, 70), (2, 2, 64), (8, 1, 4)])
+def test_prefill_odd_values_reach_all_who_see_them(Hq, Hkv, T):
+    """Values that are not finite in a tile that some rows see whole and others in part."""
+    N = T + 200
+    q, K, V = rand(1, 1, Hq, T, 128), rand(2, 1, Hkv, N, 128), rand(3, 1, Hkv, N, 128)
+    V[0, :, 201, 5], V[0, :, 203, 6], V[0, :, N - 2, 7], V[0, :, 150, 9] = float("nan"), float("inf"), float("-inf"), float("nan")
+    begin = torch.where(torch.arange(T) < 3, 160, 0)[None].int()
+    got, want = prefill(q, K, V, N - T, begin, None, 0.0, None)
+    check_attend(got, want)
+
+
+@pytest.mark.parametrize("T,Hq", [(40, 4), (20, 2), (3, 8)])
+def test_tree_odd_values_reach_all_who_see_them(T, Hq):
+    N = 150
+    q, K, V = rand(1, 1, Hq, T, 128), rand(2, 1, 1, N, 128), rand(3, 1, 1, N, 128)
+    V[0, 0, 99, 5], V[0, 0, 101, 6], V[0, 0, 2, 7] = float("nan"), float("inf"), float("-inf")
+    visible, dist = tree_view([100], None, T, N)
+    got = bpc.tree_attention(q.to(DEV), K.to(DEV), V.to(DEV), torch.tensor([100], dtype=torch.int32, device=DEV))
+    check_attend(got, attend(q, K, V, visible, dist, SM))
