@@ -714,17 +714,41 @@ static hipError_t launch_attn_shape(AttnArgs a) {
   return hipGetLastError();
 }
 
-AttnPlan attn_plan(int B, int Hkv, int G, int T, int N) {
+// How a call is cut, by a model of its time (us) over the shapes and numbers of
+// pieces S of the key axis.  A workgroup of a shape handles `keys` keys a step
+// and `slots` of them are resident on the chip.  A round of workgroups costs 3,
+// a step of 4 row blocks 1.5, or 2.1 where two workgroups share a compute unit;
+// a step of one row block (64 KiB of keys and values) 1.4 where neighbouring row
+// blocks find them in L2, else 1.7, or the memory's 2.7 with every compute unit
+// at it.  The join costs 2.5 and its partial results' way out and back.  Where
+// there are several rounds, workgroups of fewer keys make room for others: a
+// causal prefill's mean is less than its longest, ragged sequences' about 0.8.
+// Measured, one row block against four, and S against its neighbours:
+//   257 tokens, 8 heads (2 KV): 9.8 and 11.7 us; S = 2: 11.7
+//   1024 tokens, 32 heads: 45.8 and 28.2 us; S = 2: 41.3
+//   64 queries over 4096 keys: S = 4 of one row block 21.8, S = 16 of four 24.6
+//   4000 tokens, 4 heads (4 KV): S = 1 of one row block 69.5, S = 4 of four 47.8
+//   512 queries over 16384 keys: S = 2, 4, 8: 180, 152, 159 us
+//   one token over 4 x 4096 slots: S = 4, 8, 16: 22.9, 18.1, 24.0 us
+//   24 drafts over 8 x 32768 slots: S = 4, 8, 16: 239, 168, 172 us
+AttnPlan attn_plan(int B, int Hkv, int G, int T, int N, bool tree) {
   AttnPlan p{};
-  const int64_t rows = (int64_t)T * G;
-  p.rb = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-  const int64_t blocks = (rows + p.rb * kBlockRows - 1) / (p.rb * kBlockRows) * B * Hkv;
-  const int unit = p.rb == 1 ? 128 : 64;  // keys per step of a workgroup
-  const int64_t most = ((int64_t)N + 2 * unit - 1) / (2 * unit);
-  int64_t s = 1024 / blocks;
-  s = s > most ? most : s;
-  s = s > kMaxSplits ? kMaxSplits : s;
-  p.splits = s < 1 ? 1 : (int)s;
+  const int64_t rows = (int64_t)T * G, bh = (int64_t)B * Hkv;
+  double best = 0;
+  for (int rb = 1; rb <= 4; rb += 3) {
+    if (rb == 4 && rows <= kBlockRows) break;
+    const int64_t nrb = (rows + rb * kBlockRows - 1) / (rb * kBlockRows);
+    const int keys = rb == 1 ? 128 : 64, slots = rb == 1 ? 256 : 512;
+    const int64_t steps = ((int64_t)N + keys - 1) / keys;
+    for (int S = 1; S <= kMaxSplits && (S == 1 || S <= steps); S *= 2) {
+      const double wgs = (double)(bh * nrb * S), rounds = wgs <= slots ? 1 : wgs / slots;
+      const double step = rb == 4 ? (wgs > 256 ? 2.1 : 1.5) : nrb > 1 ? 1.4 : wgs > 161 ? 2.7 * (wgs < 256 ? wgs / 256 : 1) : 1.7;
+      const double mean = rounds == 1 ? 1 : tree ? 0.8 : 1.2 - 0.5 * (T < N ? (double)T / N : 1);
+      const double join = S == 1 ? 0 : 2.5 + (double)(bh * rows) * S * (2 * (kHeadDim + 2) * sizeof(float)) / 5e6;
+      const double us = 3 + rounds * (3 + mean * (double)((steps + S - 1) / S) * step) + join;
+      if (!p.rb || us < best) best = us, p.rb = rb, p.splits = S;
+    }
+  }
   size_t o = 0;
   auto take = [&](size_t bytes) {
     size_t at = o;
@@ -732,7 +756,7 @@ AttnPlan attn_plan(int B, int Hkv, int G, int T, int N) {
     return at;
   };
   if (p.splits > 1) {
-    const size_t n = (size_t)B * Hkv * rows * p.splits;
+    const size_t n = (size_t)(bh * rows) * p.splits;
     p.off_ml = take(n * sizeof(float2));
     p.off_o = take(n * kHeadDim * sizeof(float));
   }
@@ -742,9 +766,7 @@ AttnPlan attn_plan(int B, int Hkv, int G, int T, int N) {
 
 template <AttnKind KIND>
 static hipError_t launch_attn_as(const AttnArgs& a, const AttnPlan& p) {
-  hipError_t e = p.rb == 1   ? launch_attn_shape<1, 4, 32, KIND>(a)
-                 : p.rb == 2 ? launch_attn_shape<2, 2, 32, KIND>(a)
-                             : launch_attn_shape<4, 1, 64, KIND>(a);
+  const hipError_t e = p.rb == 1 ? launch_attn_shape<1, 4, 32, KIND>(a) : launch_attn_shape<4, 1, 64, KIND>(a);
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.T * a.G;
   attn_merge_kernel<KIND != kPrefill><<<(unsigned)((rows + 3) / 4), 256, 0, a.stream>>>(a);

@@ -742,7 +742,7 @@ static void attn_workspace(AttnArgs& a, const AttnPlan& plan, void* workspace) {
 }
 
 size_t bpc_prefill_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D) {
-  return attn_sizes_ok(B, Hq, Hkv, T, N, D) ? attn_plan(B, Hkv, Hq / Hkv, T, N).total : 0;
+  return attn_sizes_ok(B, Hq, Hkv, T, N, D) ? attn_plan(B, Hkv, Hq / Hkv, T, N, false).total : 0;
 }
 
 int bpc_prefill_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t, const uint16_t* K, int64_t sK_b,
@@ -764,7 +764,7 @@ int bpc_prefill_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t
   a.sm_scale = sm_scale, a.softcap = softcap, a.slopes = slopes;
   a.out = out, a.so_b = so_b, a.so_h = so_h, a.so_t = so_t;
   a.stream = static_cast<hipStream_t>(stream);
-  const AttnPlan plan = attn_plan(B, Hkv, a.G, T, N);
+  const AttnPlan plan = attn_plan(B, Hkv, a.G, T, N, false);
   if ((st = check_attn(a, Hq, D, plan, workspace, workspace_bytes))) return st;
   if (key_begin && (st = check_int32("key_begin", key_begin, sb_b))) return st;
   if (key_end && (st = check_int32("key_end", key_end, se_b))) return st;
@@ -775,7 +775,7 @@ int bpc_prefill_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t
 }
 
 size_t bpc_tree_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D) {
-  return T <= 64 && T <= N && attn_sizes_ok(B, Hq, Hkv, T, N, D) ? attn_plan(B, Hkv, Hq / Hkv, T, N).total : 0;
+  return T <= 64 && T <= N && attn_sizes_ok(B, Hq, Hkv, T, N, D) ? attn_plan(B, Hkv, Hq / Hkv, T, N, true).total : 0;
 }
 
 int bpc_tree_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t, const uint16_t* K, int64_t sK_b,
@@ -798,7 +798,7 @@ int bpc_tree_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq
   a.sm_scale = sm_scale, a.softcap = softcap, a.slopes = slopes;
   a.out = out, a.so_b = so_b, a.so_h = so_h, a.so_t = so_t;
   a.stream = static_cast<hipStream_t>(stream);
-  const AttnPlan plan = attn_plan(B, Hkv, a.G, T, N);
+  const AttnPlan plan = attn_plan(B, Hkv, a.G, T, N, true);
   if ((st = check_attn(a, Hq, D, plan, workspace, workspace_bytes))) return st;
   if ((st = check_int32("lens", lens, 0))) return st;
   if (tree) {

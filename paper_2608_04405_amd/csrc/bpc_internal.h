@@ -319,7 +319,7 @@ struct AttnPlan {
   int rb, splits;
   size_t off_ml, off_o, total;
 };
-AttnPlan attn_plan(int B, int Hkv, int G, int T, int N);
+AttnPlan attn_plan(int B, int Hkv, int G, int T, int N, bool tree);
 hipError_t launch_attn(AttnArgs a, const AttnPlan& p);
 
 struct BuildArgs {
