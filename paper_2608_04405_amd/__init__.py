@@ -678,21 +678,17 @@ def dense_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scale:
 # Rows on their way into the cache, and attention of many query rows
 # ---------------------------------------------------------------------------
 def _rows(t: torch.Tensor, name: str):
-    """The shape of a bf16 [B, H, T, 128] tensor with contiguous rows."""
-    if type(t) is torch.Tensor and t.dtype is torch.bfloat16:
-        s = t.shape
-        if len(s) == 4 and s[3] == 128 and t.stride(3) == 1 and 0 not in s:
-            return s
+    """(B, H, T, their strides) of a bf16 [B, H, T, 128] tensor with contiguous
+    rows; the stride of an extent of one, which torch leaves open, as 0."""
+    if type(t) is torch.Tensor and t.dtype is torch.bfloat16 and t.dim() == 4:
+        a, b, c, d = t.shape
+        x, y, z, one = t.stride()
+        if d == 128 and one == 1 and a and b and c:
+            return a, b, c, x if a > 1 else 0, y if b > 1 else 0, z if c > 1 else 0
     _need(t, name, torch.bfloat16, 4)
     _extent(t, name, (("ge", 1), ("ge", 1), ("ge", 1), 128))
-    return t.shape
-
-
-def _strides3(t: torch.Tensor):
-    """(batch, head, token) strides of [B, H, T, 128]; 0 for an extent of one,
-    whose stride torch leaves open."""
     (a, b, c, _), (x, y, z, _) = t.shape, t.stride()
-    return x if a > 1 else 0, y if b > 1 else 0, z if c > 1 else 0
+    return a, b, c, x if a > 1 else 0, y if b > 1 else 0, z if c > 1 else 0
 
 
 def _indices(t: Optional[torch.Tensor], name: str, shape, dtype=torch.int32) -> int:
@@ -707,13 +703,19 @@ def _indices(t: Optional[torch.Tensor], name: str, shape, dtype=torch.int32) -> 
     return t.stride(0) if len(shape) == 2 and shape[0] > 1 else 0
 
 
-def _written(t: torch.Tensor, name: str, shape) -> None:
-    _rows(t, name)
-    if t.shape != shape:
-        _extent(t, name, shape)
-    (a, b, c, _), (x, y, z, _) = shape, t.stride()
-    if (x < 128 and a > 1) or (y < 128 and b > 1) or (z < 128 and c > 1):
+def _written(t: torch.Tensor, name: str, B: int, H: int, T: int):
+    """The strides of a [B, H, T, 128] tensor whose rows a call writes."""
+    a, b, c, x, y, z = _rows(t, name)
+    if a != B or b != H or c != T:
+        _extent(t, name, (B, H, T, 128))
+    if (x < 128 and B > 1) or (y < 128 and H > 1) or (z < 128 and T > 1):
         raise ValueError(f"{name}: its rows must not overlap (strides {tuple(t.stride())})")
+    return x, y, z
+
+
+def _dense(B: int, H: int, T: int):
+    """The strides of a contiguous [B, H, T, 128] tensor."""
+    return H * T * 128, T * 128, 128
 
 
 def _norm_weight(w: Optional[torch.Tensor], name: str, H: int) -> int:
@@ -804,18 +806,18 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: Opti
         raise ValueError("q and k cannot both be None")
     Hq = Hkv = 0
     if q is not None:
-        B, Hq, T, _ = _rows(q, "q")
+        B, Hq, T, *sq = _rows(q, "q")
     if k is not None:
-        kB, Hkv, kT, _ = _rows(k, "k")
+        kB, Hkv, kT, *sk = _rows(k, "k")
         if q is None:
             B, T = kB, kT
         elif kB != B or kT != T:
             _extent(k, "k", (B, Hkv, T, 128))
     for t, src, nm in ((q_out, q, "q_out"), (k_out, k, "k_out")):
-        if t is not None:
-            if src is None:
-                raise ValueError(f"{nm} is given without its input")
-            _written(t, nm, src.shape)
+        if t is not None and src is None:
+            raise ValueError(f"{nm} is given without its input")
+    sqo = _dense(B, Hq, T) if q_out is None else _written(q_out, "q_out", B, Hq, T)
+    sko = _dense(B, Hkv, T) if k_out is None else _written(k_out, "k_out", B, Hkv, T)
     rows, R = _table(cos_sin)
     sp = 0
     if not R:
@@ -824,16 +826,16 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: Opti
         raise ValueError("pos is required with cos_sin")
     else:
         sp = _indices(pos, "pos", (B, T))
-    sq, sk = _norm_weight(wq, "wq", Hq), _norm_weight(wk, "wk", Hkv)
+    swq, swk = _norm_weight(wq, "wq", Hq), _norm_weight(wk, "wk", Hkv)
     _on_gpu(q, k, pos, cos_sin, wq, wk, q_out, k_out)
     with _place(k if q is None else q, stream):
         if q is not None and q_out is None:
-            q_out = q.new_empty(q.shape)
+            q_out = q.new_empty((B, Hq, T, 128))
         if k is not None and k_out is None:
-            k_out = k.new_empty(k.shape)
+            k_out = k.new_empty((B, Hkv, T, 128))
         _check(_lib.bpc_qk_norm_rope(
-            *(_NO_ROWS if q is None else (q.data_ptr(), *_strides3(q), q_out.data_ptr(), *_strides3(q_out), _ptr(wq), sq)),
-            *(_NO_ROWS if k is None else (k.data_ptr(), *_strides3(k), k_out.data_ptr(), *_strides3(k_out), _ptr(wk), sk)),
+            *(_NO_ROWS if q is None else (q.data_ptr(), *sq, q_out.data_ptr(), *sqo, _ptr(wq), swq)),
+            *(_NO_ROWS if k is None else (k.data_ptr(), *sk, k_out.data_ptr(), *sko, _ptr(wk), swk)),
             B, Hq, Hkv, T, 128, eps, _ptr(cos_sin), rows, R, interleaved, _ptr(pos), sp, _stream(stream)),
             "bpc_qk_norm_rope")
     return q_out, k_out
@@ -851,14 +853,12 @@ def append_kv_paged(k_new: torch.Tensor, v_new: torch.Tensor, K: torch.Tensor, V
     on), its key normed with wk and rotated as by qk_norm_rope on the way, by
     its slot or by rope_pos [B, T].  Tokens without a page, or without a row of
     cos_sin, are not stored."""
-    B, Hkv, T, _ = _rows(k_new, "k_new")
-    if _rows(v_new, "v_new") != k_new.shape:
+    B, Hkv, T, *skn = _rows(k_new, "k_new")
+    vB, vH, vT, *svn = _rows(v_new, "v_new")
+    if vB != B or vH != Hkv or vT != T:
         _extent(v_new, "v_new", (B, Hkv, T, 128))
-    pages, Hk, page, _ = _rows(K, "K")
-    if Hk != Hkv:
-        _extent(K, "K", (pages, Hkv, page, 128))
-    _written(K, "K", K.shape)
-    _written(V, "V", K.shape)
+    pages, Hk, page, *_ = _rows(K, "K")
+    sK, sV = _written(K, "K", pages, Hkv, page), _written(V, "V", pages, Hkv, page)
     _page_rows(page)
     st, max_pages = _block_table(block_table, B)
     _indices(pos, "pos", (B,))
@@ -871,10 +871,9 @@ def append_kv_paged(k_new: torch.Tensor, v_new: torch.Tensor, K: torch.Tensor, V
     _on_gpu(k_new, v_new, K, V, block_table, pos, count, cos_sin, rope_pos, wk)
     with _place(K, stream):
         _check(_lib.bpc_append_kv_paged(
-            k_new.data_ptr(), *_strides3(k_new), v_new.data_ptr(), *_strides3(v_new), K.data_ptr(), *_strides3(K), V.data_ptr(),
-            *_strides3(V), _ptr(block_table), st, max_pages, pages, page, _ptr(pos), _ptr(count), B, Hkv, T,
-            128, _ptr(wk), sw, eps, _ptr(cos_sin), rows, R, interleaved, _ptr(rope_pos), sr, _stream(stream)),
-            "bpc_append_kv_paged")
+            k_new.data_ptr(), *skn, v_new.data_ptr(), *svn, K.data_ptr(), *sK, V.data_ptr(), *sV,
+            block_table.data_ptr(), st, max_pages, pages, page, pos.data_ptr(), _ptr(count), B, Hkv, T, 128, _ptr(wk),
+            sw, eps, _ptr(cos_sin), rows, R, interleaved, _ptr(rope_pos), sr, _stream(stream)), "bpc_append_kv_paged")
 
 
 def prefill_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, D: int = 128) -> int:
@@ -887,20 +886,19 @@ def tree_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, D: int = 128
 
 def _attn_inputs(q, K, V, slopes, out, workspace):
     """Checks shared by prefill_attention and tree_attention; returns the sizes
-    of q and of K."""
-    B, Hq, T, _ = _rows(q, "q")
-    Kb, Hkv, Kn, _ = _rows(K, "K")
-    Vb, Vh, Vn, _ = _rows(V, "V")
+    and strides of q and out, and the sizes of K and V."""
+    B, Hq, T, *sq = _rows(q, "q")
+    Kb, Hkv, Kn, *_ = _rows(K, "K")
+    Vb, Vh, Vn, *_ = _rows(V, "V")
     if Hq % Hkv:
         raise ValueError(f"Hq={Hq} must be a multiple of Hkv={Hkv}")
     if slopes is not None:
         _need(slopes, "slopes", torch.float32, 1)
         _extent(slopes, "slopes", (Hq,))
-    if out is not None:
-        _written(out, "out", q.shape)
+    so = _dense(B, Hq, T) if out is None else _written(out, "out", B, Hq, T)
     if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous uint8 tensor")
-    return B, Hq, Hkv, T, Kb, Kn, Vb, Vh, Vn
+    return B, Hq, Hkv, T, sq, so, Kb, Kn, Vb, Vh, Vn
 
 
 def _cache_rows(K, V, B, Hkv, N) -> None:
@@ -923,7 +921,7 @@ def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scal
     prefix mask.  Scores are capped to softcap * tanh(s / softcap) when softcap
     > 0, then lowered by slopes[head] * distance.  A token that sees nothing
     gets zeros."""
-    B, Hq, Hkv, T, Kb, Kn, Vb, Vh, Vn = _attn_inputs(q, K, V, slopes, out, workspace)
+    B, Hq, Hkv, T, sq, so, Kb, Kn, Vb, Vh, Vn = _attn_inputs(q, K, V, slopes, out, workspace)
     N = Kn if N is None else N
     if N < 1:
         raise ValueError(f"N={N} must be >= 1")
@@ -942,13 +940,13 @@ def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scal
         sm_scale = 1.0 / math.sqrt(128)
     with _place(q, stream):
         if out is None:
-            out = q.new_empty(q.shape)
+            out = q.new_empty((B, Hq, T, 128))
         if workspace is None:
             need = _lib.bpc_prefill_workspace_bytes(B, Hq, Hkv, T, N, 128)
             workspace = q.new_empty(need, dtype=torch.uint8) if need else None
         _check(_lib.bpc_prefill_attention(
-            q.data_ptr(), *_strides3(q), K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], B, Hq, Hkv, T, N, pos0, 128,
-            sm_scale, softcap, _ptr(slopes), _ptr(key_begin), sb, _ptr(key_end), se, out.data_ptr(), *_strides3(out),
+            q.data_ptr(), *sq, K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], B, Hq, Hkv, T, N, pos0, 128,
+            sm_scale, softcap, _ptr(slopes), _ptr(key_begin), sb, _ptr(key_end), se, out.data_ptr(), *so,
             _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "bpc_prefill_attention")
     return out
 
@@ -971,7 +969,7 @@ def tree_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torc
     being lens[b] plus its depth.  A sequence whose lens[b] is not in [0, N - T]
     is skipped: its rows of `out` stay as they are (undefined where `out` is
     allocated here)."""
-    B, Hq, Hkv, T, Kb, Kn, Vb, Vh, Vn = _attn_inputs(q, K, V, slopes, out, workspace)
+    B, Hq, Hkv, T, sq, so, Kb, Kn, Vb, Vh, Vn = _attn_inputs(q, K, V, slopes, out, workspace)
     pages = page = st = 0
     if block_table is None:
         N = Kn if N is None else N
@@ -996,13 +994,13 @@ def tree_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torc
         sm_scale = 1.0 / math.sqrt(128)
     with _place(q, stream):
         if out is None:
-            out = q.new_empty(q.shape)
+            out = q.new_empty((B, Hq, T, 128))
         if workspace is None:
             need = _lib.bpc_tree_workspace_bytes(B, Hq, Hkv, T, N, 128)
             workspace = q.new_empty(need, dtype=torch.uint8) if need else None
         _check(_lib.bpc_tree_attention(
-            q.data_ptr(), *_strides3(q), K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], _ptr(block_table), st, pages,
+            q.data_ptr(), *sq, K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], _ptr(block_table), st, pages,
             page, lens.data_ptr(), _ptr(tree), sm, B, Hq, Hkv, T, N, 128, sm_scale, softcap, _ptr(slopes), out.data_ptr(),
-            *_strides3(out), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)),
+            *so, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)),
             "bpc_tree_attention")
     return out
