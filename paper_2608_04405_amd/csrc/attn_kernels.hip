@@ -281,7 +281,7 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
     place = a.pos0 + t;
   }
   // every row's keys cover [all_lo, all_hi); no row sees a key outside [any_lo, any_hi)
-  int all_lo = 0, all_hi = len, any_lo = 0, any_hi = khi;
+  int all_lo = 0, all_hi = len, any_lo = 0, any_hi = wg_row0 + rbw * kBlockRows < rows ? khi : 0;
   if (!TREE) {
     all_lo = wave_max(lo), all_hi = wave_min(hi);
     any_lo = wave_min(live && lo < hi ? lo : INT32_MAX), any_hi = wave_max(live && lo < hi ? hi : 0);
@@ -295,7 +295,8 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
     }
     __syncthreads();
   }
-  const float slope = BIAS && live ? a.slopes[h * G + g] * kLog2e : 0.f;
+  // in units of log2 behind a cap, else of the products: the scale follows later
+  const float slope = BIAS && live ? a.slopes[h * G + g] * (CAP ? kLog2e : 1.f / a.sm_scale) : 0.f;
 
   bf16x8 qf[8];
   {
@@ -364,10 +365,6 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
     __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 0);
     // key of score e of block k: n0 + 32 k + 8 (e / 4) + 4 half + e % 4
     const int nl = n0 + 4 * half;
-    // in units of log2: cap tanh(x) = cap - 2 cap / (1 + e^2x)
-    auto scored = [&](float z) {
-      return CAP ? fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * capk)), cap2) : z * c1;
-    };
     if (CAP || BIAS) {
       // (a distance beyond 2^24 is rounded to fp32 before it is weighed)
       const float ahead = (float)(place - nl);
@@ -377,7 +374,9 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int at = 32 * k + 8 * (e / 4) + e % 4;
-          float z = scored(acc[k][e]);
+          float z = acc[k][e];
+          // in units of log2: cap tanh(x) = cap - 2 cap / (1 + e^2x)
+          if (CAP) z = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * capk)), cap2);
           if (BIAS) {
             float dist = ahead - (float)at;
             if (TREE && drafts) {
@@ -412,7 +411,7 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
       for (int e = 0; e < 16; ++e) mt = fmaxf(mt, acc[k][e]);
     }
     mt = max_halves(mt);
-    if (!CAP && !BIAS) mt *= c1;
+    if (!CAP) mt *= c1;
     // the reference point of the exponentials moves only when a score lies more
     // than 2^8 above it, so that the products are seldom rescaled; any point
     // gives the same quotient
@@ -436,7 +435,7 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
         float p[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          p[i] = __builtin_amdgcn_exp2f((CAP || BIAS) ? acc[k][e + i] - mu : fmaf(acc[k][e + i], c1, -mu));
+          p[i] = __builtin_amdgcn_exp2f(CAP ? acc[k][e + i] - mu : fmaf(acc[k][e + i], c1, -mu));
         const bf16x2 pp = {(__bf16)p[0], (__bf16)p[1]};
         lsum = __builtin_amdgcn_fdot2_f32_bf16(pp, bf16x2{(__bf16)1.f, (__bf16)1.f}, lsum, false);
         pw[k][e / 8][e % 8 / 2] = __builtin_bit_cast(uint32_t, pp);
