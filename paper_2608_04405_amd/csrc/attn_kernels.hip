@@ -18,6 +18,8 @@
 // chunk ^ swz(row): eight consecutive rows' equal chunks (the K operand) and
 // four consecutive rows' neighbouring chunk pairs (the transposing reads that
 // make the V operand) then lie in different banks.
+#include <math.h>
+
 #include <atomic>
 #include <type_traits>
 
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
       const int nu = min(n0 + RU * u, khi - 1);
       const char *kt, *vt;
       if (paged) {
-        static_assert(RPW >= 16, "a wavefront's share of a tile begins with a page entry");
+        static_assert(!paged || RPW >= 16, "a wavefront's share of a tile begins with a page entry");
         int64_t page = pages[u];
 #pragma unroll
         for (int w = 1; w < RB; ++w) page = rbw == w ? pages[(w * RPW) / 16 + u] : page;
@@ -716,7 +718,8 @@ static hipError_t launch_attn_shape(AttnArgs a) {
 // How a call is cut, by a model of its time (us) over the shapes and numbers of
 // pieces S of the key axis.  A workgroup of a shape handles `keys` keys a step
 // and `slots` of them are resident on the chip.  A round of workgroups costs 3,
-// a step of 4 row blocks 1.5, or 2.1 where two workgroups share a compute unit;
+// a step of 4 row blocks 1.5, or 2.1 where two workgroups share a compute unit,
+// one of 8 row blocks 2.0 (these read each key once for twice the rows);
 // a step of one row block (64 KiB of keys and values) 1.4 where neighbouring row
 // blocks find them in L2, else 1.7, or the memory's 2.7 with every compute unit
 // at it.  The join costs 2.5 and its partial results' way out and back.  Where
@@ -726,6 +729,8 @@ static hipError_t launch_attn_shape(AttnArgs a) {
 //   257 tokens, 8 heads (2 KV): 9.8 and 11.7 us; S = 2: 11.7
 //   1024 tokens, 32 heads: 45.8 and 28.2 us; S = 2: 41.3
 //   64 queries over 4096 keys: S = 4 of one row block 21.8, S = 16 of four 24.6
+//   512 queries over 65536 keys: four row blocks 563, eight 530 us
+//   4096 tokens, 32 heads: four row blocks 157, eight 147 us
 //   4000 tokens, 4 heads (4 KV): S = 1 of one row block 69.5, S = 4 of four 47.8
 //   512 queries over 16384 keys: S = 2, 4, 8: 180, 152, 159 us
 //   one token over 4 x 4096 slots: S = 4, 8, 16: 22.9, 18.1, 24.0 us
@@ -734,14 +739,16 @@ AttnPlan attn_plan(int B, int Hkv, int G, int T, int N, bool tree) {
   AttnPlan p{};
   const int64_t rows = (int64_t)T * G, bh = (int64_t)B * Hkv;
   double best = 0;
-  for (int rb = 1; rb <= 4; rb += 3) {
-    if (rb == 4 && rows <= kBlockRows) break;
+  for (int rb = 1; rb <= (tree ? 4 : 8); rb = rb == 1 ? 4 : 2 * rb) {
+    if (rb > 1 && rows <= rb / 2 * kBlockRows) break;
     const int64_t nrb = (rows + rb * kBlockRows - 1) / (rb * kBlockRows);
-    const int keys = rb == 1 ? 128 : 64, slots = rb == 1 ? 256 : 512;
+    const int keys = rb == 1 ? 128 : 64, slots = rb == 4 ? 512 : 256;
     const int64_t steps = ((int64_t)N + keys - 1) / keys;
     for (int S = 1; S <= kMaxSplits && (S == 1 || S <= steps); S *= 2) {
-      const double wgs = (double)(bh * nrb * S), rounds = wgs <= slots ? 1 : wgs / slots;
-      const double step = rb == 4 ? (wgs > 256 ? 2.1 : 1.5) : nrb > 1 ? 1.4 : wgs > 161 ? 2.7 * (wgs < 256 ? wgs / 256 : 1) : 1.7;
+      const double wgs = (double)(bh * nrb * S), full = wgs / slots;
+      // a last round that is not full takes as long as another, at first
+      const double rounds = full <= 1 ? 1 : full < 8 ? 0.5 * (full + ceil(full)) : full;
+      const double step = rb == 8 ? 2.0 : rb == 4 ? (wgs > 256 ? 2.1 : 1.5) : nrb > 1 ? 1.4 : wgs > 161 ? 2.7 * (wgs < 256 ? wgs / 256 : 1) : 1.7;
       const double mean = rounds == 1 ? 1 : tree ? 0.8 : 1.2 - 0.5 * (T < N ? (double)T / N : 1);
       const double join = S == 1 ? 0 : 2.5 + (double)(bh * rows) * S * (2 * (kHeadDim + 2) * sizeof(float)) / 5e6;
       const double us = 3 + rounds * (3 + mean * (double)((steps + S - 1) / S) * step) + join;
@@ -765,7 +772,9 @@ AttnPlan attn_plan(int B, int Hkv, int G, int T, int N, bool tree) {
 
 template <AttnKind KIND>
 static hipError_t launch_attn_as(const AttnArgs& a, const AttnPlan& p) {
-  const hipError_t e = p.rb == 1 ? launch_attn_shape<1, 4, 32, KIND>(a) : launch_attn_shape<4, 1, 64, KIND>(a);
+  const hipError_t e = p.rb == 1 ? launch_attn_shape<1, 4, 32, KIND>(a)
+                       : p.rb == 4 ? launch_attn_shape<4, 1, 64, KIND>(a)
+                                   : launch_attn_shape<8, 1, 64, kPrefill>(a);
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.T * a.G;
   attn_merge_kernel<KIND != kPrefill><<<(unsigned)((rows + 3) / 4), 256, 0, a.stream>>>(a);
