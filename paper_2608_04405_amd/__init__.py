@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import math
 import os
 from typing import Optional, Sequence
@@ -231,17 +232,13 @@ def _exact_out(t: Optional[torch.Tensor], name: str, dtype, shape) -> None:
 
 def _on_gpu(*tensors) -> None:
     """Every given tensor (None entries skipped) on one GPU."""
-    dev = -1
-    for t in tensors:
-        if t is None:
-            continue
-        d = t.get_device()
-        if d < 0:
-            raise ValueError("every tensor must be on a GPU")
-        if dev < 0:
-            dev = d
-        elif d != dev:
-            raise ValueError(f"tensors on different devices: cuda:{dev} and {t.device}")
+    devices = {t.get_device() for t in tensors if t is not None}
+    if len(devices) == 1 and -1 not in devices:
+        return
+    if -1 in devices:
+        raise ValueError("every tensor must be on a GPU")
+    if devices:
+        raise ValueError("tensors on different devices: " + " and ".join(f"cuda:{d}" for d in sorted(devices)))
 
 
 def _budget(k: int, N: int, Ncap: int) -> None:
@@ -760,28 +757,23 @@ def _page_rows(page: int) -> None:
         raise ValueError(f"K: pages of {page} rows, must be a power of two, 16 to 2^20")
 
 
-_HERE = contextlib.nullcontext()
-
-
 @contextlib.contextmanager
-def _switch(dev, stream):
-    with torch.cuda.device(dev):
-        if isinstance(stream, torch.cuda.Stream):
-            with torch.cuda.stream(stream):
-                yield
-        else:
+def _place(t: torch.Tensor, stream):
+    """t's device and, when given, `stream` as the current ones: what a call
+    allocates then belongs to the stream that uses it, and its memory is not
+    reused elsewhere while the kernels run."""
+    if stream is not None:
+        if not isinstance(stream, torch.cuda.Stream):
+            raise TypeError("stream must be a torch.cuda.Stream")
+        if stream.device != t.device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors are on {t.device}")
+    with torch.cuda.device(t.device):
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             yield
 
 
-def _place(t: torch.Tensor, stream):
-    """The context of a call on tensors of t's device: that device current, and
-    what is allocated within it allocated on `stream`, so that its memory is not
-    reused elsewhere while the kernels run."""
-    if stream is None and t.get_device() == torch._C._cuda_getDevice():
-        return _HERE
-    if isinstance(stream, torch.cuda.Stream) and stream.device != t.device:
-        raise ValueError(f"the stream is on {stream.device}, the tensors are on {t.device}")
-    return _switch(t.device, stream)
+_current_device = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream
 
 
 _NO_ROWS = (None, 0, 0, 0, None, 0, 0, 0, None, 0)
@@ -828,16 +820,21 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: Opti
         sp = _indices(pos, "pos", (B, T))
     swq, swk = _norm_weight(wq, "wq", Hq), _norm_weight(wk, "wk", Hkv)
     _on_gpu(q, k, pos, cos_sin, wq, wk, q_out, k_out)
-    with _place(k if q is None else q, stream):
-        if q is not None and q_out is None:
-            q_out = q.new_empty((B, Hq, T, 128))
-        if k is not None and k_out is None:
-            k_out = k.new_empty((B, Hkv, T, 128))
-        _check(_lib.bpc_qk_norm_rope(
-            *(_NO_ROWS if q is None else (q.data_ptr(), *sq, q_out.data_ptr(), *sqo, _ptr(wq), swq)),
-            *(_NO_ROWS if k is None else (k.data_ptr(), *sk, k_out.data_ptr(), *sko, _ptr(wk), swk)),
-            B, Hq, Hkv, T, 128, eps, _ptr(cos_sin), rows, R, interleaved, _ptr(pos), sp, _stream(stream)),
-            "bpc_qk_norm_rope")
+    some = k if q is None else q
+    dev = some.get_device()
+    if stream is not None or dev != _current_device():
+        with _place(some, stream):
+            return qk_norm_rope(q, k, pos, cos_sin, wq=wq, wk=wk, eps=eps, interleaved=interleaved, q_out=q_out, k_out=k_out)
+    if q is not None and q_out is None:
+        q_out = q.new_empty((B, Hq, T, 128))
+    if k is not None and k_out is None:
+        k_out = k.new_empty((B, Hkv, T, 128))
+    status = _lib.bpc_qk_norm_rope(
+        *(_NO_ROWS if q is None else (q.data_ptr(), *sq, q_out.data_ptr(), *sqo, _ptr(wq), swq)),
+        *(_NO_ROWS if k is None else (k.data_ptr(), *sk, k_out.data_ptr(), *sko, _ptr(wk), swk)),
+        B, Hq, Hkv, T, 128, eps, _ptr(cos_sin), rows, R, interleaved, _ptr(pos), sp, _current_stream(dev))
+    if status:
+        _check(status, "bpc_qk_norm_rope")
     return q_out, k_out
 
 
@@ -869,19 +866,30 @@ def append_kv_paged(k_new: torch.Tensor, v_new: torch.Tensor, K: torch.Tensor, V
     sr = _indices(rope_pos, "rope_pos", (B, T))
     sw = _norm_weight(wk, "wk", Hkv)
     _on_gpu(k_new, v_new, K, V, block_table, pos, count, cos_sin, rope_pos, wk)
-    with _place(K, stream):
-        _check(_lib.bpc_append_kv_paged(
-            k_new.data_ptr(), *skn, v_new.data_ptr(), *svn, K.data_ptr(), *sK, V.data_ptr(), *sV,
-            block_table.data_ptr(), st, max_pages, pages, page, pos.data_ptr(), _ptr(count), B, Hkv, T, 128, _ptr(wk),
-            sw, eps, _ptr(cos_sin), rows, R, interleaved, _ptr(rope_pos), sr, _stream(stream)), "bpc_append_kv_paged")
+    dev = K.get_device()
+    if stream is not None or dev != _current_device():
+        with _place(K, stream):
+            return append_kv_paged(k_new, v_new, K, V, block_table, pos, count=count, cos_sin=cos_sin, rope_pos=rope_pos,
+                                   wk=wk, eps=eps, interleaved=interleaved)
+    status = _lib.bpc_append_kv_paged(
+        k_new.data_ptr(), *skn, v_new.data_ptr(), *svn, K.data_ptr(), *sK, V.data_ptr(), *sV, block_table.data_ptr(), st,
+        max_pages, pages, page, pos.data_ptr(), _ptr(count), B, Hkv, T, 128, _ptr(wk), sw, eps, _ptr(cos_sin), rows, R,
+        interleaved, _ptr(rope_pos), sr, _current_stream(dev))
+    if status:
+        _check(status, "bpc_append_kv_paged")
 
 
+@functools.lru_cache(maxsize=4096)  # (sizes alone decide it)
 def prefill_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, D: int = 128) -> int:
     return int(_lib.bpc_prefill_workspace_bytes(B, Hq, Hkv, T, N, D))
 
 
+@functools.lru_cache(maxsize=4096)
 def tree_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, D: int = 128) -> int:
     return int(_lib.bpc_tree_workspace_bytes(B, Hq, Hkv, T, N, D))
+
+
+_SM_SCALE = 1.0 / math.sqrt(128)
 
 
 def _attn_inputs(q, K, V, slopes, out, workspace):
@@ -936,18 +944,23 @@ def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scal
     sb = _indices(key_begin, "key_begin", (B, T))
     se = _indices(key_end, "key_end", (B, T))
     _on_gpu(q, K, V, slopes, key_begin, key_end, out, workspace)
-    if sm_scale is None:
-        sm_scale = 1.0 / math.sqrt(128)
-    with _place(q, stream):
-        if out is None:
-            out = q.new_empty((B, Hq, T, 128))
-        if workspace is None:
-            need = _lib.bpc_prefill_workspace_bytes(B, Hq, Hkv, T, N, 128)
-            workspace = q.new_empty(need, dtype=torch.uint8) if need else None
-        _check(_lib.bpc_prefill_attention(
-            q.data_ptr(), *sq, K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], B, Hq, Hkv, T, N, pos0, 128,
-            sm_scale, softcap, _ptr(slopes), _ptr(key_begin), sb, _ptr(key_end), se, out.data_ptr(), *so,
-            _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)), "bpc_prefill_attention")
+    dev = q.get_device()
+    if stream is not None or dev != _current_device():
+        with _place(q, stream):
+            return prefill_attention(q, K, V, sm_scale, N, pos0=pos0, softcap=softcap, slopes=slopes, key_begin=key_begin,
+                                     key_end=key_end, out=out, workspace=workspace)
+    if out is None:
+        out = q.new_empty((B, Hq, T, 128))
+    if workspace is None:
+        need = prefill_workspace_bytes(B, Hq, Hkv, T, N)
+        if need:
+            workspace = q.new_empty(need, dtype=torch.uint8)
+    status = _lib.bpc_prefill_attention(
+        q.data_ptr(), *sq, K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], B, Hq, Hkv, T, N, pos0, 128,
+        _SM_SCALE if sm_scale is None else sm_scale, softcap, _ptr(slopes), _ptr(key_begin), sb, _ptr(key_end), se,
+        out.data_ptr(), *so, _ptr(workspace), 0 if workspace is None else workspace.numel(), _current_stream(dev))
+    if status:
+        _check(status, "bpc_prefill_attention")
     return out
 
 
@@ -990,17 +1003,22 @@ def tree_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torc
     _indices(lens, "lens", (B,))
     sm = _indices(tree, "tree", (B, T), torch.int64)
     _on_gpu(q, K, V, lens, tree, block_table, slopes, out, workspace)
-    if sm_scale is None:
-        sm_scale = 1.0 / math.sqrt(128)
-    with _place(q, stream):
-        if out is None:
-            out = q.new_empty((B, Hq, T, 128))
-        if workspace is None:
-            need = _lib.bpc_tree_workspace_bytes(B, Hq, Hkv, T, N, 128)
-            workspace = q.new_empty(need, dtype=torch.uint8) if need else None
-        _check(_lib.bpc_tree_attention(
-            q.data_ptr(), *sq, K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], _ptr(block_table), st, pages,
-            page, lens.data_ptr(), _ptr(tree), sm, B, Hq, Hkv, T, N, 128, sm_scale, softcap, _ptr(slopes), out.data_ptr(),
-            *so, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)),
-            "bpc_tree_attention")
+    dev = q.get_device()
+    if stream is not None or dev != _current_device():
+        with _place(q, stream):
+            return tree_attention(q, K, V, lens, tree, sm_scale, N, block_table=block_table, softcap=softcap, slopes=slopes,
+                                  out=out, workspace=workspace)
+    if out is None:
+        out = q.new_empty((B, Hq, T, 128))
+    if workspace is None:
+        need = tree_workspace_bytes(B, Hq, Hkv, T, N)
+        if need:
+            workspace = q.new_empty(need, dtype=torch.uint8)
+    status = _lib.bpc_tree_attention(
+        q.data_ptr(), *sq, K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], _ptr(block_table), st, pages,
+        page, lens.data_ptr(), _ptr(tree), sm, B, Hq, Hkv, T, N, 128, _SM_SCALE if sm_scale is None else sm_scale,
+        softcap, _ptr(slopes), out.data_ptr(), *so, _ptr(workspace), 0 if workspace is None else workspace.numel(),
+        _current_stream(dev))
+    if status:
+        _check(status, "bpc_tree_attention")
     return out
