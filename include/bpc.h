@@ -581,7 +581,8 @@ int bpc_append_kv_paged(const uint16_t* k_new, int64_t sKn_b, int64_t sKn_h, int
  * K, V       [B, Hkv, >=N, D] bf16, strides as in bpc_decode_attention; any
  *            group size G = Hq / Hkv up to 128
  * pos0       >= 0
- * softcap    0 (none) or finite > 0
+ * sm_scale   2^-40 to 2^40
+ * softcap    0 (none), or 2^-20 to 1024
  * slopes     [Hq] fp32 or NULL
  * key_begin, key_end  [B, T] int32, strides sb_b, se_b (0 = shared), or NULL
  * out        [B, Hq, T, D] bf16, strides (so_b, so_h, so_t) (written)

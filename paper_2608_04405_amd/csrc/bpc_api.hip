@@ -711,9 +711,14 @@ static int check_attn(const AttnArgs& a, int Hq, int D, const AttnPlan& plan, co
   if ((st = check_written("out", a.out, a.so_b, a.so_h, a.so_t, a.B, Hq, a.T))) return st;
   if (!(a.sm_scale > 0.0f) || !__builtin_isfinite(a.sm_scale)) return fail(BPC_EINVAL, "sm_scale must be finite and > 0");
   if (!(a.softcap >= 0.0f) || !__builtin_isfinite(a.softcap)) return fail(BPC_EINVAL, "softcap must be finite and >= 0");
+  // fp32 holds slope * distance / sm_scale, and softcap * tanh() to 2^-12
+  if (a.sm_scale < 0x1p-40f || a.sm_scale > 0x1p40f) return fail(BPC_EUNSUPPORTED, "sm_scale=%g: 2^-40 to 2^40", a.sm_scale);
+  if (a.softcap != 0.0f && (a.softcap < 0x1p-20f || a.softcap > 1024.0f))
+    return fail(BPC_EUNSUPPORTED, "softcap=%g: 2^-20 to 1024", a.softcap);
   if (a.slopes && !aligned4(a.slopes)) return fail(BPC_EALIGN, "slopes must be 4-byte aligned");
   const int64_t blocks = ((int64_t)a.T * a.G + plan.rb * 32 - 1) / (plan.rb * 32) * a.B * a.Hkv * plan.splits;
-  if (blocks > (int64_t)(1 << 30)) return fail(BPC_EUNSUPPORTED, "%lld workgroups: too many rows in one call", (long long)blocks);
+  if (blocks > (int64_t)(1 << 30) || (plan.splits > 1 && (int64_t)a.B * a.Hkv * a.T * a.G > (int64_t)(1 << 30)))
+    return fail(BPC_EUNSUPPORTED, "%lld workgroups: too many rows in one call", (long long)blocks);
   if (plan.total) {
     if (!workspace || workspace_bytes < plan.total)
       return fail(BPC_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : 0, plan.total);

@@ -258,3 +258,20 @@ def test_tree_odd_values_reach_all_who_see_them(T, Hq):
     visible, dist = tree_view([100], None, T, N)
     got = bpc.tree_attention(q.to(DEV), K.to(DEV), V.to(DEV), torch.tensor([100], dtype=torch.int32, device=DEV))
     check_attend(got, attend(q, K, V, visible, dist, SM))
+
+
+@pytest.mark.parametrize("cap", [2.0 ** -20, 0.01, 1.0, 1024.0])
+@pytest.mark.parametrize("sm", [2.0 ** -40, 0.01, 1.0, 2.0 ** 10])
+def test_prefill_caps_and_scales(cap, sm):
+    """The ends of what is taken; scales at which scores saturate, all equal or one-hot."""
+    q, K, V = rand(1, 1, 2, 9, 128), rand(2, 1, 1, 77, 128), rand(3, 1, 1, 77, 128)
+    # one coordinate alone, a power of two per key: scores are exact, whatever their size
+    q[..., 1:], K[..., 1:] = 0, 0
+    q[..., 0], K[0, 0, :, 0] = 1, torch.tensor([2.0 ** (i % 5 - 2) * (-1) ** i for i in range(77)])
+    got = bpc.prefill_attention(dev(q), dev(K), dev(V), sm, softcap=cap)
+    visible = torch.ones(9, 77, dtype=torch.bool).tril(68)[None]
+    check_attend(got, attend(q, K, V, visible, torch.zeros(1, 9, 77), sm, cap))
+
+
+def dev(x):
+    return x.to(DEV)

@@ -200,7 +200,8 @@ TREE = (rows("q", 8) + rows("K", 2) + rows("V", 2) +
 ANY_ATTN = [
     (dict(q=None), EINVAL), (dict(K=None), EINVAL), (dict(V=None), EINVAL), (dict(o=None), EINVAL), (dict(B=0), EINVAL), (dict(T=0), EINVAL),
     (dict(N=0), EINVAL), (dict(Hq=9), EINVAL), (dict(Hq=2 * 129), EUNSUP), (dict(D=64), EUNSUP), (dict(sm=0.0), EINVAL),
-    (dict(sm=float("inf")), EINVAL), (dict(cap=-1.0), EINVAL), (dict(cap=float("nan")), EINVAL), (dict(slopes=FAKE + 2), EALIGN),
+    (dict(sm=float("inf")), EINVAL), (dict(cap=-1.0), EINVAL), (dict(cap=float("nan")), EINVAL), (dict(cap=1025.0), EUNSUP), (dict(cap=2.0 ** -21), EUNSUP),
+    (dict(sm=2.0 ** -41), EUNSUP), (dict(sm=2.0 ** 41), EUNSUP), (dict(slopes=FAKE + 2), EALIGN),
     (dict(q=FAKE + 2), EALIGN), (dict(o=FAKE + 8), EALIGN), (dict(K_t=100), EINVAL), (dict(K_t=132), EALIGN), (dict(V_t=1 << 25), EUNSUP),
     (dict(o_h=64), EINVAL), (dict(q_h=-8), EINVAL), (dict(ws=None), EWS), (dict(wsb=256), EWS), (dict(ws=FAKE + 16), EALIGN),
 ]
