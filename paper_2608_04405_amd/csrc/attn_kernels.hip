@@ -566,71 +566,72 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
 
   // ---- results ---------------------------------------------------------------
   lsum = sum_halves(lsum);
-  if (KW > 1) {
-    // the groups of a row block join in LDS: [group][row block][coordinate / 4][row] of 4 fp32, then (max, sum) [group][row block][row]
-    __syncthreads();
+  // coordinates 8 c + 4 half + 0..3 of this lane's row
+  auto sums = [&](int c) { return make_float4(o[c / 4][4 * (c % 4)], o[c / 4][4 * (c % 4) + 1], o[c / 4][4 * (c % 4) + 2], o[c / 4][4 * (c % 4) + 3]); };
+  constexpr int CW = 16 / KW;  // such groups of coordinates that a wavefront writes, from c0 on
+  float4 res[CW];
+  if (KW == 1) {
+#pragma unroll
+    for (int c = 0; c < CW; ++c) res[c] = sums(c);
+  } else {
+    // The groups of a row block join in LDS, each wavefront a quarter of the
+    // coordinates: sums [group][c][half][row], then (max, sum) [group][row].
+    static_assert(KW == 1 || RB == 1, "one row block");
+    static_assert(KW * (16 * 2 * kBlockRows * (int)sizeof(float4) + kBlockRows * (int)sizeof(float2)) <= S::kLds, "fits the tiles' LDS");
     float4* so = reinterpret_cast<float4*>(smem);
-    float2* sm = reinterpret_cast<float2*>(smem + (KW - 1) * RB * kBlockRows * kHeadDim * sizeof(float));
-    if (half == 0) sm[(grp * RB + rbw) * kBlockRows + col] = make_float2(mrun, lsum);
+    float2* sm = reinterpret_cast<float2*>(so + KW * 16 * 2 * kBlockRows);
     __syncthreads();
+#pragma unroll
+    for (int c = 0; c < 16; ++c) so[((grp * 16 + c) * 2 + half) * kBlockRows + col] = sums(c);
+    if (half == 0) sm[grp * kBlockRows + col] = make_float2(mrun, lsum);
+    __syncthreads();
+    float2 st[KW];
     float mx = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < KW; ++k) mx = fmaxf(mx, sm[(k * RB + rbw) * kBlockRows + col].x);
-    float tot = 0.f;
+    for (int k = 0; k < KW; ++k) {
+      st[k] = sm[k * kBlockRows + col];
+      mx = fmaxf(mx, st[k].x);
+    }
+    float tot = 0.f, f[KW];
 #pragma unroll
     for (int k = 0; k < KW; ++k) {
-      const float2 x = sm[(k * RB + rbw) * kBlockRows + col];
-      tot += x.y == 0.f ? 0.f : x.y * __builtin_amdgcn_exp2f(x.x - mx);
+      f[k] = st[k].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[k].x - mx);
+      tot = fmaf(st[k].y, f[k], tot);
     }
-    const float f = lsum == 0.f ? 0.f : __builtin_amdgcn_exp2f(mrun - mx);
 #pragma unroll
-    for (int d = 0; d < 4; ++d) {
+    for (int c = 0; c < CW; ++c) {
+      res[c] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) o[d][e] *= f;
-    }
-    if (grp > 0) {
-#pragma unroll
-      for (int c = 0; c < 16; ++c)
-        so[(((grp - 1) * RB + rbw) * 32 + 2 * c + half) * kBlockRows + col] =
-            make_float4(o[c / 4][4 * (c % 4)], o[c / 4][4 * (c % 4) + 1], o[c / 4][4 * (c % 4) + 2], o[c / 4][4 * (c % 4) + 3]);
-    }
-    __syncthreads();
-    if (grp > 0) return;
-#pragma unroll
-    for (int k = 0; k < KW - 1; ++k) {
-#pragma unroll
-      for (int c = 0; c < 16; ++c) {
-        const float4 x = so[((k * RB + rbw) * 32 + 2 * c + half) * kBlockRows + col];
-        o[c / 4][4 * (c % 4)] += x.x, o[c / 4][4 * (c % 4) + 1] += x.y;
-        o[c / 4][4 * (c % 4) + 2] += x.z, o[c / 4][4 * (c % 4) + 3] += x.w;
+      for (int k = 0; k < KW; ++k) {
+        const float4 x = so[((k * 16 + grp * CW + c) * 2 + half) * kBlockRows + col];
+        res[c].x = fmaf(x.x, f[k], res[c].x), res[c].y = fmaf(x.y, f[k], res[c].y);
+        res[c].z = fmaf(x.z, f[k], res[c].z), res[c].w = fmaf(x.w, f[k], res[c].w);
       }
     }
     mrun = mx, lsum = tot;
   }
   const LateArgs la = late_args();
+  const int d0 = 8 * CW * (KW > 1 ? grp : 0) + 4 * half;
   const int end_row = (rb * RB + rbw) * kBlockRows + col, end_rows = la->T * la->G;
   if (end_row >= end_rows) return;
   if (la->splits > 1) {
     const int64_t at = ((int64_t)bh * end_rows + end_row) * la->splits + split;
-    if (half == 0) la->part_ml[at] = make_float2(mrun, lsum);
+    if (d0 == 0) la->part_ml[at] = make_float2(mrun, lsum);
     if (lsum == 0.f) return;
-    float* po = la->part_o + at * kHeadDim + 4 * half;
+    float* po = la->part_o + at * kHeadDim + d0;
 #pragma unroll
-    for (int c = 0; c < 16; ++c)
-      *reinterpret_cast<float4*>(po + 8 * c) =
-          make_float4(o[c / 4][4 * (c % 4)], o[c / 4][4 * (c % 4) + 1], o[c / 4][4 * (c % 4) + 2], o[c / 4][4 * (c % 4) + 3]);
+    for (int c = 0; c < CW; ++c) *reinterpret_cast<float4*>(po + 8 * c) = res[c];
     return;
   }
   const float inv = lsum == 0.f ? 0.f : 1.f / lsum;  // a row that sees no key: zeros
   const FastDiv by_G{la->div_G.mul, la->div_G.shift}, by_Hkv{la->div_Hkv.mul, la->div_Hkv.shift};
   const int end_t = by_G.quotient(end_row), end_b = by_Hkv.quotient(bh);
   const int head = (bh - end_b * la->Hkv) * la->G + end_row - end_t * la->G;
-  uint16_t* op = la->out + end_b * la->so_b + head * la->so_h + end_t * la->so_t + 4 * half;
+  uint16_t* op = la->out + end_b * la->so_b + head * la->so_h + end_t * la->so_t + d0;
 #pragma unroll
-  for (int c = 0; c < 16; ++c)
+  for (int c = 0; c < CW; ++c)
     *reinterpret_cast<uint2*>(op + 8 * c) =
-        make_uint2(cvt_pk_bf16(o[c / 4][4 * (c % 4)] * inv, o[c / 4][4 * (c % 4) + 1] * inv),
-                   cvt_pk_bf16(o[c / 4][4 * (c % 4) + 2] * inv, o[c / 4][4 * (c % 4) + 3] * inv));
+        make_uint2(cvt_pk_bf16(res[c].x * inv, res[c].y * inv), cvt_pk_bf16(res[c].z * inv, res[c].w * inv));
 }
 
 // The splits of a row joined: a wavefront per row.  Lane s holds split s's
