@@ -15,8 +15,8 @@
 //
 // K and V tiles go from global memory to LDS without passing registers, double
 // buffered.  A row of 256 bytes holds its sixteen 16-byte chunks at position
-// chunk ^ swz(row): eight consecutive rows' equal chunks (the K operand) and
-// four consecutive rows' neighbouring chunk pairs (the transposing reads that
+// chunk ^ swz(row): sixteen consecutive rows' equal chunks (the K operand) and
+// four consecutive rows' neighbouring four chunks (the transposing reads that
 // make the V operand) then lie in different banks.
 #include <math.h>
 
@@ -44,7 +44,7 @@ constexpr int kBlockRows = 32;  // query rows of a wavefront
 constexpr int kMaxSplits = 64;  // pieces of the key axis
 
 __device__ __forceinline__ uint32_t swz(uint32_t row) {
-  return (row & 8u) | ((row & 3u) << 1) | ((row >> 2) & 1u);
+  return ((row & 3u) << 2) | ((row >> 2) & 3u);
 }
 
 __device__ __forceinline__ uint32_t cvt_pk_bf16(float lo, float hi) {
@@ -343,11 +343,11 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
     if (n0 >= any_hi || n0 + KT <= any_lo) return;
     const bool full = n0 >= all_lo && n0 + KT <= all_hi && !bad;  // every row sees every key
     const uint32_t bo = buf * S::kTileBytes;
-    uint32_t ka[8], va[4];
+    uint32_t ka[8], va[4], vb[4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) ka[i] = opaque(kaddr[i] + bo);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) va[i] = opaque(vaddr[i] + bo);
+    for (int i = 0; i < 4; ++i) va[i] = opaque(vaddr[i] + bo), vb[i] = opaque(va[i] ^ 32u);
     f32x16 acc[NB];
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
@@ -451,9 +451,9 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
           // keys 16 s + 4 half + j and 16 s + 8 + 4 half + j: the second lies eight
-          // rows on, whose swizzle differs in bit 3
+          // rows on, whose swizzle differs in bit 1
           const uint32_t at = (32 * k + 16 * s) * kRowBytes;
-          const s16x8 vf = __builtin_shufflevector(lds_read_tr(va[d], at), lds_read_tr(va[d ^ 2], at + 8 * kRowBytes), 0, 1,
+          const s16x8 vf = __builtin_shufflevector(lds_read_tr(va[d], at), lds_read_tr(vb[d], at + 8 * kRowBytes), 0, 1,
                                                    2, 3, 4, 5, 6, 7);
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), pf, o[d], 0, 0, 0);
         }
