@@ -22,7 +22,7 @@
 // Bound by the matrix units and the power limit where rows are many (2 x 8192
 // causal tokens, 32 heads: 1.09 ms, 1.0 PFLOP/s of visible pairs, matrix units 44 %
 // busy at 2.1 GHz), by memory where they are few (8 tokens over 16 x 131072 slots:
-// 1.04 ms, 6.2 TB/s), by vector issue where scores are capped (8001 tokens in
+// 0.94 ms, 6.8 TB/s), by vector issue where scores are capped (8001 tokens in
 // documents: 0.19 ms, 0.55 PFLOP/s).
 #include <math.h>
 
@@ -81,11 +81,19 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t x) {
 // such copy in flight before any LDS read; the kernel waits by itself (dma_wait).
 // No register is written, so there is nothing in flight that the compiler does
 // not know of but the LDS bytes, which it cannot touch before dma_wait.
+// ONCE: bytes that no other workgroup reads, which need not stay in a cache.
+template <bool ONCE>
 __device__ __forceinline__ void dma16(const char* base, uint32_t off, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-               :
-               : "v"(off), "s"(base), "s"(dst)
-               : "memory");
+  if (ONCE)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+                 :
+                 : "v"(off), "s"(base), "s"(dst)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(off), "s"(base), "s"(dst)
+                 : "memory");
 }
 template <int N>
 __device__ __forceinline__ void dma_wait() {  // until at most N copies of this wavefront are in flight
@@ -135,7 +143,7 @@ struct AttnShape {
   static constexpr int kLds = KW * 2 * 2 * kTileBytes;  // K and V, two buffers, per group
 };
 
-template <int RB, int KW, int KT, AttnKind KIND, bool CAP, bool BIAS>
+template <int RB, int KW, int KT, AttnKind KIND, bool CAP, bool BIAS, bool ONCE>
 __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnArgs a) {
   using S = AttnShape<RB, KW, KT, KIND, CAP, BIAS>;
   constexpr bool TREE = KIND != kPrefill, paged = KIND == kPagedTree;
@@ -252,15 +260,15 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
       if (last >= RU - 1) {
 #pragma unroll
         for (int i = 0; i < RU / 4; ++i) {
-          dma16(kt, koff[i], ldsK + dst + 4 * i * kRowBytes);
-          dma16(vt, voff[i], ldsV + dst + 4 * i * kRowBytes);
+          dma16<ONCE>(kt, koff[i], ldsK + dst + 4 * i * kRowBytes);
+          dma16<ONCE>(vt, voff[i], ldsV + dst + 4 * i * kRowBytes);
         }
       } else {
 #pragma unroll
         for (int i = 0; i < RU / 4; ++i) {
           const uint32_t r = min(4 * i + r4, last);
-          dma16(kt, r * (uint32_t)kstep + chunk[i], ldsK + dst + 4 * i * kRowBytes);
-          dma16(vt, r * (uint32_t)vstep + chunk[i], ldsV + dst + 4 * i * kRowBytes);
+          dma16<ONCE>(kt, r * (uint32_t)kstep + chunk[i], ldsK + dst + 4 * i * kRowBytes);
+          dma16<ONCE>(vt, r * (uint32_t)vstep + chunk[i], ldsV + dst + 4 * i * kRowBytes);
         }
       }
     }
@@ -700,7 +708,7 @@ static hipError_t allow_lds(const void* f, int bytes, std::atomic<uint64_t>& all
   return e;
 }
 
-template <int RB, int KW, int KT, AttnKind KIND>
+template <int RB, int KW, int KT, AttnKind KIND, bool ONCE = false>
 static hipError_t launch_attn_shape(AttnArgs a) {
   const int rows = a.T * a.G, nrb = (rows + RB * kBlockRows - 1) / (RB * kBlockRows);
   const int items = a.B * a.Hkv * nrb * a.splits;
@@ -708,7 +716,7 @@ static hipError_t launch_attn_shape(AttnArgs a) {
   const int grid = KIND != kPrefill ? (items / nrb + 7) / 8 * 8 * nrb : (items + 7) / 8 * 8;
 #define BPC_ATTN(CAP, BIAS)                                                                                       \
   {                                                                                                               \
-    auto* f = attn_kernel<RB, KW, KT, KIND, CAP, BIAS>;                                                           \
+    auto* f = attn_kernel<RB, KW, KT, KIND, CAP, BIAS, ONCE>;                                                           \
     constexpr int lds = AttnShape<RB, KW, KT, KIND, CAP, BIAS>::kLds;                                             \
     static std::atomic<uint64_t> allowed{0}; /* devices on which the kernel may use that much LDS */               \
     if (hipError_t e = allow_lds(reinterpret_cast<const void*>(f), lds, allowed); e != hipSuccess) return e;      \
@@ -780,7 +788,13 @@ AttnPlan attn_plan(int B, int Hkv, int G, int T, int N, bool tree) {
 
 template <AttnKind KIND>
 static hipError_t launch_attn_as(const AttnArgs& a, const AttnPlan& p) {
-  const hipError_t e = p.rb == 1 ? launch_attn_shape<1, 4, 32, KIND>(a)
+  // Keys that one row block reads, and more of them than the last-level cache
+  // (256 MB) holds until the next call, pass it by: 16 x 32768 slots, one token, 276
+  // and 246 us, 16 x 131072, eight tokens, 1047 and 945 us (6.9 TB/s); but 8 heads
+  // of 65536 keys (268 MB) 49 and 52 us, and for several row blocks 168 and 174 us
+  // (16 tokens over 8 x 32768 slots), 1094 and 1116 us (2 x 8192 causal tokens).
+  const bool once = (int64_t)a.T * a.G <= kBlockRows && (int64_t)a.B * a.Hkv * a.N * (4 * kHeadDim) > (int64_t)320 << 20;
+  const hipError_t e = p.rb == 1   ? once ? launch_attn_shape<1, 4, 32, KIND, true>(a) : launch_attn_shape<1, 4, 32, KIND>(a)
                        : p.rb == 4 ? launch_attn_shape<4, 1, 64, KIND>(a)
                                    : launch_attn_shape<8, 1, 64, kPrefill>(a);
   if (e != hipSuccess || a.splits == 1) return e;
