@@ -12,7 +12,7 @@
 // raw values: R / 16 lanes away for pairs (i, i + R/2), where R = 128 is one
 // DPP rotation by eight lanes, or in the same 32-bit word for adjacent pairs.
 // Bound by memory: the loads of kRopeBatch passes are issued before the first is
-// used.  32749 tokens of 40 heads take 136 us (5.06 TB/s; a copy of as many bytes
+// used.  32749 tokens of 40 heads take 124 us (5.5 TB/s; a copy of as many bytes
 // runs at 5.4), the append of 4 x 8192 tokens of 8 heads 38 us, one token 2.5 us.
 #include "bpc_internal.h"
 
@@ -155,38 +155,56 @@ __device__ __forceinline__ uint4 turn_row(const uint4& x, bool norm, float eps, 
   return make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
 }
 
+// 16 bytes of a row; STREAM: past the caches
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <bool STREAM>
+__device__ __forceinline__ uint4 load_chunk(const uint16_t* p) {
+  const u32x4* at = reinterpret_cast<const u32x4*>(p);
+  const u32x4 x = STREAM ? __builtin_nontemporal_load(at) : *at;
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+template <bool STREAM>
+__device__ __forceinline__ void store_chunk(uint16_t* p, const uint4& y) {
+  u32x4* at = reinterpret_cast<u32x4*>(p);
+  const u32x4 x = {y.x, y.y, y.z, y.w};
+  if (STREAM)
+    __builtin_nontemporal_store(x, at);
+  else
+    *at = x;
+}
+
 // Passes [p0, p1) of a token's heads through `row(chunk, head)`, from `src` with
 // head stride ss to `dst` with head stride sd: up to kRopeBatch passes' loads
 // before the first is used.
-template <int N, class Row>
+template <int N, bool STREAM, class Row>
 __device__ __forceinline__ void move_passes(const uint16_t* src, int64_t ss, uint16_t* dst, int64_t sd, int H, int p, Row row) {
   const int sub = (threadIdx.x & 63) / kRowLanes, d0 = 8 * (threadIdx.x % kRowLanes);
   uint4 x[N];
 #pragma unroll
   for (int i = 0; i < N; ++i)
-    x[i] = *reinterpret_cast<const uint4*>(src + min((p + i) * kPassRows + sub, H - 1) * ss + d0);
+    x[i] = load_chunk<STREAM>(src + min((p + i) * kPassRows + sub, H - 1) * ss + d0);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int h = (p + i) * kPassRows + sub;
     const uint4 y = row(x[i], min(h, H - 1));
-    if (h < H) *reinterpret_cast<uint4*>(dst + h * sd + d0) = y;
+    if (h < H) store_chunk<STREAM>(dst + h * sd + d0, y);
   }
 }
-template <class Row>
+template <bool STREAM, class Row>
 __device__ __forceinline__ void move_heads(const uint16_t* src, int64_t ss, uint16_t* dst, int64_t sd, int H, int p0, int p1, Row row) {
   int p = p0;
-  for (; p + kRopeBatch <= p1; p += kRopeBatch) move_passes<kRopeBatch>(src, ss, dst, sd, H, p, row);
-  if (p + 2 <= p1) move_passes<2>(src, ss, dst, sd, H, p, row), p += 2;
-  if (p < p1) move_passes<1>(src, ss, dst, sd, H, p, row);
+  for (; p + kRopeBatch <= p1; p += kRopeBatch) move_passes<kRopeBatch, STREAM>(src, ss, dst, sd, H, p, row);
+  if (p + 2 <= p1) move_passes<2, STREAM>(src, ss, dst, sd, H, p, row), p += 2;
+  if (p < p1) move_passes<1, STREAM>(src, ss, dst, sd, H, p, row);
 }
 
 // rows of H heads of one token; PER_HEAD: weights of their own for every head
-template <Pairing PAIR, bool PER_HEAD>
+template <Pairing PAIR, bool PER_HEAD, bool STREAM>
 __device__ __forceinline__ void turn_heads(const uint16_t* src, int64_t ss, uint16_t* dst, int64_t sd, const uint16_t* w,
                                            int64_t sw, float eps, const Turn& t, int H, int p0, int p1) {
   float C[8], S[8];
   if (!PER_HEAD) row_factors<PAIR>(t, w, C, S);
-  move_heads(src, ss, dst, sd, H, p0, p1, [&](const uint4& x, int h) {
+  move_heads<STREAM>(src, ss, dst, sd, H, p0, p1, [&](const uint4& x, int h) {
     if (PER_HEAD) row_factors<PAIR>(t, w ? w + h * sw : nullptr, C, S);
     return turn_row<PAIR>(x, w != nullptr, eps, t, C, S);
   });
@@ -196,7 +214,7 @@ __device__ __forceinline__ void turn_heads(const uint16_t* src, int64_t ss, uint
 // qk_norm_rope: a wavefront takes `per` of the passes of one token, those of the
 // query heads before those of the key heads
 // ---------------------------------------------------------------------------
-template <Pairing PAIR, bool PER_HEAD>
+template <Pairing PAIR, bool PER_HEAD, bool STREAM>
 __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, int per, int parts) {
   // (fewer than 2^32 wavefronts: 2^30 tokens, or few of them in parts)
   const uint32_t wave = blockIdx.x * kRopeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -213,10 +231,10 @@ __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, 
   const int nq = (a.q.H + kPassRows - 1) / kPassRows, nk = (a.k.H + kPassRows - 1) / kPassRows;
   const int p0 = (int)(wave - tok * (uint32_t)parts) * per, p1 = min(nq + nk, p0 + per);
   if (p0 < nq)
-    turn_heads<PAIR, PER_HEAD>(a.q.in + b * a.q.si_b + t * a.q.si_t, a.q.si_h, a.q.out + b * a.q.so_b + t * a.q.so_t,
+    turn_heads<PAIR, PER_HEAD, STREAM>(a.q.in + b * a.q.si_b + t * a.q.si_t, a.q.si_h, a.q.out + b * a.q.so_b + t * a.q.so_t,
                                a.q.so_h, a.q.w, a.q.sw_h, a.eps, turn, a.q.H, p0, min(p1, nq));
   if (p1 > nq)
-    turn_heads<PAIR, PER_HEAD>(a.k.in + b * a.k.si_b + t * a.k.si_t, a.k.si_h, a.k.out + b * a.k.so_b + t * a.k.so_t,
+    turn_heads<PAIR, PER_HEAD, STREAM>(a.k.in + b * a.k.si_b + t * a.k.si_t, a.k.si_h, a.k.out + b * a.k.so_b + t * a.k.so_t,
                                a.k.so_h, a.k.w, a.k.sw_h, a.eps, turn, a.k.H, max(p0 - nq, 0), p1 - nq);
 }
 
@@ -232,12 +250,12 @@ static Pairing pairing_of(int R, int inter) {
   return R == 0 ? kPairNone : inter ? kPairAdjacent : R == kHeadDim ? kPairEight : kPairLanes;
 }
 
-#define BPC_BY_PAIRING(KERNEL, PER_HEAD, ...)                                                          \
-  switch (pairing_of(a.R, a.inter)) {                                                                  \
-    case kPairNone: KERNEL<kPairNone, PER_HEAD><<<grid, kRopeThreads, 0, a.stream>>>(__VA_ARGS__); break;   \
-    case kPairEight: KERNEL<kPairEight, PER_HEAD><<<grid, kRopeThreads, 0, a.stream>>>(__VA_ARGS__); break; \
-    case kPairLanes: KERNEL<kPairLanes, PER_HEAD><<<grid, kRopeThreads, 0, a.stream>>>(__VA_ARGS__); break; \
-    case kPairAdjacent: KERNEL<kPairAdjacent, PER_HEAD><<<grid, kRopeThreads, 0, a.stream>>>(__VA_ARGS__); break; \
+#define BPC_BY_PAIRING(KERNEL, ...)                             \
+  switch (pairing_of(a.R, a.inter)) {                           \
+    case kPairNone: KERNEL(kPairNone, __VA_ARGS__) break;         \
+    case kPairEight: KERNEL(kPairEight, __VA_ARGS__) break;       \
+    case kPairLanes: KERNEL(kPairLanes, __VA_ARGS__) break;       \
+    case kPairAdjacent: KERNEL(kPairAdjacent, __VA_ARGS__) break; \
   }
 
 hipError_t launch_qk_norm_rope(const RopeArgs& a) {
@@ -245,11 +263,18 @@ hipError_t launch_qk_norm_rope(const RopeArgs& a) {
   const int64_t tokens = (int64_t)a.B * a.T;
   const int per = passes_per_wave(tokens, passes), parts = (passes + per - 1) / per;
   const unsigned grid = (unsigned)((tokens * parts + kRopeWaves - 1) / kRopeWaves);
-  if ((a.q.w && a.q.sw_h) || (a.k.w && a.k.sw_h)) {
-    BPC_BY_PAIRING(qk_norm_rope_kernel, true, a, per, parts)
+  const bool per_head = (a.q.w && a.q.sw_h) || (a.k.w && a.k.sw_h);
+  // More rows than the last-level cache (256 MB) could hold for their reader pass
+  // it by: 32749 tokens of 40 heads (335 MB out) 136 and 124 us.
+  const bool stream = tokens * (a.q.H + a.k.H) * (kHeadDim * 2) > (int64_t)256 << 20;
+#define BPC_QK(PAIR, PER_HEAD, STREAM) \
+  qk_norm_rope_kernel<PAIR, PER_HEAD, STREAM><<<grid, kRopeThreads, 0, a.stream>>>(a, per, parts);
+  if (per_head) {
+    if (stream) BPC_BY_PAIRING(BPC_QK, true, true) else BPC_BY_PAIRING(BPC_QK, true, false)
   } else {
-    BPC_BY_PAIRING(qk_norm_rope_kernel, false, a, per, parts)
+    if (stream) BPC_BY_PAIRING(BPC_QK, false, true) else BPC_BY_PAIRING(BPC_QK, false, false)
   }
+#undef BPC_QK
   return hipGetLastError();
 }
 
@@ -279,10 +304,10 @@ __global__ __launch_bounds__(kRopeThreads) void append_paged_kernel(AppendPagedA
   const int n = (a.Hkv + kPassRows - 1) / kPassRows;
   const int p0 = (int)(wave - tok * (uint32_t)parts) * per, p1 = min(2 * n, p0 + per);
   if (p0 < n)
-    turn_heads<PAIR, PER_HEAD>(a.kn + b * a.skn_b + t * a.skn_t, a.skn_h, a.K + page * a.sK_p + row * a.sK_n, a.sK_h,
+    turn_heads<PAIR, PER_HEAD, false>(a.kn + b * a.skn_b + t * a.skn_t, a.skn_h, a.K + page * a.sK_p + row * a.sK_n, a.sK_h,
                                a.wk, a.sw_h, a.eps, token_turn<PAIR>(cs, a.R), a.Hkv, p0, min(p1, n));
   if (p1 > n)
-    move_heads(a.vn + b * a.svn_b + t * a.svn_t, a.svn_h, a.V + page * a.sV_p + row * a.sV_n, a.sV_h, a.Hkv, max(p0 - n, 0),
+    move_heads<false>(a.vn + b * a.svn_b + t * a.svn_t, a.svn_h, a.V + page * a.sV_p + row * a.sV_n, a.sV_h, a.Hkv, max(p0 - n, 0),
                p1 - n, [](const uint4& x, int) { return x; });
 }
 
@@ -291,11 +316,13 @@ hipError_t launch_append_paged(const AppendPagedArgs& a) {
   const int64_t tokens = (int64_t)a.B * a.T;
   const int per = passes_per_wave(tokens, passes), parts = (passes + per - 1) / per;
   const unsigned grid = (unsigned)((tokens * parts + kRopeWaves - 1) / kRopeWaves);
+#define BPC_APPEND(PAIR, PER_HEAD) append_paged_kernel<PAIR, PER_HEAD><<<grid, kRopeThreads, 0, a.stream>>>(a, per, parts);
   if (a.wk && a.sw_h) {
-    BPC_BY_PAIRING(append_paged_kernel, true, a, per, parts)
+    BPC_BY_PAIRING(BPC_APPEND, true)
   } else {
-    BPC_BY_PAIRING(append_paged_kernel, false, a, per, parts)
+    BPC_BY_PAIRING(BPC_APPEND, false)
   }
+#undef BPC_APPEND
   return hipGetLastError();
 }
 #undef BPC_BY_PAIRING

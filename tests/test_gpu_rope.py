@@ -174,3 +174,17 @@ def test_append_into_a_contiguous_cache():
     bpc.append_kv_paged(k.to(DEV), v.to(DEV), dK, dV, torch.arange(B, dtype=torch.int32, device=DEV)[:, None], pos.to(DEV))
     store(K, V, torch.arange(B)[:, None], pos.tolist(), [T] * B, k, v)
     assert torch.equal(dK.cpu(), K) and torch.equal(dV.cpu(), V)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_more_rows_than_a_cache_holds(inter):
+    """Rows past 256 MB (written past the caches), against the same rows in parts."""
+    T, Hq, Hkv = 9001, 128, 5
+    g = torch.Generator(device=DEV).manual_seed(1)
+    q, k = (torch.randn(1, H, T, 128, generator=g, device=DEV).to(torch.bfloat16) for H in (Hq, Hkv))
+    table, w = rope_table(T, 128).to(DEV), (1 + rand(2, Hq, 128)).to(DEV)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)[None]
+    oq, ok = bpc.qk_norm_rope(q, k, pos, table, wq=w, eps=EPS, interleaved=inter)
+    for a in range(0, T, 2500):
+        pq, pk = bpc.qk_norm_rope(q[:, :, a:a + 2500], k[:, :, a:a + 2500], pos[:, a:a + 2500], table, wq=w, eps=EPS, interleaved=inter)
+        assert torch.equal(oq[:, :, a:a + 2500], pq) and torch.equal(ok[:, :, a:a + 2500], pk)
