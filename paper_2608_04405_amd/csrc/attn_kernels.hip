@@ -138,7 +138,6 @@ enum AttnKind { kPrefill, kTree, kPagedTree };
 
 template <int RB, int KW, int KT, AttnKind KIND, bool CAP, bool BIAS>
 struct AttnShape {
-  static constexpr int kThreads = RB * KW * 64;
   static constexpr int kTileBytes = KT * kRowBytes;    // K or V of a tile
   static constexpr int kLds = KW * 2 * 2 * kTileBytes;  // K and V, two buffers, per group
 };
