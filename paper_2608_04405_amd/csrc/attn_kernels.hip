@@ -48,6 +48,7 @@ constexpr int kSchedValu = 0x2, kSchedMfma = 0x8, kSchedLds = 0x100;
 constexpr int kRowBytes = kHeadDim * 2;
 constexpr int kBlockRows = 32;  // query rows of a wavefront
 constexpr int kMaxSplits = 64;  // pieces of the key axis
+constexpr float kFarScore = 0x1p24f;  // in log2: from here on fp32 holds no score to better than one
 
 __device__ __forceinline__ uint32_t swz(uint32_t row) {
   return ((row & 3u) << 2) | ((row >> 2) & 3u);
@@ -70,6 +71,26 @@ __device__ __forceinline__ float sum_halves(float x) {
 }
 __device__ __forceinline__ int wave_min(int x) { return wave_reduce_maxmin<false>(x); }
 __device__ __forceinline__ int wave_max(int x) { return wave_reduce_maxmin<true>(x); }
+
+// What a unit of the running maximum is in log2: capped scores are held in units
+// of log2, others in those of the products, which need no multiplication.
+template <bool CAP>
+__device__ __forceinline__ float log2_units(float sm_scale) {
+  return CAP ? 1.f : sm_scale * kLog2e;
+}
+
+// The reference point that a maximum m stands for, in log2: the rounded product
+// m * unit, so that an exponent is one multiply-add away from a score.  Far from
+// zero its rounding would take the largest score's exponential from one to any
+// power of two, out of range in the end: there it is the product itself, and the
+// difference of score and maximum comes first.
+__device__ __forceinline__ bool far_from_zero(float m, float unit) { return fabsf(m * unit) > kFarScore; }
+// From the reference point of b to that of a.
+template <bool CAP>
+__device__ __forceinline__ float reference_step(float a, float b, float unit) {
+  if (CAP) return a - b;
+  return far_from_zero(b, unit) ? (a - b) * unit : a * unit - b * unit;
+}
 
 // a value equal in all lanes, in scalar registers
 __device__ __forceinline__ uint64_t uniform64(uint64_t x) {
@@ -348,7 +369,8 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
     for (int d = 0; d < 4; ++d)
       vaddr[d] = ldsV + (4 * half + (i16 >> 2)) * kRowBytes + ((4 * d + chunk) ^ f) * 16 + (i16 & 1) * 8;
   }
-  const float c1 = a.sm_scale * kLog2e;
+  // Of the uncapped scores' units (the products') one is c1 in log2, 8 are c8.
+  const float c1 = log2_units<CAP>(a.sm_scale), c8 = 8.f / c1;
   const float cap2 = a.softcap * kLog2e, capk = CAP ? 2.f * kLog2e * a.sm_scale / a.softcap : 0.f;
 
   auto compute = [&](int it, int buf, uint32_t bad, bool cleared, uint64_t odd) {
@@ -426,13 +448,12 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
       for (int e = 0; e < 16; ++e) mt = fmaxf(mt, acc[k][e]);
     }
     mt = max_halves(mt);
-    if (!CAP) mt *= c1;
     // the reference point of the exponentials moves only when a score lies more
     // than 2^8 above it, so that the products are seldom rescaled; any point
     // gives the same quotient
-    if (__any(mt > mrun + 8.f)) {
+    if (__any(mt > mrun + (CAP ? 8.f : c8))) {
       const float mn = fmaxf(mrun, mt);
-      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrun - mn);
+      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(reference_step<CAP>(mrun, mn, c1));
       mrun = mn;
       lsum *= f;
 #pragma unroll
@@ -441,7 +462,17 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
         for (int e = 0; e < 16; ++e) o[d][e] *= f;
       }
     }
-    const float mu = mrun == -INFINITY ? 0.f : mrun;
+    const float ref = mrun == -INFINITY ? 0.f : mrun;
+    float mu = CAP ? ref : ref * c1;
+    if (!CAP && __any(far_from_zero(ref, c1))) {
+      const float first = far_from_zero(ref, c1) ? ref : 0.f;
+#pragma unroll
+      for (int k = 0; k < NB; ++k) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[k][e] -= first;
+      }
+      mu = far_from_zero(ref, c1) ? 0.f : mu;
+    }
     u32x4 pw[NB][2];
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
@@ -593,6 +624,7 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
     static_assert(KW * (16 * 2 * kBlockRows * (int)sizeof(float4) + kBlockRows * (int)sizeof(float2)) <= S::kLds, "fits the tiles' LDS");
     float4* so = reinterpret_cast<float4*>(smem);
     float2* sm = reinterpret_cast<float2*>(so + KW * 16 * 2 * kBlockRows);
+    const float unit = log2_units<CAP>(late_args()->sm_scale);
     __syncthreads();
 #pragma unroll
     for (int c = 0; c < 16; ++c) so[((grp * 16 + c) * 2 + half) * kBlockRows + col] = sums(c);
@@ -608,7 +640,7 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
     float tot = 0.f, f[KW];
 #pragma unroll
     for (int k = 0; k < KW; ++k) {
-      f[k] = st[k].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[k].x - mx);
+      f[k] = st[k].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(reference_step<CAP>(st[k].x, mx, unit));
       tot = fmaf(st[k].y, f[k], tot);
     }
 #pragma unroll
@@ -672,7 +704,8 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
   float mx = mine.y == 0.f ? -INFINITY : mine.x;
 #pragma unroll
   for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
-  const float w = mine.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(mine.x - mx);
+  const float unit = a.softcap > 0.f ? log2_units<true>(a.sm_scale) : log2_units<false>(a.sm_scale);
+  const float w = mine.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(reference_step<false>(mine.x, mx, unit));
   float tot = mine.y * w;
 #pragma unroll
   for (int o = 32; o; o >>= 1) tot += __shfl_xor(tot, o, 64);

@@ -310,7 +310,7 @@ struct AttnArgs {
   int splits;
   FastDiv div_G, div_Hkv, div_nrb, div_splits;
   int nrb, items;  // row blocks of a (b, h), workgroups
-  float2* part_ml;  // [B, Hkv, T G][splits] (max, sum), and o[128]
+  float2* part_ml;  // [B, Hkv, T G][splits] (max, in units of log2 or of the products, and sum), and o[128]
   float* part_o;
   hipStream_t stream;
 };
