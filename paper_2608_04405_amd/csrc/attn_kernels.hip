@@ -314,7 +314,9 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
   } else if (live) {
     lo = a.key_begin ? max(a.key_begin[b * a.s_begin + t], 0) : 0;
     hi = a.key_end ? min(a.key_end[b * a.s_end + t], a.N) : (int)min((int64_t)a.N, (int64_t)a.pos0 + t + 1);
-    place = a.pos0 + t;
+    // A bias counts from the nearest key that the row sees: what all of its keys
+    // have in common falls out of the softmax, and would cost fp32 what they differ in.
+    if (lo < hi) place = min(max(a.pos0 + t, lo), hi - 1);
   }
   // every row's keys cover [all_lo, all_hi); no row sees a key outside [any_lo, any_hi)
   int all_lo = 0, all_hi = len, any_lo = 0, any_hi = wg_row0 + rbw * kBlockRows < rows ? khi : 0;

@@ -1,16 +1,17 @@
 """prefill_attention and tree_attention where fp32 needs care: scores far from
-zero.
+zero, and distances that are large against what they differ in.
 
-The bounds are those of attn_plain: the inputs have one or two coordinates that
-count, so that products are exact.
+The bounds are those of attn_plain: where scores are large the inputs have one or
+two coordinates that count, so that products are exact, and a bias enters by its
+difference from the nearest visible key's, below 2^9 here.
 """
 
 import pytest
 import torch
 
 import paper_2608_04405_amd as bpc
-from attn_plain import attend, check_attend
-from test_gpu_attn import rand
+from attn_plain import attend, check_attend, ranges_visible
+from test_gpu_attn import rand, slopes_of
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -65,3 +66,30 @@ def test_scores_that_differ_little_far_from_zero(base):
     K[..., 0], K[..., 1] = base, torch.arange(N) % 7 if base < 2 ** 20 else 0
     visible = torch.ones(T, N, dtype=torch.bool).tril(N - T)[None]
     check_attend(bpc.prefill_attention(dev(q), dev(K), dev(V), 1.0), attend(q, K, V, visible, torch.zeros(1, T, N), 1.0))
+
+
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+@pytest.mark.parametrize("pos0", [300, 2 ** 20, 2 ** 24 - 7, 2 ** 30 - 40, 2 ** 30])
+def test_bias_of_positions_past_all_keys(pos0, cap):
+    """Every key lies far back: only the differences of the distances count."""
+    B, Hq, Hkv, T, N = 1, 4, 2, 40, 300
+    q, K, V, slopes = rand(1, B, Hq, T, 128), rand(2, B, Hkv, N, 128), rand(3, B, Hkv, N, 128), slopes_of(Hq)
+    visible = torch.ones(B, T, N, dtype=torch.bool)
+    dist = (pos0 + torch.arange(T)[:, None] - torch.arange(N))[None]
+    got = bpc.prefill_attention(dev(q), dev(K), dev(V), pos0=pos0, softcap=cap, slopes=dev(slopes))
+    check_attend(got, attend(q, K, V, visible, dist, 128 ** -0.5, cap, slopes))
+
+
+@pytest.mark.parametrize("N,pos0,begin,end", [(2 ** 20, 2 ** 20 - 9, 50, 170), (2 ** 20, 0, 2 ** 20 - 130, 2 ** 20 - 10), (2 ** 20, 2 ** 19, 2 ** 19 - 60, 2 ** 19 + 40)])
+def test_bias_of_a_far_window(N, pos0, begin, end):
+    """A row's window behind, ahead of and around its position, a million keys long the cache."""
+    Hq, T = 4, 9
+    first, last = torch.full((1, T), begin, dtype=torch.int32), (end + torch.arange(T, dtype=torch.int32))[None]
+    a, b = begin, end + T  # the keys that any row sees; the others hold anything
+    q, k, v, slopes = rand(1, 1, Hq, T, 128), rand(2, 1, 1, b - a, 128), rand(3, 1, 1, b - a, 128), slopes_of(Hq)
+    K, V = (torch.full((1, 1, N, 128), float("nan"), dtype=torch.bfloat16) for _ in range(2))
+    K[:, :, a:b], V[:, :, a:b] = k, v
+    dist = (pos0 + torch.arange(T)[:, None] - torch.arange(a, b)).abs()[None]
+    want = attend(q, k, v, ranges_visible(first - a, last - a, b - a), dist, 128 ** -0.5, 0.0, slopes)
+    got = bpc.prefill_attention(dev(q), dev(K), dev(V), pos0=pos0, slopes=dev(slopes), key_begin=dev(first), key_end=dev(last))
+    check_attend(got, want)
