@@ -702,7 +702,9 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
   const float* po = a.part_o + (int64_t)r * a.splits * kHeadDim + d;
   float2 mine = make_float2(-INFINITY, 0.f);
   if (lane < a.splits) mine = ml[lane];
-  // a split that saw no key of this row has the sum 0, and its o was not written
+  // a split that saw no key of this row has the sum 0, and its o was not written;
+  // one whose weight is 0 beside the others' counts, for the NaN it may hold
+  const uint64_t seen = __ballot(mine.y != 0.f);
   float mx = mine.y == 0.f ? -INFINITY : mine.x;
 #pragma unroll
   for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
@@ -718,9 +720,9 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
     for (int i = 0; i < 4; ++i)
       v[i] = *reinterpret_cast<const float4*>(po + (int64_t)min(s0 + 2 * i + half, a.splits - 1) * kHeadDim);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i) {  // (lanes from `splits` on have seen nothing)
       const float f = __shfl(w, (s0 + 2 * i + half) & 63, 64);
-      const bool on = f != 0.f && s0 + 2 * i + half < a.splits;
+      const bool on = (seen >> ((s0 + 2 * i + half) & 63)) & 1;
       x.x = on ? fmaf(v[i].x, f, x.x) : x.x, x.y = on ? fmaf(v[i].y, f, x.y) : x.y;
       x.z = on ? fmaf(v[i].z, f, x.z) : x.z, x.w = on ? fmaf(v[i].w, f, x.w) : x.w;
     }

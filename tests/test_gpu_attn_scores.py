@@ -1,5 +1,6 @@
 """prefill_attention and tree_attention where fp32 needs care: scores far from
-zero, and distances that are large against what they differ in.
+zero, distances that are large against what they differ in, and weights that
+leave fp32's range.
 
 The bounds are those of attn_plain: where scores are large the inputs have one or
 two coordinates that count, so that products are exact, and a bias enters by its
@@ -10,7 +11,7 @@ import pytest
 import torch
 
 import paper_2608_04405_amd as bpc
-from attn_plain import attend, check_attend, ranges_visible
+from attn_plain import attend, check_attend, ranges_visible, tree_view
 from test_gpu_attn import rand, slopes_of
 
 pytestmark = pytest.mark.gpu
@@ -92,4 +93,23 @@ def test_bias_of_a_far_window(N, pos0, begin, end):
     dist = (pos0 + torch.arange(T)[:, None] - torch.arange(a, b)).abs()[None]
     want = attend(q, k, v, ranges_visible(first - a, last - a, b - a), dist, 128 ** -0.5, 0.0, slopes)
     got = bpc.prefill_attention(dev(q), dev(K), dev(V), pos0=pos0, slopes=dev(slopes), key_begin=dev(first), key_end=dev(last))
+    check_attend(got, want)
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_a_visible_nan_counts_in_a_piece_of_no_weight(tree):
+    """A value that is not a number, at a key whose weight fp32 rounds to zero beside those of the axis' other pieces."""
+    T, N = 2, 9000
+    q, K, V = line([1.0] * T, 1, 2), line([0.0] * N, 1, 1), rand(3, 1, 1, N, 128)
+    K[0, 0, N - 5, 0], V[0, 0, 5, 7] = 200.0, float("nan")
+    if tree:
+        assert bpc.tree_workspace_bytes(1, 2, 1, T, N) > 0  # the axis is in pieces
+        visible, dist = tree_view([N - T], None, T, N)
+        got = bpc.tree_attention(dev(q), dev(K), dev(V), dev(torch.tensor([N - T], dtype=torch.int32)), sm_scale=1.0)
+    else:
+        assert bpc.prefill_workspace_bytes(1, 2, 1, T, N) > 0
+        visible, dist = ranges_visible(torch.zeros(1, T), torch.full((1, T), N), N), torch.zeros(1, T, N)
+        got = bpc.prefill_attention(dev(q), dev(K), dev(V), 1.0, key_end=dev(torch.full((1, T), N, dtype=torch.int32)))
+    want = attend(q, K, V, visible, dist, 1.0)
+    assert bool(want[0][..., 7].isnan().all())
     check_attend(got, want)
