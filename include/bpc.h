@@ -510,6 +510,7 @@ int bpc_decode_attention_noalloc(const uint16_t* q,
  *            most 128
  * pos        [B, T] int32, stride sp_b (0 = shared).  The rows of a token whose
  *            position is not in [0, table_rows) are not written.
+ * B, T       at most 2^26 - 4 tokens in a call (a launch's 2^32 threads)
  * No workspace; one kernel launch.
  */
 int bpc_qk_norm_rope(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
@@ -546,7 +547,7 @@ int bpc_qk_norm_rope(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t
  * count      [B] int32: new tokens of each sequence, or NULL: T of each
  * rope_pos   [B, T] int32, stride sr_b: rotation position of each token (the
  *            depth of a drafted token, say), or NULL: its slot
- * wk, sw_k, eps, cos_sin, table_rows, R, interleaved  as in bpc_qk_norm_rope
+ * wk, sw_k, eps, cos_sin, table_rows, R, interleaved, B, T  as in bpc_qk_norm_rope
  * No workspace; one kernel launch.
  */
 int bpc_append_kv_paged(const uint16_t* k_new, int64_t sKn_b, int64_t sKn_h, int64_t sKn_t,
@@ -590,7 +591,9 @@ int bpc_append_kv_paged(const uint16_t* k_new, int64_t sKn_b, int64_t sKn_h, int
  *            sizes), 256-byte aligned; its contents on entry do not matter.
  * fp32 scores, statistics and sums; the probabilities enter the second product
  * as bf16, out is rounded once.  One launch, or two where few query rows face
- * many keys (the key axis is then split and joined).
+ * many keys (the key axis is then split and joined).  More rows than a launch has
+ * threads for (2^32: no fewer than 2^26 rows, B Hq T) are refused with
+ * BPC_EUNSUPPORTED.
  */
 size_t bpc_prefill_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D);
 int bpc_prefill_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,

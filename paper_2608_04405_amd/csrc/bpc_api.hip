@@ -606,11 +606,15 @@ static int check_int32(const char* name, const int32_t* p, int64_t stride) {
   return BPC_OK;
 }
 
-// sequences, heads and tokens of a call whose wavefronts a 32-bit grid counts
+// a launch has fewer than 2^32 threads
+static bool launchable(int64_t blocks, int threads) { return blocks * threads <= (int64_t)UINT32_MAX; }
+
+// sequences, heads and tokens of a call that gives a wavefront at least a token
 static int check_tokens(int B, int H, int T) {
   if (B < 1 || H < 1 || T < 1) return fail(BPC_EINVAL, "B=%d, heads=%d, T=%d must all be >= 1", B, H, T);
   if (H > (1 << 16)) return fail(BPC_EUNSUPPORTED, "%d heads: at most 65536", H);
-  if ((int64_t)B * T > (int64_t)(1 << 30)) return fail(BPC_EUNSUPPORTED, "B T = %lld tokens: at most 2^30", (long long)B * T);
+  if (!launchable(((int64_t)B * T + 3) / 4, 256))
+    return fail(BPC_EUNSUPPORTED, "B T = %lld tokens: at most 2^26 - 4", (long long)B * T);
   return BPC_OK;
 }
 
@@ -716,8 +720,10 @@ static int check_attn(const AttnArgs& a, int Hq, int D, const AttnPlan& plan, co
   if (a.softcap != 0.0f && (a.softcap < 0x1p-20f || a.softcap > 1024.0f))
     return fail(BPC_EUNSUPPORTED, "softcap=%g: 2^-20 to 1024", a.softcap);
   if (a.slopes && !aligned4(a.slopes)) return fail(BPC_EALIGN, "slopes must be 4-byte aligned");
-  const int64_t blocks = ((int64_t)a.T * a.G + plan.rb * 32 - 1) / (plan.rb * 32) * a.B * a.Hkv * plan.splits;
-  if (blocks > (int64_t)(1 << 30) || (plan.splits > 1 && (int64_t)a.B * a.Hkv * a.T * a.G > (int64_t)(1 << 30)))
+  // row blocks and pieces, a multiple of eight of them (one XCD's each), and the join's four rows a workgroup
+  const int64_t rows = (int64_t)a.T * a.G, pairs = (int64_t)a.B * a.Hkv;
+  const int64_t blocks = (rows + plan.rb * 32 - 1) / (plan.rb * 32) * ((pairs * plan.splits + 7) / 8 * 8);
+  if (!launchable(blocks, plan.rb == 8 ? 512 : 256) || (plan.splits > 1 && !launchable((pairs * rows + 3) / 4, 256)))
     return fail(BPC_EUNSUPPORTED, "%lld workgroups: too many rows in one call", (long long)blocks);
   if (plan.total) {
     if (!workspace || workspace_bytes < plan.total)

@@ -216,7 +216,6 @@ __device__ __forceinline__ void turn_heads(const uint16_t* src, int64_t ss, uint
 // ---------------------------------------------------------------------------
 template <Pairing PAIR, bool PER_HEAD, bool STREAM>
 __global__ __launch_bounds__(kRopeThreads) void qk_norm_rope_kernel(RopeArgs a, int per, int parts) {
-  // (fewer than 2^32 wavefronts: 2^30 tokens, or few of them in parts)
   const uint32_t wave = blockIdx.x * kRopeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t tok = wave / (uint32_t)parts;
   if (tok >= (uint32_t)a.B * (uint32_t)a.T) return;
@@ -284,7 +283,6 @@ hipError_t launch_qk_norm_rope(const RopeArgs& a) {
 // ---------------------------------------------------------------------------
 template <Pairing PAIR, bool PER_HEAD>
 __global__ __launch_bounds__(kRopeThreads) void append_paged_kernel(AppendPagedArgs a, int per, int parts) {
-  // (fewer than 2^32 wavefronts: 2^30 tokens, or few of them in parts)
   const uint32_t wave = blockIdx.x * kRopeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t tok = wave / (uint32_t)parts;
   if (tok >= (uint32_t)a.B * (uint32_t)a.T) return;
