@@ -499,7 +499,10 @@ int bpc_decode_attention_noalloc(const uint16_t* q,
  * q          [B, Hq, T, D] bf16, strides (sq_b, sq_h, sq_t); Hq = 0 (and NULL
  *            pointers): no queries
  * q_out      the same shape, strides (sqo_*): either q itself with q's
- *            strides, or memory that overlaps none of the inputs
+ *            strides, or memory that overlaps none of the inputs.  Its rows lie
+ *            apart (here and below where rows are written): no stride is smaller
+ *            than what the dimensions of smaller strides span, as in any slice or
+ *            transposition of a dense tensor, else BPC_EINVAL.
  * wq         [Hq, D] bf16 norm weights, head stride sw_q (0 = one row of
  *            weights for all heads), or NULL: no norm
  * k, k_out, wk, Hkv  likewise (k_out may be the cache); Hq + Hkv >= 1

@@ -705,8 +705,13 @@ def _written(t: torch.Tensor, name: str, B: int, H: int, T: int):
     a, b, c, x, y, z = _rows(t, name)
     if a != B or b != H or c != T:
         _extent(t, name, (B, H, T, 128))
-    if (x < 128 and B > 1) or (y < 128 and H > 1) or (z < 128 and T > 1):
-        raise ValueError(f"{name}: its rows must not overlap (strides {tuple(t.stride())})")
+    if not t.is_contiguous():
+        span = 128  # a stride is no smaller than what those below it span
+        for stride, extent in sorted(((x, B), (y, H), (z, T))):
+            if extent > 1:
+                if stride < span:
+                    raise ValueError(f"{name}: its rows must not overlap (strides {tuple(t.stride())})")
+                span += stride * (extent - 1)
     return x, y, z
 
 

@@ -7,6 +7,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 
 #include "bpc_internal.h"
@@ -570,12 +571,30 @@ static int check_rows(const char* name, const void* p, int64_t sb, int64_t sh, i
   return BPC_OK;
 }
 
-// A tensor that is written: no two of its rows in the same place
+// A tensor that is written
 static int check_written(const char* name, const void* p, int64_t sb, int64_t sh, int64_t st, int B, int H, int T) {
   int rc = check_rows(name, p, sb, sh, st);
   if (rc) return rc;
   if ((B > 1 && sb < kHeadDim) || (H > 1 && sh < kHeadDim) || (T > 1 && st < kHeadDim))
     return fail(BPC_EINVAL, "%s: strides of written rows must be at least 128", name);
+  return BPC_OK;
+}
+
+// And no two of its rows in the same place: a stride is no smaller than what the
+// dimensions of smaller strides span, as in every slice or transposition of a
+// dense tensor.
+static int check_apart(const char* name, int64_t sb, int64_t sh, int64_t st, int B, int H, int T) {
+  struct {
+    int64_t stride, extent;
+  } d[3] = {{sb, B}, {sh, H}, {st, T}};
+  std::sort(d, d + 3, [](const auto& x, const auto& y) { return x.stride < y.stride; });
+  int64_t span = kHeadDim;
+  for (const auto& [stride, extent] : d) {
+    if (extent < 2) continue;
+    if (stride < span || stride > INT64_MAX / 4 / extent)
+      return fail(BPC_EINVAL, "%s: written rows must not overlap, strides (%lld, %lld, %lld)", name, (long long)sb, (long long)sh, (long long)st);
+    span += stride * (extent - 1);
+  }
   return BPC_OK;
 }
 
@@ -651,6 +670,8 @@ int bpc_qk_norm_rope(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t
     if ((st = check_norm("wk", wk, sw_k))) return st;
     a.k = RopeTensor{k, sk_b, sk_h, sk_t, k_out, sko_b, sko_h, sko_t, wk, sw_k, Hkv};
   }
+  if (Hq && (st = check_apart("q_out", sqo_b, sqo_h, sqo_t, B, Hq, T))) return st;
+  if (Hkv && (st = check_apart("k_out", sko_b, sko_h, sko_t, B, Hkv, T))) return st;
   a.pos = pos, a.sp_b = sp_b, a.cos_sin = cos_sin, a.table_rows = table_rows, a.R = R, a.inter = interleaved != 0;
   a.eps = eps, a.B = B, a.T = T, a.stream = static_cast<hipStream_t>(stream);
   hipError_t e = launch_qk_norm_rope(a);
@@ -683,6 +704,8 @@ int bpc_append_kv_paged(const uint16_t* k_new, int64_t sKn_b, int64_t sKn_h, int
   if ((st = check_eps(eps))) return st;
   if ((st = check_rotation(cos_sin, table_rows, R))) return st;
   if (rope_pos && (st = check_int32("rope_pos", rope_pos, sr_b))) return st;
+  if ((st = check_apart("K", sK_p, sK_h, sK_n, num_pages, Hkv, page_size))) return st;
+  if ((st = check_apart("V", sV_p, sV_h, sV_n, num_pages, Hkv, page_size))) return st;
   AppendPagedArgs a{};
   a.kn = k_new, a.skn_b = sKn_b, a.skn_h = sKn_h, a.skn_t = sKn_t;
   a.vn = v_new, a.svn_b = sVn_b, a.svn_h = sVn_h, a.svn_t = sVn_t;
@@ -779,6 +802,7 @@ int bpc_prefill_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t
   if ((st = check_attn(a, Hq, D, plan, workspace, workspace_bytes))) return st;
   if (key_begin && (st = check_int32("key_begin", key_begin, sb_b))) return st;
   if (key_end && (st = check_int32("key_end", key_end, se_b))) return st;
+  if ((st = check_apart("out", so_b, so_h, so_t, B, Hq, T))) return st;
   attn_workspace(a, plan, workspace);
   hipError_t e = launch_attn(a, plan);
   if (e != hipSuccess) return hip_fail(e, "bpc_prefill_attention launch");
@@ -823,6 +847,7 @@ int bpc_tree_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq
     if (num_pages < 1) return fail(BPC_EINVAL, "num_pages=%d must be >= 1", num_pages);
     a.table = block_table, a.st_b = st_b, a.num_pages = num_pages, a.page_shift = shift;
   }
+  if ((st = check_apart("out", so_b, so_h, so_t, B, Hq, T))) return st;
   attn_workspace(a, plan, workspace);
   hipError_t e = launch_attn(a, plan);
   if (e != hipSuccess) return hip_fail(e, "bpc_tree_attention launch");
