@@ -499,7 +499,9 @@ int bpc_decode_attention_noalloc(const uint16_t* q,
  * q          [B, Hq, T, D] bf16, strides (sq_b, sq_h, sq_t); Hq = 0 (and NULL
  *            pointers): no queries
  * q_out      the same shape, strides (sqo_*): either q itself with q's
- *            strides, or memory that overlaps none of the inputs.  Its rows lie
+ *            strides, or memory that overlaps neither q, k nor k_out (refused with
+ *            BPC_EINVAL where the two have the same strides; rows of different
+ *            strides that interleave are the caller's to keep apart).  Its rows lie
  *            apart (here and below where rows are written): no stride is smaller
  *            than what the dimensions of smaller strides span, as in any slice or
  *            transposition of a dense tensor, else BPC_EINVAL.

@@ -798,7 +798,8 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: Opti
     coordinates (R a multiple of 16, up to 128) in pairs (i, i + R/2), or
     (2i, 2i + 1) with `interleaved`; None: no rotation.  pos [B, T] int32; the
     rows of a token whose position is not in the table are not written.
-    q_out, k_out may be q and k themselves, or the rows of a cache."""
+    q_out, k_out may be q and k themselves, or the rows of a cache, but overlap
+    neither input otherwise, nor one another."""
     if q is None and k is None:
         raise ValueError("q and k cannot both be None")
     Hq = Hkv = 0

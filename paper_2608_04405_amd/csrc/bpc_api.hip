@@ -598,6 +598,52 @@ static int check_apart(const char* name, int64_t sb, int64_t sh, int64_t st, int
   return BPC_OK;
 }
 
+// Whether rows that are written share memory with others, where that can be told:
+// from the ranges of the addresses, or, where the two have the same strides (views
+// of one buffer), by their distance along each dimension.
+struct RowSet {
+  const char* name;
+  const uint16_t* p;
+  int64_t stride[3];
+  int extent[3];
+};
+struct Distances {  // rows of one set may lie first .. last strides before those of the other
+  int64_t stride, first, last;
+  int64_t reach() const { return stride * std::max(last, -first); }
+};
+
+// Whether rows `away` elements apart meet by a step along each of the dimensions,
+// of which a later one reaches no further than an earlier one's stride.
+static bool rows_meet(int64_t away, const Distances* d, int dims) {
+  if (!dims) return away > -kHeadDim && away < kHeadDim;
+  int64_t rest = kHeadDim;
+  for (int i = 1; i < dims; ++i) rest += d[i].reach();
+  const int64_t x0 = std::max(d->first, (away - rest) / d->stride), x1 = std::min(d->last, (away + rest) / d->stride);
+  for (int64_t x = x0; x <= x1; ++x)
+    if (rows_meet(away - x * d->stride, d + 1, dims - 1)) return true;
+  return false;
+}
+
+static int check_separate(const RowSet& out, const RowSet& in) {
+  if (!out.p || !in.p) return BPC_OK;
+  int64_t out_span = kHeadDim, in_span = kHeadDim;
+  Distances d[3];
+  int dims = 0;
+  bool alike = true;
+  for (int i = 0; i < 3; ++i) {
+    out_span += out.stride[i] * (out.extent[i] - 1), in_span += in.stride[i] * (in.extent[i] - 1);
+    const int64_t stride = out.extent[i] > 1 ? out.stride[i] : in.stride[i];
+    if (out.extent[i] > 1 && in.extent[i] > 1 && in.stride[i] != stride) alike = false;
+    if (stride && (out.extent[i] > 1 || in.extent[i] > 1)) d[dims++] = {stride, 1 - (int64_t)in.extent[i], (int64_t)out.extent[i] - 1};
+  }
+  const int64_t away = (int64_t)(reinterpret_cast<uintptr_t>(in.p) - reinterpret_cast<uintptr_t>(out.p)) / 2;
+  if (away >= out_span || -away >= in_span) return BPC_OK;
+  std::sort(d, d + dims, [](const Distances& x, const Distances& y) { return x.stride > y.stride; });
+  int64_t span = kHeadDim;
+  for (int i = dims; i--;) alike = alike && d[i].stride >= span, span += d[i].reach();
+  return alike && rows_meet(away, d, dims) ? fail(BPC_EINVAL, "%s overlaps %s", out.name, in.name) : BPC_OK;
+}
+
 static int check_rotation(const float* cos_sin, int table_rows, int R) {
   if (R < 0 || R > kHeadDim || R % 16) return fail(BPC_EINVAL, "R=%d must be a multiple of 16, 0 to 128", R);
   if (R == 0) return BPC_OK;
@@ -672,6 +718,15 @@ int bpc_qk_norm_rope(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t
   }
   if (Hq && (st = check_apart("q_out", sqo_b, sqo_h, sqo_t, B, Hq, T))) return st;
   if (Hkv && (st = check_apart("k_out", sko_b, sko_h, sko_t, B, Hkv, T))) return st;
+  const RowSet in[2] = {{"q", a.q.in, {sq_b, sq_h, sq_t}, {B, Hq, T}}, {"k", a.k.in, {sk_b, sk_h, sk_t}, {B, Hkv, T}}};
+  const RowSet out[2] = {{"q_out", a.q.out, {sqo_b, sqo_h, sqo_t}, {B, Hq, T}}, {"k_out", a.k.out, {sko_b, sko_h, sko_t}, {B, Hkv, T}}};
+  for (int i = 0; i < 2; ++i) {
+    bool in_place = out[i].p == in[i].p;
+    for (int x = 0; x < 3; ++x) in_place = in_place && (out[i].extent[x] == 1 || out[i].stride[x] == in[i].stride[x]);
+    if (!in_place && (st = check_separate(out[i], in[i]))) return st;
+    if ((st = check_separate(out[i], in[1 - i]))) return st;
+  }
+  if ((st = check_separate(out[0], out[1]))) return st;
   a.pos = pos, a.sp_b = sp_b, a.cos_sin = cos_sin, a.table_rows = table_rows, a.R = R, a.inter = interleaved != 0;
   a.eps = eps, a.B = B, a.T = T, a.stream = static_cast<hipStream_t>(stream);
   hipError_t e = launch_qk_norm_rope(a);

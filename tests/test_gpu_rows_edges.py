@@ -1,0 +1,36 @@
+"""qk_norm_rope: results in the buffer of the inputs."""
+
+import pytest
+import torch
+
+import paper_2608_04405_amd as bpc
+from attn_plain import rope_table
+from test_gpu_attn import rand
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def dev(x):
+    return None if x is None else x.to(DEV)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_fused_projection_in_place(inter):
+    """Queries and keys of one buffer, each in its own place, or moved to that of the values and behind it."""
+    B, T, Hq, Hkv = 2, 9, 8, 2
+    x = rand(5, B, T, Hq + 2 * Hkv, 128)
+    table, pos, w = rope_table(T, 128), torch.arange(T, dtype=torch.int32).expand(B, T), 1 + rand(6, 128)
+    y = dev(x)
+    q, k, v = y[:, :, :Hq].transpose(1, 2), y[:, :, Hq:Hq + Hkv].transpose(1, 2), y[:, :, Hq + Hkv:].transpose(1, 2)
+    want_q, want_k = bpc.qk_norm_rope(q, k, dev(pos), dev(table), wq=dev(w), wk=dev(w), interleaved=inter)
+    moved = v.clone()
+    bpc.qk_norm_rope(q, k, dev(pos), dev(table), wq=dev(w), wk=dev(w), interleaved=inter, q_out=q, k_out=v)  # k_out: where v was
+    assert torch.equal(q, want_q) and torch.equal(v, want_k)
+    y = dev(x)
+    q, k, v = y[:, :, :Hq].transpose(1, 2), y[:, :, Hq:Hq + Hkv].transpose(1, 2), y[:, :, Hq + Hkv:].transpose(1, 2)
+    bpc.qk_norm_rope(q, k, dev(pos), dev(table), wq=dev(w), wk=dev(w), interleaved=inter, q_out=q, k_out=k)
+    assert torch.equal(q, want_q) and torch.equal(k, want_k) and torch.equal(v, moved)
+    with pytest.raises(bpc.BPCError, match="overlaps"):
+        bpc.qk_norm_rope(q, k, dev(pos), dev(table), q_out=q, k_out=q[:, :Hkv])
+    assert torch.equal(q, want_q)

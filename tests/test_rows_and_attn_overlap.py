@@ -50,3 +50,30 @@ def test_append_refuses_pools_whose_rows_meet(lib, kw):
     good = dict(K_b=4096, K_h=2048, V_b=4096, V_h=2048)
     assert call(lib, "bpc_append_kv_paged", APPEND, {**good, **kw}) == EINVAL
     assert b"overlap" in lib.bpc_last_error()
+
+
+# q and k of a fused projection [2, 5, 12, 128] (8 heads of q, 2 of k, 2 of v), in elements from its start
+FUSED = dict(q_b=7680, q_h=128, q_t=1536, qo_b=7680, qo_h=128, qo_t=1536, k_b=7680, k_h=128, k_t=1536, ko_b=7680, ko_h=128, ko_t=1536)
+FAR = 1 << 24
+
+
+def fused(q, qo, k, ko, **kw):
+    return {**FUSED, **{n: FAKE + 2 * at for n, at in (("q", q), ("qo", qo), ("k", k), ("ko", ko))}, **kw}
+
+
+@pytest.mark.parametrize("kw,word", [
+    (fused(0, 128, 1024, FAR), b"q_out overlaps q"),  # a head on
+    (fused(0, 1536, 1024, FAR), b"q_out overlaps q"),  # a token on
+    (fused(0, 7680 * 2 - 512, 1024, FAR), b"q_out overlaps k"),  # from the last token's k on
+    (fused(0, 8, 1024, FAR), b"q_out overlaps q"),
+    (fused(0, 0, 1024, 1024 - 256), b"k_out overlaps q"),  # the last heads of q
+    (fused(0, 128, 1024 + FAR, 2 * FAR), b"q_out overlaps q"),
+    (fused(0, FAR, 1024, FAR + 1024 - 128), b"q_out overlaps k_out"),
+    (fused(0, FAR, 1024, 1024 + 128), b"k_out overlaps k"),
+    (fused(0, 1024, FAR, 2 * FAR), b"q_out overlaps q"),  # eight heads from the k of a token on reach its next token's q
+    (fused(0, FAR, 2 * FAR, 0), b"k_out overlaps q"),
+])
+def test_results_on_their_inputs(lib, kw, word):
+    """Neither in place nor apart: another wavefront may not have read what a row replaces."""
+    assert call(lib, "bpc_qk_norm_rope", ROPE, kw) == EINVAL
+    assert word in lib.bpc_last_error()
