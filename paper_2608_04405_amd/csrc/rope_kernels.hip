@@ -58,7 +58,8 @@ __device__ __forceinline__ void unpack8(const uint4& x, float v[8]) {
 }
 
 // a lane's place in the rotation of its token: cosines and signed sines of its
-// eight coordinates (1 and 0 outside), and its partner's lane
+// eight coordinates (1 and -0 outside, where x + 0 * -0 is x for every x), and its
+// partner's lane
 struct Turn {
   float c[8], s[8];
   int partner;
@@ -71,7 +72,7 @@ __device__ __forceinline__ Turn token_turn(const float* __restrict__ cs, int R) 
   const int lane = threadIdx.x & 63, j = lane % kRowLanes, half = R / 2;
   r.partner = lane, r.keep = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r.c[e] = 1.f, r.s[e] = 0.f;
+  for (int e = 0; e < 8; ++e) r.c[e] = 1.f, r.s[e] = -0.f;
   if (PAIR == kPairNone || 8 * j >= R) return r;
   r.keep = 0xFFFFFFFFu;
   if (PAIR == kPairAdjacent) {
@@ -115,7 +116,7 @@ __device__ __forceinline__ void row_factors(const Turn& t, const uint16_t* w, fl
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     C[e] *= wv[e];
-    if (PAIR != kPairNone) S[e] *= wu[e];
+    if (PAIR == kPairEight || (PAIR != kPairNone && t.keep)) S[e] *= wu[e];
   }
 }
 

@@ -1,4 +1,5 @@
-"""qk_norm_rope: results in the buffer of the inputs."""
+"""qk_norm_rope: results in the buffer of the inputs, coordinates outside the
+rotation."""
 
 import pytest
 import torch
@@ -34,3 +35,23 @@ def test_fused_projection_in_place(inter):
     with pytest.raises(bpc.BPCError, match="overlaps"):
         bpc.qk_norm_rope(q, k, dev(pos), dev(table), q_out=q, k_out=q[:, :Hkv])
     assert torch.equal(q, want_q)
+
+
+@pytest.mark.parametrize("R,inter", [(16, False), (64, False), (96, False), (64, True), (112, True)])
+def test_coordinates_outside_the_rotation_are_their_own(R, inter):
+    """No partner reaches them, by its value or its weight, and without weights they keep their bits."""
+    B, H, T = 2, 5, 7
+    q = rand(1, B, H, T, 128)
+    q[..., ::9] = -0.0
+    table, pos = rope_table(T, R), torch.arange(T, dtype=torch.int32).expand(B, T)
+    plain = bpc.qk_norm_rope(dev(q), None, dev(pos), dev(table), interleaved=inter)[0].cpu()
+    assert torch.equal(plain[..., R:].view(torch.int16), q[..., R:].contiguous().view(torch.int16))
+    w = torch.ones(128, dtype=torch.bfloat16)
+    w[R + 1], w[R + 6] = float("inf"), float("nan")
+    q[..., R + 1] = 2.0
+    for weights in (w, w.expand(H, 128).contiguous()):
+        got = bpc.qk_norm_rope(dev(q), None, dev(pos), dev(table), wq=dev(weights), interleaved=inter)[0].cpu()
+        odd = torch.zeros(128, dtype=torch.bool)
+        odd[R + 1], odd[R + 6] = True, True
+        assert bool((got[..., R + 1] == float("inf")).all()) and bool(got[..., R + 6].isnan().all())
+        assert bool(got[..., ~odd].isfinite().all())
