@@ -700,6 +700,12 @@ def _indices(t: Optional[torch.Tensor], name: str, shape, dtype=torch.int32) -> 
     return t.stride(0) if len(shape) == 2 and shape[0] > 1 else 0
 
 
+def _cache(t: torch.Tensor, name: str):
+    """As _rows, with the strides that the C entries take a cache's to be."""
+    a, b, c, x, y, z = _rows(t, name)
+    return a, b, c, (x, y, z if c > 1 else 128)
+
+
 def _written(t: torch.Tensor, name: str, B: int, H: int, T: int):
     """The strides of a [B, H, T, 128] tensor whose rows a call writes."""
     a, b, c, x, y, z = _rows(t, name)
@@ -900,10 +906,10 @@ _SM_SCALE = 1.0 / math.sqrt(128)
 
 def _attn_inputs(q, K, V, slopes, out, workspace):
     """Checks shared by prefill_attention and tree_attention; returns the sizes
-    and strides of q and out, and the sizes of K and V."""
+    and strides of q and out, and those of K and V."""
     B, Hq, T, *sq = _rows(q, "q")
-    Kb, Hkv, Kn, *_ = _rows(K, "K")
-    Vb, Vh, Vn, *_ = _rows(V, "V")
+    Kb, Hkv, Kn, sK = _cache(K, "K")
+    Vb, Vh, Vn, sV = _cache(V, "V")
     if Hq % Hkv:
         raise ValueError(f"Hq={Hq} must be a multiple of Hkv={Hkv}")
     if slopes is not None:
@@ -912,7 +918,7 @@ def _attn_inputs(q, K, V, slopes, out, workspace):
     so = _dense(B, Hq, T) if out is None else _written(out, "out", B, Hq, T)
     if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous uint8 tensor")
-    return B, Hq, Hkv, T, sq, so, Kb, Kn, Vb, Vh, Vn
+    return B, Hq, Hkv, T, sq, so, Kb, Kn, sK, Vb, Vh, Vn, sV
 
 
 def _cache_rows(K, V, B, Hkv, N) -> None:
@@ -935,7 +941,7 @@ def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scal
     prefix mask.  Scores are capped to softcap * tanh(s / softcap) when softcap
     > 0, then lowered by slopes[head] * distance.  A token that sees nothing
     gets zeros."""
-    B, Hq, Hkv, T, sq, so, Kb, Kn, Vb, Vh, Vn = _attn_inputs(q, K, V, slopes, out, workspace)
+    B, Hq, Hkv, T, sq, so, Kb, Kn, sK, Vb, Vh, Vn, sV = _attn_inputs(q, K, V, slopes, out, workspace)
     N = Kn if N is None else N
     if N < 1:
         raise ValueError(f"N={N} must be >= 1")
@@ -962,7 +968,7 @@ def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scal
         if need:
             workspace = q.new_empty(need, dtype=torch.uint8)
     status = _lib.bpc_prefill_attention(
-        q.data_ptr(), *sq, K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], B, Hq, Hkv, T, N, pos0, 128,
+        q.data_ptr(), *sq, K.data_ptr(), *sK, V.data_ptr(), *sV, B, Hq, Hkv, T, N, pos0, 128,
         _SM_SCALE if sm_scale is None else sm_scale, softcap, _ptr(slopes), _ptr(key_begin), sb, _ptr(key_end), se,
         out.data_ptr(), *so, _ptr(workspace), 0 if workspace is None else workspace.numel(), _current_stream(dev))
     if status:
@@ -988,7 +994,7 @@ def tree_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torc
     being lens[b] plus its depth.  A sequence whose lens[b] is not in [0, N - T]
     is skipped: its rows of `out` stay as they are (undefined where `out` is
     allocated here)."""
-    B, Hq, Hkv, T, sq, so, Kb, Kn, Vb, Vh, Vn = _attn_inputs(q, K, V, slopes, out, workspace)
+    B, Hq, Hkv, T, sq, so, Kb, Kn, sK, Vb, Vh, Vn, sV = _attn_inputs(q, K, V, slopes, out, workspace)
     pages = page = st = 0
     if block_table is None:
         N = Kn if N is None else N
@@ -1021,7 +1027,7 @@ def tree_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torc
         if need:
             workspace = q.new_empty(need, dtype=torch.uint8)
     status = _lib.bpc_tree_attention(
-        q.data_ptr(), *sq, K.data_ptr(), *K.stride()[:3], V.data_ptr(), *V.stride()[:3], _ptr(block_table), st, pages,
+        q.data_ptr(), *sq, K.data_ptr(), *sK, V.data_ptr(), *sV, _ptr(block_table), st, pages,
         page, lens.data_ptr(), _ptr(tree), sm, B, Hq, Hkv, T, N, 128, _SM_SCALE if sm_scale is None else sm_scale,
         softcap, _ptr(slopes), out.data_ptr(), *so, _ptr(workspace), 0 if workspace is None else workspace.numel(),
         _current_stream(dev))

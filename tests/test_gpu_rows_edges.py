@@ -1,5 +1,5 @@
 """qk_norm_rope: results in the buffer of the inputs, coordinates outside the
-rotation."""
+rotation.  prefill_attention and tree_attention: strides that no element uses."""
 
 import pytest
 import torch
@@ -55,3 +55,15 @@ def test_coordinates_outside_the_rotation_are_their_own(R, inter):
         odd[R + 1], odd[R + 6] = True, True
         assert bool((got[..., R + 1] == float("inf")).all()) and bool(got[..., R + 6].isnan().all())
         assert bool(got[..., ~odd].isfinite().all())
+
+
+def test_strides_of_single_extents_do_not_matter():
+    """A cache of one sequence, one head, one key: whatever stride its view has there."""
+    N, T = 40, 3
+    q, k, v = rand(1, 1, 4, T, 128), rand(2, 1, 1, N, 128), rand(3, 1, 1, N, 128)
+    lens = torch.tensor([N - T], dtype=torch.int32)
+    K, V = (dev(x).as_strided((1, 1, N, 128), (7, 3, 128, 1)) for x in (k, v))
+    assert torch.equal(bpc.prefill_attention(dev(q), K, V), bpc.prefill_attention(dev(q), dev(k), dev(v)))
+    assert torch.equal(bpc.tree_attention(dev(q), K, V, dev(lens)), bpc.tree_attention(dev(q), dev(k), dev(v), dev(lens)))
+    K, V = (dev(x)[:, :, :1].as_strided((1, 1, 1, 128), (7, 3, 5, 1)) for x in (k, v))
+    assert torch.equal(bpc.prefill_attention(dev(q), K, V, pos0=0), bpc.prefill_attention(dev(q), dev(k), dev(v), N=1, pos0=0))
