@@ -651,6 +651,16 @@ int bpc_tree_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq
                        void* workspace, size_t workspace_bytes,
                        void* stream);
 
+/*
+ * bpc_attention_cut -- how bpc_prefill_attention, or with `tree`
+ * bpc_tree_attention, cuts a call of these sizes: *row_blocks (1, 4 or 8) blocks
+ * of 32 (token, head) rows a workgroup, *pieces (1 to 64) of the key axis, and
+ * whether keys and values are *streamed past the last-level cache.  For
+ * measurements and tests; results do not depend on it beyond rounding.
+ */
+int bpc_attention_cut(int B, int Hq, int Hkv, int T, int N, int D, int tree,
+                      int* row_blocks, int* pieces, int* streamed);
+
 #ifdef __cplusplus
 }
 #endif

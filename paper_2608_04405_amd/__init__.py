@@ -22,6 +22,7 @@ __all__ = [
     "BPCError",
     "append_kv",
     "append_kv_paged",
+    "attention_cut",
     "LIB_PATH",
     "build_hash",
     "build_workspace_bytes",
@@ -135,6 +136,9 @@ _lib.bpc_tree_workspace_bytes.argtypes = [_i] * 6
 _lib.bpc_tree_attention.restype = _i
 _lib.bpc_tree_attention.argtypes = [_p, _i64, _i64, _i64] * 3 + [_p, _i64, _i, _i, _p, _p, _i64] + [_i] * 6 + \
     [_f, _f, _p, _p, _i64, _i64, _i64, _p, _sz, _p]
+
+_lib.bpc_attention_cut.restype = _i
+_lib.bpc_attention_cut.argtypes = [_i] * 7 + [ctypes.POINTER(_i)] * 3
 
 DECODE_STAGES = 3
 DECODE_STAGE_NAMES = ("score", "attend", "merge")
@@ -899,6 +903,16 @@ def prefill_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, D: int = 
 @functools.lru_cache(maxsize=4096)
 def tree_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, D: int = 128) -> int:
     return int(_lib.bpc_tree_workspace_bytes(B, Hq, Hkv, T, N, D))
+
+
+def attention_cut(B: int, Hq: int, Hkv: int, T: int, N: int, D: int = 128, tree: bool = False):
+    """(row_blocks, pieces, streamed): the blocks of 32 rows (1, 4 or 8) of a
+    workgroup, the pieces of the key axis, and whether keys and values pass the
+    last-level cache by, in prefill_attention or (tree) tree_attention of these
+    sizes."""
+    row_blocks, pieces, streamed = _i(), _i(), _i()
+    _check(_lib.bpc_attention_cut(B, Hq, Hkv, T, N, D, tree, row_blocks, pieces, streamed), "bpc_attention_cut")
+    return row_blocks.value, pieces.value, bool(streamed.value)
 
 
 _SM_SCALE = 1.0 / math.sqrt(128)

@@ -807,6 +807,12 @@ AttnPlan attn_plan(int B, int Hkv, int G, int T, int N, bool tree) {
       if (!p.rb || us < best) best = us, p.rb = rb, p.splits = S;
     }
   }
+  // Keys that one row block reads, and more of them than the last-level cache
+  // (256 MB) holds until the next call, pass it by: 16 x 32768 slots, one token, 276
+  // and 246 us, 16 x 131072, eight tokens, 1047 and 945 us (6.9 TB/s); but 8 heads
+  // of 65536 keys (268 MB) 49 and 52 us, and for several row blocks 168 and 174 us
+  // (16 tokens over 8 x 32768 slots), 1094 and 1116 us (2 x 8192 causal tokens).
+  p.once = rows <= kBlockRows && bh * N * (4 * kHeadDim) > (int64_t)320 << 20;
   size_t o = 0;
   auto take = [&](size_t bytes) {
     size_t at = o;
@@ -824,13 +830,7 @@ AttnPlan attn_plan(int B, int Hkv, int G, int T, int N, bool tree) {
 
 template <AttnKind KIND>
 static hipError_t launch_attn_as(const AttnArgs& a, const AttnPlan& p) {
-  // Keys that one row block reads, and more of them than the last-level cache
-  // (256 MB) holds until the next call, pass it by: 16 x 32768 slots, one token, 276
-  // and 246 us, 16 x 131072, eight tokens, 1047 and 945 us (6.9 TB/s); but 8 heads
-  // of 65536 keys (268 MB) 49 and 52 us, and for several row blocks 168 and 174 us
-  // (16 tokens over 8 x 32768 slots), 1094 and 1116 us (2 x 8192 causal tokens).
-  const bool once = (int64_t)a.T * a.G <= kBlockRows && (int64_t)a.B * a.Hkv * a.N * (4 * kHeadDim) > (int64_t)320 << 20;
-  const hipError_t e = p.rb == 1   ? once ? launch_attn_shape<1, 4, 32, KIND, true>(a) : launch_attn_shape<1, 4, 32, KIND>(a)
+  const hipError_t e = p.rb == 1   ? p.once ? launch_attn_shape<1, 4, 32, KIND, true>(a) : launch_attn_shape<1, 4, 32, KIND>(a)
                        : p.rb == 4 ? launch_attn_shape<4, 1, 64, KIND>(a)
                                    : launch_attn_shape<8, 1, 64, kPrefill>(a);
   if (e != hipSuccess || a.splits == 1) return e;

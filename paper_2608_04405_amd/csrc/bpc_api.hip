@@ -823,11 +823,28 @@ static int check_attn_sizes(int B, int Hq, int Hkv, int T, int N, int D) {
   return BPC_OK;
 }
 
+static int check_drafts(int T, int N) {
+  if (T > 64) return fail(BPC_EUNSUPPORTED, "T=%d: at most 64 drafted tokens", T);
+  if (T > N) return fail(BPC_EINVAL, "T=%d drafts need as many slots, N=%d", T, N);
+  return BPC_OK;
+}
+
 static void attn_workspace(AttnArgs& a, const AttnPlan& plan, void* workspace) {
   a.splits = plan.splits;
   if (!plan.total) return;
   a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + plan.off_ml);
   a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.off_o);
+}
+
+int bpc_attention_cut(int B, int Hq, int Hkv, int T, int N, int D, int tree, int* row_blocks, int* pieces, int* streamed) {
+  g_last_error[0] = 0;
+  int st;
+  if ((st = check_attn_sizes(B, Hq, Hkv, T, N, D))) return st;
+  if (tree && (st = check_drafts(T, N))) return st;
+  if (!row_blocks || !pieces || !streamed) return fail(BPC_EINVAL, "row_blocks, pieces and streamed must not be NULL");
+  const AttnPlan plan = attn_plan(B, Hkv, Hq / Hkv, T, N, tree != 0);
+  *row_blocks = plan.rb, *pieces = plan.splits, *streamed = plan.once;
+  return BPC_OK;
 }
 
 size_t bpc_prefill_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D) {
@@ -877,8 +894,7 @@ int bpc_tree_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq
   g_last_error[0] = 0;
   int st;
   if ((st = check_attn_sizes(B, Hq, Hkv, T, N, D))) return st;
-  if (T > 64) return fail(BPC_EUNSUPPORTED, "T=%d: at most 64 drafted tokens", T);
-  if (T > N) return fail(BPC_EINVAL, "T=%d drafts need as many slots, N=%d", T, N);
+  if ((st = check_drafts(T, N))) return st;
   AttnArgs a{};
   a.q = q, a.sq_b = sq_b, a.sq_h = sq_h, a.sq_t = sq_t;
   a.K = K, a.sK_b = sK_b, a.sK_h = sK_h, a.sK_n = sK_n;

@@ -314,9 +314,11 @@ struct AttnArgs {
   float* part_o;
   hipStream_t stream;
 };
-// how a call is cut: 32-row blocks per workgroup, and pieces of the key axis
+// how a call is cut: 32-row blocks per workgroup, and pieces of the key axis;
+// once: keys and values pass the last-level cache by
 struct AttnPlan {
   int rb, splits;
+  bool once;
   size_t off_ml, off_o, total;
 };
 AttnPlan attn_plan(int B, int Hkv, int G, int T, int N, bool tree);

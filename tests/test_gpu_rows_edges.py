@@ -67,3 +67,19 @@ def test_strides_of_single_extents_do_not_matter():
     assert torch.equal(bpc.tree_attention(dev(q), K, V, dev(lens)), bpc.tree_attention(dev(q), dev(k), dev(v), dev(lens)))
     K, V = (dev(x)[:, :, :1].as_strided((1, 1, 1, 128), (7, 3, 5, 1)) for x in (k, v))
     assert torch.equal(bpc.prefill_attention(dev(q), K, V, pos0=0), bpc.prefill_attention(dev(q), dev(k), dev(v), N=1, pos0=0))
+
+
+@pytest.mark.parametrize("R,inter", [(0, False), (128, False), (64, False), (96, True)])
+@pytest.mark.parametrize("weights", ["none", "one", "each"])
+def test_rows_past_the_caches(R, inter, weights):
+    """More rows than the last-level cache holds, against the same rows in parts that it does hold."""
+    T, Hq, Hkv = 9001, 128, 5
+    g = torch.Generator(device=DEV).manual_seed(1)
+    q, k = (torch.randn(1, H, T, 128, generator=g, device=DEV).to(torch.bfloat16) for H in (Hq, Hkv))
+    table, pos = (dev(rope_table(T, R)), torch.arange(T, dtype=torch.int32, device=DEV)[None]) if R else (None, None)
+    w = {"none": {}, "one": dict(wq=dev(1 + rand(2, 128)), wk=dev(1 + rand(3, 128))),
+         "each": dict(wq=dev(1 + rand(2, Hq, 128)), wk=dev(1 + rand(3, Hkv, 128)))}[weights]
+    oq, ok = bpc.qk_norm_rope(q, k, pos, table, interleaved=inter, **w)
+    for a in range(0, T, 2500):
+        pq, pk = bpc.qk_norm_rope(q[:, :, a:a + 2500], k[:, :, a:a + 2500], pos[:, a:a + 2500] if R else None, table, interleaved=inter, **w)
+        assert torch.equal(oq[:, :, a:a + 2500], pq) and torch.equal(ok[:, :, a:a + 2500], pk)
