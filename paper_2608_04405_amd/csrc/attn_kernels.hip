@@ -102,7 +102,8 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t x) {
 // such copy in flight before any LDS read; the kernel waits by itself (dma_wait).
 // No register is written, so there is nothing in flight that the compiler does
 // not know of but the LDS bytes, which it cannot touch before dma_wait.
-// ONCE: bytes that no other workgroup reads, which need not stay in a cache.
+// ONCE: bytes that need not stay in a cache, as no other workgroup reads them (but
+// where sequences have pages in common).
 template <bool ONCE>
 __device__ __forceinline__ void dma16(const char* base, uint32_t off, uint32_t dst) {
   if (ONCE)
@@ -157,7 +158,7 @@ __device__ __forceinline__ LateArgs late_args() {
 // tiles of KT keys; RB KW wavefronts.
 enum AttnKind { kPrefill, kTree, kPagedTree };
 
-template <int RB, int KW, int KT, AttnKind KIND, bool CAP, bool BIAS>
+template <int KW, int KT>
 struct AttnShape {
   static constexpr int kTileBytes = KT * kRowBytes;    // K or V of a tile
   static constexpr int kLds = KW * 2 * 2 * kTileBytes;  // K and V, two buffers, per group
@@ -165,7 +166,7 @@ struct AttnShape {
 
 template <int RB, int KW, int KT, AttnKind KIND, bool CAP, bool BIAS, bool ONCE>
 __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnArgs a) {
-  using S = AttnShape<RB, KW, KT, KIND, CAP, BIAS>;
+  using S = AttnShape<KW, KT>;
   constexpr bool TREE = KIND != kPrefill, paged = KIND == kPagedTree;
   constexpr int NB = KT / 32;   // 32-key blocks of a tile
   constexpr int RPW = KT / RB;  // rows of a tile's K (and V) that a wavefront copies
@@ -753,7 +754,7 @@ static hipError_t launch_attn_shape(AttnArgs a) {
 #define BPC_ATTN(CAP, BIAS)                                                                                       \
   {                                                                                                               \
     auto* f = attn_kernel<RB, KW, KT, KIND, CAP, BIAS, ONCE>;                                                           \
-    constexpr int lds = AttnShape<RB, KW, KT, KIND, CAP, BIAS>::kLds;                                             \
+    constexpr int lds = AttnShape<KW, KT>::kLds;                                                                  \
     static std::atomic<uint64_t> allowed{0}; /* devices on which the kernel may use that much LDS */               \
     if (hipError_t e = allow_lds(reinterpret_cast<const void*>(f), lds, allowed); e != hipSuccess) return e;      \
     f<<<grid, RB * KW * 64, lds, a.stream>>>(a);                                                      \
@@ -808,10 +809,13 @@ AttnPlan attn_plan(int B, int Hkv, int G, int T, int N, bool tree) {
     }
   }
   // Keys that one row block reads, and more of them than the last-level cache
-  // (256 MB) holds until the next call, pass it by: 16 x 32768 slots, one token, 276
-  // and 246 us, 16 x 131072, eight tokens, 1047 and 945 us (6.9 TB/s); but 8 heads
-  // of 65536 keys (268 MB) 49 and 52 us, and for several row blocks 168 and 174 us
-  // (16 tokens over 8 x 32768 slots), 1094 and 1116 us (2 x 8192 causal tokens).
+  // (256 MB) holds until the next call, pass it by.  One token over 16 sequences, 8 KV
+  // heads, kept and streamed: 4096 slots (268 MB) 49.5 and 49.5 us, 5120 65.6 and
+  // 60.7, 8192 104 and 89, 32768 377 and 325 (pages of 64: 52.3 and 52.0, 64.5 and
+  // 61.3, 100 and 87, 363 and 323).  Of a cache that is filled in part, streaming what
+  // would have fitted costs little: 2000 of 131072 slots 32.9 and 32.9, 4000 48.8 and
+  // 50.4, 8000 104 and 85.  Several row blocks read each key again: 168 and 174 (16
+  // tokens over 8 x 32768 slots), 1094 and 1116 (2 x 8192 causal tokens).
   p.once = rows <= kBlockRows && bh * N * (4 * kHeadDim) > (int64_t)320 << 20;
   size_t o = 0;
   auto take = [&](size_t bytes) {
@@ -830,9 +834,14 @@ AttnPlan attn_plan(int B, int Hkv, int G, int T, int N, bool tree) {
 
 template <AttnKind KIND>
 static hipError_t launch_attn_as(const AttnArgs& a, const AttnPlan& p) {
-  const hipError_t e = p.rb == 1   ? p.once ? launch_attn_shape<1, 4, 32, KIND, true>(a) : launch_attn_shape<1, 4, 32, KIND>(a)
-                       : p.rb == 4 ? launch_attn_shape<4, 1, 64, KIND>(a)
-                                   : launch_attn_shape<8, 1, 64, kPrefill>(a);
+  hipError_t e;
+  if (p.rb == 1) {
+    e = p.once ? launch_attn_shape<1, 4, 32, KIND, true>(a) : launch_attn_shape<1, 4, 32, KIND>(a);
+  } else if (KIND != kPrefill || p.rb == 4) {  // (a tree's plan has no eight)
+    e = launch_attn_shape<4, 1, 64, KIND>(a);
+  } else {
+    e = launch_attn_shape<8, 1, 64, kPrefill>(a);
+  }
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.T * a.G;
   attn_merge_kernel<KIND != kPrefill><<<(unsigned)((rows + 3) / 4), 256, 0, a.stream>>>(a);

@@ -272,7 +272,8 @@ hipError_t launch_append_paged(const AppendPagedArgs& a);
 
 // ---- attention of many query rows -----------------------------------------
 // n / d of 0 <= n < 2^31 by a product (mul = 2^32 (2^shift - d) / d + 1, shift the
-// bits of d - 1): a division in a kernel costs it some 40 instructions.
+// bits of d - 1; Granlund and Montgomery, Division by invariant integers using
+// multiplication, 1994): a division in a kernel costs it some 40 instructions.
 struct FastDiv {
   uint32_t mul, shift;
   static FastDiv by(int d) {
