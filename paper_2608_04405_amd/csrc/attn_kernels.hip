@@ -359,7 +359,8 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
   }
-  float mrun = -INFINITY, lsum = 0.f;
+  // maximum, what a score has to exceed to move it, reference point (log2), sum
+  float mrun = -INFINITY, limit = -INFINITY, mu = 0.f, lsum = 0.f;
 
   const uint32_t kswz = swz(col & 15) ^ half;
   uint32_t kaddr[8], vaddr[4];
@@ -454,7 +455,7 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
     // the reference point of the exponentials moves only when a score lies more
     // than 2^8 above it, so that the products are seldom rescaled; any point
     // gives the same quotient
-    if (__any(mt > mrun + (CAP ? 8.f : c8))) {
+    if (__any(mt > limit)) {
       const float mn = fmaxf(mrun, mt);
       const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(reference_step<CAP>(mrun, mn, c1));
       mrun = mn;
@@ -464,17 +465,18 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] *= f;
       }
-    }
-    const float ref = mrun == -INFINITY ? 0.f : mrun;
-    float mu = CAP ? ref : ref * c1;
-    if (!CAP && __any(far_from_zero(ref, c1))) {
-      const float first = far_from_zero(ref, c1) ? ref : 0.f;
+      limit = mn + (CAP ? 8.f : c8);
+      const float ref = mn == -INFINITY ? 0.f : mn;
+      mu = CAP ? ref : ref * c1;
+      const bool far = !CAP && far_from_zero(ref, c1);
+      if (__any(far)) {  // every tile of such a row comes this way
+        if (far) limit = -INFINITY, mu = 0.f;
 #pragma unroll
-      for (int k = 0; k < NB; ++k) {
+        for (int k = 0; k < NB; ++k) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[k][e] -= first;
+          for (int e = 0; e < 16; ++e) acc[k][e] -= far ? ref : 0.f;
+        }
       }
-      mu = far_from_zero(ref, c1) ? 0.f : mu;
     }
     u32x4 pw[NB][2];
 #pragma unroll
