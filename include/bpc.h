@@ -543,8 +543,9 @@ int bpc_qk_norm_rope(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t
  *
  * k_new, v_new [B, Hkv, T, D] bf16, strides as in bpc_append_kv
  * K, V       [num_pages, Hkv, page_size, D] bf16 pools of pages, strides
- *            (sK_p, sK_h, sK_n) and (sV_p, sV_h, sV_n).  A contiguous cache
- *            [B, Hkv, Ncap, D] is one of B pages.
+ *            (sK_p, sK_h, sK_n) and (sV_p, sV_h, sV_n), apart from one another (two
+ *            views of one pool, say).  A contiguous cache [B, Hkv, Ncap, D] is one of
+ *            B pages.
  * block_table [B, max_pages] int32, stride st_b; no page serves two of the
  *            slots written
  * page_size  a power of two, 16 to 2^20

@@ -761,6 +761,8 @@ int bpc_append_kv_paged(const uint16_t* k_new, int64_t sKn_b, int64_t sKn_h, int
   if (rope_pos && (st = check_int32("rope_pos", rope_pos, sr_b))) return st;
   if ((st = check_apart("K", sK_p, sK_h, sK_n, num_pages, Hkv, page_size))) return st;
   if ((st = check_apart("V", sV_p, sV_h, sV_n, num_pages, Hkv, page_size))) return st;
+  const RowSet pools[2] = {{"K", K, {sK_p, sK_h, sK_n}, {num_pages, Hkv, page_size}}, {"V", V, {sV_p, sV_h, sV_n}, {num_pages, Hkv, page_size}}};
+  if ((st = check_separate(pools[0], pools[1]))) return st;
   AppendPagedArgs a{};
   a.kn = k_new, a.skn_b = sKn_b, a.skn_h = sKn_h, a.skn_t = sKn_t;
   a.vn = v_new, a.svn_b = sVn_b, a.svn_h = sVn_h, a.svn_t = sVn_t;

@@ -83,3 +83,18 @@ def test_rows_past_the_caches(R, inter, weights):
     for a in range(0, T, 2500):
         pq, pk = bpc.qk_norm_rope(q[:, :, a:a + 2500], k[:, :, a:a + 2500], pos[:, a:a + 2500] if R else None, table, interleaved=inter, **w)
         assert torch.equal(oq[:, :, a:a + 2500], pq) and torch.equal(ok[:, :, a:a + 2500], pk)
+
+
+def test_pools_in_one_buffer():
+    """Keys and values as the two halves of each page, and of each head's page."""
+    B, Hkv, T, page, pages = 2, 2, 5, 16, 7
+    k, v, table, pos = rand(1, B, Hkv, T, 128), rand(2, B, Hkv, T, 128), torch.tensor([[3, 0], [6, 2]], dtype=torch.int32), torch.tensor([13, 0], dtype=torch.int32)
+    K, V = (torch.zeros(pages, Hkv, page, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    bpc.append_kv_paged(dev(k), dev(v), K, V, dev(table), dev(pos))
+    assert torch.equal(K[3, :, 13:].cpu(), k[0, :, :3]) and torch.equal(V[0, :, :2].cpu(), v[0, :, 3:]) and torch.equal(K[6, :, :5].cpu(), k[1])
+    by_page, by_head = torch.zeros(pages, 2, Hkv, page, 128, dtype=torch.bfloat16, device=DEV), torch.zeros(pages, Hkv, 2, page, 128, dtype=torch.bfloat16, device=DEV)
+    for a, b in ((by_page[:, 0], by_page[:, 1]), (by_head[:, :, 1], by_head[:, :, 0])):
+        bpc.append_kv_paged(dev(k), dev(v), a, b, dev(table), dev(pos))
+        assert torch.equal(a, K) and torch.equal(b, V)
+    with pytest.raises(bpc.BPCError, match="overlaps"):
+        bpc.append_kv_paged(dev(k), dev(v), K, K, dev(table), dev(pos))

@@ -77,3 +77,11 @@ def test_results_on_their_inputs(lib, kw, word):
     """Neither in place nor apart: another wavefront may not have read what a row replaces."""
     assert call(lib, "bpc_qk_norm_rope", ROPE, kw) == EINVAL
     assert word in lib.bpc_last_error()
+
+
+@pytest.mark.parametrize("away", [0, 8, 2048, 8192, 6 * 8192 - 2048])
+def test_append_refuses_pools_that_share_rows(lib, away):
+    """K and V as views of a pool [7, 2, 2, 16, 128] whose pages meet."""
+    pool = dict(K_b=8192, K_h=2048, V_b=8192, V_h=2048)
+    assert call(lib, "bpc_append_kv_paged", APPEND, dict(pool, K=FAKE, V=FAKE + 2 * away)) == EINVAL
+    assert b"K overlaps V" in lib.bpc_last_error()
