@@ -582,7 +582,9 @@ int bpc_append_kv_paged(const uint16_t* k_new, int64_t sKn_b, int64_t sKn_h, int
  * key_begin at the first token of each token's document; a prefix mask is
  * key_end at the prefix's end where that lies behind the token.  A token that
  * sees no key (padding) gets zeros; what K and V hold at keys that a token does
- * not see does not reach it, whatever it is.
+ * not see does not reach it, whatever it is.  A bias enters without what the
+ * distances of all keys that a token sees have in common, so that positions may
+ * lie far from all of them.
  *
  * q          [B, Hq, T, D] bf16, strides (sq_b, sq_h, sq_t)
  * K, V       [B, Hkv, >=N, D] bf16, strides as in bpc_decode_attention; any
@@ -592,11 +594,13 @@ int bpc_append_kv_paged(const uint16_t* k_new, int64_t sKn_b, int64_t sKn_h, int
  * softcap    0 (none), or 2^-20 to 1024
  * slopes     [Hq] fp32 or NULL
  * key_begin, key_end  [B, T] int32, strides sb_b, se_b (0 = shared), or NULL
- * out        [B, Hq, T, D] bf16, strides (so_b, so_h, so_t) (written)
+ * out        [B, Hq, T, D] bf16, strides (so_b, so_h, so_t) (written); overlaps no
+ *            input
  * workspace  at least bpc_prefill_workspace_bytes(...) bytes (0 for most
  *            sizes), 256-byte aligned; its contents on entry do not matter.
  * fp32 scores, statistics and sums; the probabilities enter the second product
- * as bf16, out is rounded once.  One launch, or two where few query rows face
+ * as bf16, out is rounded once.  q_t . K_n has to be finite in fp32, as has 2^8
+ * times the sum of |V_n| over the keys that a token sees.  One launch, or two where few query rows face
  * many keys (the key axis is then split and joined).  More rows than a launch has
  * threads for (2^32: no fewer than 2^26 rows, B Hq T) are refused with
  * BPC_EUNSUPPORTED.
@@ -634,8 +638,10 @@ int bpc_prefill_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t
  *            skipped: its rows of out stay as they are.
  * tree       [B, T] int64 bit masks, stride sm_b, or NULL: a chain (draft t sees
  *            drafts 0..t).  Bits from T on are ignored.
- * N          slots that any sequence may use, drafts included (sets the
- *            workspace; need not be near the lengths)
+ * N          slots that any sequence may use, drafts included.  Sets the workspace
+ *            and how the work is cut, so that one near the longest sequence's is
+ *            the faster (one token over 1 x 4000 slots of 8 KV heads: N = 4096
+ *            12.4 us, N = 131072 18.7; over 4 x 4000 19.2 and 23.4).
  * sm_scale, softcap, slopes, out, workspace  as in bpc_prefill_attention, with
  *            bpc_tree_workspace_bytes(...)
  */

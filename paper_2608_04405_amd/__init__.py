@@ -954,7 +954,7 @@ def prefill_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, sm_scal
     document's first token for a document mask, end at the prefix's end for a
     prefix mask.  Scores are capped to softcap * tanh(s / softcap) when softcap
     > 0, then lowered by slopes[head] * distance.  A token that sees nothing
-    gets zeros."""
+    gets zeros.  `out` overlaps no input."""
     B, Hq, Hkv, T, sq, so, Kb, Kn, sK, Vb, Vh, Vn, sV = _attn_inputs(q, K, V, slopes, out, workspace)
     N = Kn if N is None else N
     if N < 1:
@@ -1004,7 +1004,7 @@ def tree_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torc
     contiguous cache [B, Hkv, >=N, 128], or with block_table (int32 [B, pages of
     a sequence]) pools of pages [pages, Hkv, page, 128] as append_kv_paged writes
     them.  N: slots that any sequence may use (default: what the cache or the
-    table holds).  softcap and slopes as in prefill_attention, a draft's position
+    table holds); one near the longest sequence cuts the work best.  softcap and slopes as in prefill_attention, a draft's position
     being lens[b] plus its depth.  A sequence whose lens[b] is not in [0, N - T]
     is skipped: its rows of `out` stay as they are (undefined where `out` is
     allocated here)."""

@@ -19,11 +19,13 @@
 // four consecutive rows' neighbouring four chunks (the transposing reads that
 // make the V operand) then lie in different banks.
 //
-// Bound by the matrix units and the power limit where rows are many (2 x 8192
-// causal tokens, 32 heads: 1.09 ms, 1.0 PFLOP/s of visible pairs, matrix units 44 %
-// busy at 2.1 GHz), by memory where they are few (8 tokens over 16 x 131072 slots:
-// 0.94 ms, 6.8 TB/s), by vector issue where scores are capped (8001 tokens in
-// documents: 0.19 ms, 0.55 PFLOP/s).
+// Where rows are many a SIMD's two wavefronts are in the same phase of a tile, so
+// products and softmax run almost one after the other: 2 x 8192 causal tokens, 32
+// heads, 1.04 ms, 1.05 PFLOP/s of visible pairs, matrix units busy 46 % of the cycles,
+// other vector instructions 35 % and more; 512 queries over 65536 keys with a bias
+// 0.57 ms, 41 and 50 %; capped scores (8001 tokens in documents, 0.19 ms, 0.55 PFLOP/s)
+// 22 and 37 %, three of their instructions transcendental.  Where rows are few by
+// memory (8 tokens over 16 x 131072 slots: 0.94 ms, 6.8 TB/s).
 #include <math.h>
 
 #include <atomic>
