@@ -668,6 +668,143 @@ int bpc_tree_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq
 int bpc_attention_cut(int B, int Hq, int Hkv, int T, int N, int D, int tree,
                       int* row_blocks, int* pieces, int* streamed);
 
+/*
+ * bpc_chunk_attention -- dense attention of a chunk of new tokens over the cache,
+ * paged or contiguous, that holds them (bpc_append_kv_paged with the same pos and
+ * count): the prefill of a prompt piece by piece, sequences at lengths of their
+ * own, and with T = 1 a dense step.  Token t < count[b] of sequence b stands at
+ * slot p = pos[b] + t and sees the slots n <= p; with a window the last `window`
+ * of them, p itself included, and the first `sinks` of the cache:
+ *     s_n = sm_scale * q_t . K_n
+ *     s_n = softcap * tanh(s_n / softcap)          (softcap > 0)
+ *     s_n = s_n - slopes[head] * (p - n)           (slopes given)
+ *     out_t = softmax over the visible n of s_n, applied to V_n
+ *     lse_t = log of the sum over the visible n of exp(s_n)
+ * Rows of tokens t >= count[b] stay as they are, as do all rows of a sequence whose
+ * slots are not all in [0, N).  A token that sees no slot (none of its pages is in
+ * the pool) gets zeros, and -inf as lse; what K and V hold at slots that a token
+ * does not see does not reach it, whatever it is.
+ *
+ * q          [B, Hq, T, D] bf16, strides (sq_b, sq_h, sq_t)
+ * K, V       without block_table [B, Hkv, >=N, D], strides (batch, head, row);
+ *            with it pools [num_pages, Hkv, page_size, D], strides (page, head, row)
+ * block_table, st_b, num_pages, page_size  as in bpc_tree_attention
+ * pos        [B] int32: slot of each sequence's first new token
+ * count      [B] int32: new tokens of each sequence (below 0 as 0, above T as T),
+ *            or NULL: T of each
+ * N          slots that any sequence may use, new tokens included; sets the
+ *            workspace and how the work is cut, as in bpc_tree_attention
+ * window     slots that a token sees up to its own, or 0: all
+ * sinks      first slots that stay visible (ignored without a window)
+ * sm_scale, softcap, slopes, out  as in bpc_prefill_attention
+ * lse        [B, Hq, T] fp32, strides (sl_b, sl_h), or NULL (written).  Its rows
+ *            overlap neither one another nor another argument.
+ * workspace  at least bpc_chunk_workspace_bytes(...) bytes, as in
+ *            bpc_prefill_attention, whose limits hold here too
+ */
+size_t bpc_chunk_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D, int window, int sinks);
+int bpc_chunk_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
+                        const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n,
+                        const uint16_t* V, int64_t sV_b, int64_t sV_h, int64_t sV_n,
+                        const int32_t* block_table, int64_t st_b, int num_pages, int page_size,
+                        const int32_t* pos, const int32_t* count,
+                        int B, int Hq, int Hkv, int T, int N, int D,
+                        float sm_scale, float softcap, const float* slopes,
+                        int window, int sinks,
+                        uint16_t* out, int64_t so_b, int64_t so_h, int64_t so_t,
+                        float* lse, int64_t sl_b, int64_t sl_h,
+                        void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/*
+ * bpc_chunk_cut -- how bpc_chunk_attention cuts a call of these sizes, as
+ * bpc_attention_cut for the others.
+ */
+int bpc_chunk_cut(int B, int Hq, int Hkv, int T, int N, int D, int window, int sinks,
+                  int* row_blocks, int* pieces, int* streamed);
+
+/*
+ * bpc_key_weights -- the attention weight that each cached slot gathers from a
+ * chunk of tokens, by which bpc_evict_kv chooses.  With the tokens, the slots that
+ * they see and the scores s of bpc_chunk_attention, and its lse:
+ *     weights[b][h][n] = decay * weights[b][h][n]
+ *                      + sum over t < count[b] that see n, query heads j of h, of
+ *                        exp(s_{j,t,n} - lse[b][j][t])
+ * for every slot n < pos[b] + count[b]; the weights of other slots, and of a
+ * sequence whose slots are not all in [0, N), stay as they are.  A token whose lse
+ * is -inf adds nothing.  The last tokens of a prompt alone: views of q and lse, and
+ * pos moved on.
+ *
+ * q, K, block_table, st_b, num_pages, page_size, pos, count, N, sm_scale, softcap,
+ * slopes, window, sinks  as in bpc_chunk_attention
+ * lse        [B, Hq, T] fp32, strides (sl_b, sl_h)
+ * weights    [B, Hkv, >=N] fp32, strides (sw_b, sw_h) (read and written; with
+ *            decay 0 written only).  Its rows overlap neither one another nor
+ *            another argument.
+ * decay      finite, >= 0; 1 adds to what is there
+ * fp32 scores, exponentials and sums; equal calls give equal bits.  A sum over many
+ * tokens loses no more than its last rounding and those of 16 terms at a time.
+ * No workspace; one kernel launch.
+ */
+int bpc_key_weights(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
+                    const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n,
+                    const float* lse, int64_t sl_b, int64_t sl_h,
+                    float* weights, int64_t sw_b, int64_t sw_h,
+                    const int32_t* block_table, int64_t st_b, int num_pages, int page_size,
+                    const int32_t* pos, const int32_t* count,
+                    int B, int Hq, int Hkv, int T, int N, int D,
+                    float sm_scale, float softcap, const float* slopes,
+                    int window, int sinks, float decay,
+                    void* stream);
+
+/*
+ * bpc_evict_kv -- a cache cut to the slots that gather the most attention.  Of the
+ * n = lens[b] slots of each (b, h), all stay if n <= keep; else the first `sinks`,
+ * the last `recent`, and of the others the keep - sinks - recent of the largest
+ * weights, the lower slot first among equals (a NaN counts as less than anything,
+ * and the two zeros as equal).  With their indices s_0 < s_1 < ...:
+ *     kept[b][h][i] = s_i                      (-1 from min(n, keep) on)
+ *     K_out[b][h][i] = K[b][h][s_i], V_out, codes_out likewise
+ *     weights_out[b][h][i] = weights[b][h][s_i] (0 from min(n, keep) on)
+ * Sequences then have min(n, keep) slots, in the order of the old ones, and
+ * bpc_append_kv_paged and the others go on from there (with positions of the tokens'
+ * own as rope_pos).  A sequence whose lens[b] is not in [0, N] is skipped.  Nothing
+ * else is written; rows whose page, read or written, is not in its pool are left out.
+ *
+ * K, V       [B, Hkv, >=N, D], or with block_table pools of pages, as in
+ *            bpc_chunk_attention
+ * weights    [B, Hkv, >=N] fp32, strides (sw_b, sw_h)
+ * keep       1 to N; sinks, recent >= 0, together at most keep
+ * K_out, V_out  [B, Hkv, >=keep, D], or with table_out pools [out_pages, Hkv,
+ *            out_page_size, D], table_out [B, >= ceil(keep / out_page_size)] int32,
+ *            stride sto_b.  Apart from one another and from K and V; with both tables
+ *            they may be the same pools, in which no page that is written is read
+ *            (pages shared by sequences stay whole for the others) or written twice.
+ * codes, codes_out  [B, Hkv, >=N, W] and [B, Hkv, >=keep, W] words as in
+ *            bpc_build_hash, W 1, 2 or 4, or both NULL
+ * weights_out [B, Hkv, cap] fp32, strides (swo_b, swo_h), cap >= keep, or NULL
+ * kept       [B, Hkv, keep] int32 contiguous
+ * No output's range of addresses meets another's or an input's (K and V: above).
+ * workspace  at least bpc_evict_workspace_bytes(...) bytes (may be 0), 256-byte
+ *            aligned; its contents on entry do not matter.
+ */
+size_t bpc_evict_workspace_bytes(int B, int Hkv, int N, int keep);
+int bpc_evict_kv(const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n,
+                 const uint16_t* V, int64_t sV_b, int64_t sV_h, int64_t sV_n,
+                 const int32_t* block_table, int64_t st_b, int num_pages, int page_size,
+                 const float* weights, int64_t sw_b, int64_t sw_h,
+                 const int32_t* lens,
+                 int B, int Hkv, int N, int D, int keep, int sinks, int recent,
+                 uint16_t* K_out, int64_t sKo_b, int64_t sKo_h, int64_t sKo_n,
+                 uint16_t* V_out, int64_t sVo_b, int64_t sVo_h, int64_t sVo_n,
+                 const int32_t* table_out, int64_t sto_b, int out_pages, int out_page_size,
+                 const uint32_t* codes, int64_t sC_b, int64_t sC_h,
+                 uint32_t* codes_out, int64_t sCo_b, int64_t sCo_h, int W,
+                 float* weights_out, int64_t swo_b, int64_t swo_h, int cap,
+                 int32_t* kept,
+                 void* workspace, size_t workspace_bytes,
+                 void* stream);
+
 #ifdef __cplusplus
 }
 #endif

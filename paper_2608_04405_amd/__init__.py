@@ -23,6 +23,9 @@ __all__ = [
     "append_kv",
     "append_kv_paged",
     "attention_cut",
+    "chunk_attention",
+    "chunk_cut",
+    "chunk_workspace_bytes",
     "LIB_PATH",
     "build_hash",
     "build_workspace_bytes",
@@ -36,6 +39,9 @@ __all__ = [
     "decode_noalloc_max_bytes",
     "decode_per_head_workspace_bytes",
     "dense_attention",
+    "evict_kv",
+    "evict_workspace_bytes",
+    "key_weights",
     "prefill_attention",
     "prefill_workspace_bytes",
     "qk_norm_rope",
@@ -137,6 +143,21 @@ _lib.bpc_tree_attention.restype = _i
 _lib.bpc_tree_attention.argtypes = [_p, _i64, _i64, _i64] * 3 + [_p, _i64, _i, _i, _p, _p, _i64] + [_i] * 6 + \
     [_f, _f, _p, _p, _i64, _i64, _i64, _p, _sz, _p]
 
+_lib.bpc_chunk_workspace_bytes.restype = _sz
+_lib.bpc_chunk_workspace_bytes.argtypes = [_i] * 8
+_lib.bpc_chunk_attention.restype = _i
+_lib.bpc_chunk_attention.argtypes = [_p, _i64, _i64, _i64] * 3 + [_p, _i64, _i, _i, _p, _p] + [_i] * 6 + \
+    [_f, _f, _p, _i, _i, _p, _i64, _i64, _i64, _p, _i64, _i64, _p, _sz, _p]
+_lib.bpc_chunk_cut.restype = _i
+_lib.bpc_chunk_cut.argtypes = [_i] * 8 + [ctypes.POINTER(_i)] * 3
+_lib.bpc_key_weights.restype = _i
+_lib.bpc_key_weights.argtypes = [_p, _i64, _i64, _i64] * 2 + [_p, _i64, _i64] * 2 + [_p, _i64, _i, _i, _p, _p] + [_i] * 6 + \
+    [_f, _f, _p, _i, _i, _f, _p]
+_lib.bpc_evict_workspace_bytes.restype = _sz
+_lib.bpc_evict_workspace_bytes.argtypes = [_i] * 4
+_lib.bpc_evict_kv.restype = _i
+_lib.bpc_evict_kv.argtypes = [_p, _i64, _i64, _i64] * 2 + [_p, _i64, _i, _i, _p, _i64, _i64, _p] + [_i] * 7 + \
+    [_p, _i64, _i64, _i64] * 2 + [_p, _i64, _i, _i] + [_p, _i64, _i64] * 2 + [_i, _p, _i64, _i64, _i, _p, _p, _sz, _p]
 _lib.bpc_attention_cut.restype = _i
 _lib.bpc_attention_cut.argtypes = [_i] * 7 + [ctypes.POINTER(_i)] * 3
 
@@ -1048,3 +1069,245 @@ def tree_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torc
     if status:
         _check(status, "bpc_tree_attention")
     return out
+
+
+@functools.lru_cache(maxsize=4096)
+def chunk_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, window: int = 0, sinks: int = 0, D: int = 128) -> int:
+    return int(_lib.bpc_chunk_workspace_bytes(B, Hq, Hkv, T, N, D, window, sinks))
+
+
+def chunk_cut(B: int, Hq: int, Hkv: int, T: int, N: int, window: int = 0, sinks: int = 0, D: int = 128):
+    """(row_blocks, pieces, streamed) of chunk_attention, as attention_cut."""
+    row_blocks, pieces, streamed = _i(), _i(), _i()
+    _check(_lib.bpc_chunk_cut(B, Hq, Hkv, T, N, D, window, sinks, row_blocks, pieces, streamed), "bpc_chunk_cut")
+    return row_blocks.value, pieces.value, bool(streamed.value)
+
+
+def _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, V=None, weights=None):
+    """(N, pages, page, table stride) of a call over a contiguous cache or pools
+    of pages, whose extents it checks; N: by default what they and the weights
+    hold."""
+    most_weights = weights.shape[2] if isinstance(weights, torch.Tensor) and weights.dim() == 3 else 1 << 30
+    if block_table is None:
+        N = min(Kn, most_weights) if N is None else N
+        if Kb != B or Kn < N:
+            _extent(K, "K", (B, Hkv, ("ge", N), 128))
+        if V is not None and (V.shape[0] != B or V.shape[1] != Hkv or V.shape[2] < N):
+            _extent(V, "V", (B, Hkv, ("ge", N), 128))
+        pages = page = st = 0
+    else:
+        pages, page = Kb, Kn
+        if V is not None and V.shape[:3] != K.shape[:3]:
+            _extent(V, "V", (pages, Hkv, page, 128))
+        _page_rows(page)
+        st, most = _block_table(block_table, B)
+        most *= page
+        N = min(most, most_weights) if N is None else N
+        if N > most:
+            raise ValueError(f"N={N}: the block_table holds {most} slots per sequence")
+    if N < 1:
+        raise ValueError(f"N={N} must be >= 1")
+    return N, pages, page, st
+
+
+def _float_rows(t: Optional[torch.Tensor], name: str, shape, written: bool):
+    """(batch, head) strides of an fp32 [B, H, n] tensor with contiguous rows
+    (spec of n as for _extent); rows that are written must not overlap."""
+    if t is None:
+        return 0, 0
+    if type(t) is not torch.Tensor or t.dtype is not torch.float32 or t.dim() != 3 or t.shape != shape or t.stride(2) != 1:
+        _need(t, name, torch.float32, 3)
+        _extent(t, name, shape)
+    (B, H, n), (x, y, _) = t.shape, t.stride()
+    if written and not t.is_contiguous():
+        span = n
+        for stride, extent in sorted(((x, B), (y, H))):
+            if extent > 1:
+                if stride < span:
+                    raise ValueError(f"{name}: its rows must not overlap (strides {tuple(t.stride())})")
+                span += stride * (extent - 1)
+    return x if B > 1 else 0, y if H > 1 else 0
+
+
+def _window(window: int, sinks: int) -> None:
+    if window < 0 or sinks < 0:
+        raise ValueError(f"window={window} and sinks={sinks} must be >= 0")
+
+
+def chunk_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, pos: torch.Tensor, sm_scale: Optional[float] = None,
+                    N: Optional[int] = None, *, count: Optional[torch.Tensor] = None,
+                    block_table: Optional[torch.Tensor] = None, softcap: float = 0.0,
+                    slopes: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0,
+                    out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Dense attention of a chunk of new tokens q [B, Hq, T, 128] bf16 over the
+    cache that holds them, token t < count[b] (int32 [B], default T) of sequence b
+    at slot pos[b] + t (int32 [B]), where append_kv_paged stores it; returns out
+    [B, Hq, T, 128] bf16.
+
+    A token sees the slots up to its own; with `window` the last so many of them
+    and the first `sinks` of the cache.  K, V are the contiguous cache [B, Hkv,
+    >=N, 128], or with block_table (int32 [B, pages of a sequence]) pools of pages
+    [pages, Hkv, page, 128].  N: slots that any sequence may use (default: what the
+    cache or the table holds); one near the longest sequence cuts the work best.
+    softcap and slopes as in prefill_attention.  lse_out [B, Hq, T] fp32, when
+    given, gets the logarithm of each row's sum of exponentials.  Rows of tokens
+    from count[b] on, and of a sequence whose slots are not all in [0, N), stay as
+    they are (undefined where `out` is allocated here)."""
+    B, Hq, Hkv, T, sq, so, Kb, Kn, sK, Vb, Vh, Vn, sV = _attn_inputs(q, K, V, slopes, out, workspace)
+    N, pages, page, st = _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, V)
+    _window(window, sinks)
+    _indices(pos, "pos", (B,))
+    _indices(count, "count", (B,))
+    sl = _float_rows(lse_out, "lse_out", (B, Hq, T), True)
+    _on_gpu(q, K, V, pos, count, block_table, slopes, out, lse_out, workspace)
+    dev = q.get_device()
+    if stream is not None or dev != _current_device():
+        with _place(q, stream):
+            return chunk_attention(q, K, V, pos, sm_scale, N, count=count, block_table=block_table, softcap=softcap,
+                                   slopes=slopes, window=window, sinks=sinks, out=out, lse_out=lse_out, workspace=workspace)
+    if out is None:
+        out = q.new_empty((B, Hq, T, 128))
+    if workspace is None:
+        need = chunk_workspace_bytes(B, Hq, Hkv, T, N, window, sinks)
+        if need:
+            workspace = q.new_empty(need, dtype=torch.uint8)
+    status = _lib.bpc_chunk_attention(
+        q.data_ptr(), *sq, K.data_ptr(), *sK, V.data_ptr(), *sV, _ptr(block_table), st, pages, page, pos.data_ptr(),
+        _ptr(count), B, Hq, Hkv, T, N, 128, _SM_SCALE if sm_scale is None else sm_scale, softcap, _ptr(slopes),
+        min(window, 1 << 30), min(sinks, 1 << 30), out.data_ptr(), *so, _ptr(lse_out), *sl, _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _current_stream(dev))
+    if status:
+        _check(status, "bpc_chunk_attention")
+    return out
+
+
+def key_weights(q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, weights: torch.Tensor, pos: torch.Tensor,
+                sm_scale: Optional[float] = None, N: Optional[int] = None, *, count: Optional[torch.Tensor] = None,
+                block_table: Optional[torch.Tensor] = None, softcap: float = 0.0,
+                slopes: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0, decay: float = 1.0,
+                stream=None) -> torch.Tensor:
+    """Adds to `weights` [B, Hkv, >=N] fp32 the attention weight that each cached
+    slot gathers from the tokens of a chunk_attention call: the sum over its
+    tokens and the query heads of a KV head of exp(score - lse), lse [B, Hq, T]
+    fp32 being that call's lse_out; the other arguments are that call's.  What was
+    there is multiplied by `decay` first (0: not even read).  Slots from pos[b] +
+    count[b] on, and sequences whose slots are not all in [0, N), stay as they are
+    (N: by default what the cache or the table, and the weights, hold).  Returns
+    weights."""
+    B, Hq, T, *sq = _rows(q, "q")
+    Kb, Hkv, Kn, sK = _cache(K, "K")
+    if Hq % Hkv:
+        raise ValueError(f"Hq={Hq} must be a multiple of Hkv={Hkv}")
+    if slopes is not None:
+        _need(slopes, "slopes", torch.float32, 1)
+        _extent(slopes, "slopes", (Hq,))
+    N, pages, page, st = _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, None, weights)
+    _window(window, sinks)
+    _indices(pos, "pos", (B,))
+    _indices(count, "count", (B,))
+    sl = _float_rows(lse, "lse", (B, Hq, T), False)
+    sw = _float_rows(weights, "weights", (B, Hkv, ("ge", N)), True)
+    _on_gpu(q, K, lse, weights, pos, count, block_table, slopes)
+    dev = q.get_device()
+    if stream is not None or dev != _current_device():
+        with _place(q, stream):
+            return key_weights(q, K, lse, weights, pos, sm_scale, N, count=count, block_table=block_table, softcap=softcap,
+                               slopes=slopes, window=window, sinks=sinks, decay=decay)
+    status = _lib.bpc_key_weights(
+        q.data_ptr(), *sq, K.data_ptr(), *sK, lse.data_ptr(), *sl, weights.data_ptr(), *sw, _ptr(block_table), st, pages, page,
+        pos.data_ptr(), _ptr(count), B, Hq, Hkv, T, N, 128, _SM_SCALE if sm_scale is None else sm_scale, softcap,
+        _ptr(slopes), min(window, 1 << 30), min(sinks, 1 << 30), decay, _current_stream(dev))
+    if status:
+        _check(status, "bpc_key_weights")
+    return weights
+
+
+@functools.lru_cache(maxsize=4096)
+def evict_workspace_bytes(B: int, Hkv: int, N: int, keep: int) -> int:
+    return int(_lib.bpc_evict_workspace_bytes(B, Hkv, N, keep))
+
+
+def evict_kv(K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, lens: torch.Tensor, keep: int, K_out: torch.Tensor,
+             V_out: torch.Tensor, *, sinks: int = 0, recent: int = 0, N: Optional[int] = None,
+             block_table: Optional[torch.Tensor] = None, table_out: Optional[torch.Tensor] = None,
+             codes: Optional[torch.Tensor] = None, codes_out: Optional[torch.Tensor] = None,
+             weights_out: Optional[torch.Tensor] = None, kept_out: Optional[torch.Tensor] = None,
+             workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Cuts a cache to `keep` slots of each KV head: the first `sinks`, the last
+    `recent`, and of the others those of the largest weights [B, Hkv, >=N] fp32, the
+    lower slot first among equals (all lens[b] of them where these are not more;
+    lens int32 [B]).  Their rows of K and V go, in order, to the first slots of
+    K_out and V_out, those of codes to codes_out, their weights to weights_out
+    (zeros behind); returns their old slots [B, Hkv, keep] int32, -1 behind.
+
+    K, V are the contiguous cache [B, Hkv, >=N, 128], or with block_table pools of
+    pages; K_out, V_out [B, Hkv, >=keep, 128], or with table_out (int32 [B, pages of
+    a sequence]) pools of pages, which may be K and V themselves as long as no page
+    that is written is read or written twice.  codes as build_hash gives them.  N:
+    slots that any sequence may use (default: what the cache or the table, and the
+    weights, hold); one whose lens[b] is not in [0, N] is skipped.  The sequences'
+    new lengths are lens.clamp(max=keep)."""
+    Kb, Hkv, Kn, sK = _cache(K, "K")
+    Vb, Vh, Vn, sV = _cache(V, "V")
+    _indices(lens, "lens", (lens.shape[0],) if isinstance(lens, torch.Tensor) and lens.dim() == 1 else (1,))
+    B = lens.shape[0]
+    if Vh != Hkv:
+        _extent(V, "V", (Vb, Hkv, Vn, 128))
+    N, pages, page, st = _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, V, weights)
+    if not 1 <= keep <= N:
+        raise ValueError(f"keep={keep} must be in [1, N={N}]")
+    if sinks < 0 or recent < 0 or sinks + recent > keep:
+        raise ValueError(f"sinks={sinks} and recent={recent} must be >= 0, together at most keep={keep}")
+    Ob, Oh, On, *_ = _rows(K_out, "K_out")
+    out_pages = out_page = sto = 0
+    if table_out is None:
+        if Ob != B or Oh != Hkv or On < keep:
+            _extent(K_out, "K_out", (B, Hkv, ("ge", keep), 128))
+        _extent(V_out, "V_out", (B, Hkv, ("ge", keep), 128))
+    else:
+        out_pages, out_page = Ob, On
+        _page_rows(out_page)
+        sto, most = _block_table(table_out, B)
+        if most * out_page < keep:
+            raise ValueError(f"table_out holds {most * out_page} slots per sequence, keep={keep}")
+    sKo, sVo = _written(K_out, "K_out", Ob, Hkv, On), _written(V_out, "V_out", Ob, Hkv, V_out.shape[2] if table_out is None else On)
+    sw = _float_rows(weights, "weights", (B, Hkv, ("ge", N)), False)
+    swo = _float_rows(weights_out, "weights_out", (B, Hkv, ("ge", keep)), True)
+    if (codes is None) != (codes_out is None):
+        raise ValueError("codes and codes_out are given together or not at all")
+    W, sC, sCo = 0, (0, 0), (0, 0)
+    if codes is not None:
+        _u32_codes(codes)
+        _u32_codes(codes_out, "codes_out")
+        W = codes.shape[3]
+        if W not in (1, 2, 4):
+            raise ValueError(f"codes of {W} words: the code length must be 32, 64 or 128")
+        _extent(codes, "codes", (B, Hkv, ("ge", N), W))
+        _extent(codes_out, "codes_out", (B, Hkv, ("ge", keep), W))
+        sC, sCo = (codes.stride(0), codes.stride(1)), (codes_out.stride(0), codes_out.stride(1))
+    _exact_out(kept_out, "kept_out", torch.int32, (B, Hkv, keep))
+    if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 tensor")
+    _on_gpu(K, V, weights, lens, K_out, V_out, block_table, table_out, codes, codes_out, weights_out, kept_out, workspace)
+    dev = K.get_device()
+    if stream is not None or dev != _current_device():
+        with _place(K, stream):
+            return evict_kv(K, V, weights, lens, keep, K_out, V_out, sinks=sinks, recent=recent, N=N, block_table=block_table,
+                            table_out=table_out, codes=codes, codes_out=codes_out, weights_out=weights_out,
+                            kept_out=kept_out, workspace=workspace)
+    if kept_out is None:
+        kept_out = lens.new_empty((B, Hkv, keep))
+    if workspace is None:
+        need = evict_workspace_bytes(B, Hkv, N, keep)
+        if need:
+            workspace = lens.new_empty(need, dtype=torch.uint8)
+    status = _lib.bpc_evict_kv(
+        K.data_ptr(), *sK, V.data_ptr(), *sV, _ptr(block_table), st, pages, page, weights.data_ptr(), *sw, lens.data_ptr(),
+        B, Hkv, N, 128, keep, sinks, recent, K_out.data_ptr(), *sKo, V_out.data_ptr(), *sVo, _ptr(table_out), sto, out_pages,
+        out_page, _ptr(codes), *sC, _ptr(codes_out), *sCo, W, _ptr(weights_out), *swo,
+        0 if weights_out is None else weights_out.shape[2], kept_out.data_ptr(), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _current_stream(dev))
+    if status:
+        _check(status, "bpc_evict_kv")
+    return kept_out

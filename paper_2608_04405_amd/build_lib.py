@@ -23,8 +23,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libbpc.so")
 OUT_TRACE = os.path.join(HERE, "libbpc_trace.so")
 BUILD_DIR = os.path.join(os.path.dirname(HERE), "_build")
-SOURCES = ["attn_kernels.hip", "bpc_api.hip", "build_kernels.hip", "build_scan_kernels.hip", "decode_kernels.hip", "eas_kernels.hip", "hash_mm_kernels.hip",
-           "rope_kernels.hip"]
+SOURCES = ["attn_chunk_kernels.hip", "attn_chunk_paged_kernels.hip", "attn_kernels.hip", "bpc_api.hip", "build_kernels.hip", "build_scan_kernels.hip", "decode_kernels.hip", "eas_kernels.hip", "evict_kernels.hip",
+           "hash_mm_kernels.hip", "rope_kernels.hip", "weights_kernels.hip"]
 ARCH = os.environ.get("BPC_OFFLOAD_ARCH", "gfx950")
 
 COMMON = [

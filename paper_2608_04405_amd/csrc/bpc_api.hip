@@ -785,7 +785,18 @@ static bool attn_sizes_ok(int B, int Hq, int Hkv, int T, int N, int D) {
          N <= (1 << 30) && (int64_t)B * Hkv <= (1 << 20) && (int64_t)T * (Hq / Hkv) <= (1 << 30);
 }
 
-// what the two attention entry points have in common
+// how products become scores
+static int check_scores(float sm_scale, float softcap, const float* slopes) {
+  if (!(sm_scale > 0.0f) || !__builtin_isfinite(sm_scale)) return fail(BPC_EINVAL, "sm_scale must be finite and > 0");
+  if (!(softcap >= 0.0f) || !__builtin_isfinite(softcap)) return fail(BPC_EINVAL, "softcap must be finite and >= 0");
+  // fp32 holds slope * distance / sm_scale, and softcap * tanh() to 2^-12
+  if (sm_scale < 0x1p-40f || sm_scale > 0x1p40f) return fail(BPC_EUNSUPPORTED, "sm_scale=%g: 2^-40 to 2^40", sm_scale);
+  if (softcap != 0.0f && (softcap < 0x1p-20f || softcap > 1024.0f)) return fail(BPC_EUNSUPPORTED, "softcap=%g: 2^-20 to 1024", softcap);
+  if (slopes && !aligned4(slopes)) return fail(BPC_EALIGN, "slopes must be 4-byte aligned");
+  return BPC_OK;
+}
+
+// what the attention entry points have in common
 static int check_attn(const AttnArgs& a, int Hq, int D, const AttnPlan& plan, const void* workspace, size_t workspace_bytes) {
   int st;
   if ((st = check_rows("q", a.q, a.sq_b, a.sq_h, a.sq_t))) return st;
@@ -793,13 +804,7 @@ static int check_attn(const AttnArgs& a, int Hq, int D, const AttnPlan& plan, co
   if ((st = check_kv("V", a.V, a.sV_b, a.sV_h, a.sV_n))) return st;
   if (a.sK_n > (1 << 24) || a.sV_n > (1 << 24)) return fail(BPC_EUNSUPPORTED, "row strides of K and V: at most 2^24 elements");
   if ((st = check_written("out", a.out, a.so_b, a.so_h, a.so_t, a.B, Hq, a.T))) return st;
-  if (!(a.sm_scale > 0.0f) || !__builtin_isfinite(a.sm_scale)) return fail(BPC_EINVAL, "sm_scale must be finite and > 0");
-  if (!(a.softcap >= 0.0f) || !__builtin_isfinite(a.softcap)) return fail(BPC_EINVAL, "softcap must be finite and >= 0");
-  // fp32 holds slope * distance / sm_scale, and softcap * tanh() to 2^-12
-  if (a.sm_scale < 0x1p-40f || a.sm_scale > 0x1p40f) return fail(BPC_EUNSUPPORTED, "sm_scale=%g: 2^-40 to 2^40", a.sm_scale);
-  if (a.softcap != 0.0f && (a.softcap < 0x1p-20f || a.softcap > 1024.0f))
-    return fail(BPC_EUNSUPPORTED, "softcap=%g: 2^-20 to 1024", a.softcap);
-  if (a.slopes && !aligned4(a.slopes)) return fail(BPC_EALIGN, "slopes must be 4-byte aligned");
+  if ((st = check_scores(a.sm_scale, a.softcap, a.slopes))) return st;
   // row blocks and pieces, a multiple of eight of them (one XCD's each), and the join's four rows a workgroup
   const int64_t rows = (int64_t)a.T * a.G, pairs = (int64_t)a.B * a.Hkv;
   const int64_t blocks = (rows + plan.rb * 32 - 1) / (plan.rb * 32) * ((pairs * plan.splits + 7) / 8 * 8);
@@ -924,6 +929,231 @@ int bpc_tree_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq
   attn_workspace(a, plan, workspace);
   hipError_t e = launch_attn(a, plan);
   if (e != hipSuccess) return hip_fail(e, "bpc_tree_attention launch");
+  return BPC_OK;
+}
+
+// fp32 rows [B, H][len], the innermost dimension contiguous
+static int check_floats(const char* name, const void* p, int64_t sb, int64_t sh) {
+  if (!p) return fail(BPC_EINVAL, "%s is NULL", name);
+  if (sb < 0 || sh < 0) return fail(BPC_EINVAL, "%s strides must be >= 0", name);
+  if (!aligned4(p)) return fail(BPC_EALIGN, "%s must be 4-byte aligned", name);
+  return BPC_OK;
+}
+
+// that are written: no two in the same place
+static int check_floats_apart(const char* name, int64_t sb, int64_t sh, int B, int H, int64_t len) {
+  const bool heads_inside = sh <= sb;
+  const int64_t in = heads_inside ? sh : sb, out = heads_inside ? sb : sh;
+  const int in_n = heads_inside ? H : B, out_n = heads_inside ? B : H;
+  if (out > INT64_MAX / 4 / std::max(B, H)) return fail(BPC_EINVAL, "%s: strides (%lld, %lld)", name, (long long)sb, (long long)sh);
+  if ((in_n > 1 && in < len) || (out_n > 1 && out < (in_n > 1 ? in * (in_n - 1) : 0) + len))
+    return fail(BPC_EINVAL, "%s: written rows must not overlap, strides (%lld, %lld)", name, (long long)sb, (long long)sh);
+  return BPC_OK;
+}
+
+static int check_window(int window, int sinks) {
+  if (window < 0 || sinks < 0) return fail(BPC_EINVAL, "window=%d and sinks=%d must be >= 0", window, sinks);
+  return BPC_OK;
+}
+constexpr int kMaxWindow = 1 << 30;  // slots are below it
+
+// a page table, or none
+static int check_table(AttnArgs& a, const int32_t* block_table, int64_t st_b, int num_pages, int page_size) {
+  if (!block_table) return BPC_OK;
+  int st;
+  if ((st = check_int32("block_table", block_table, st_b))) return st;
+  const int shift = page_shift(page_size);
+  if (shift < 0) return fail(BPC_EINVAL, "page_size=%d must be a power of two, 16 to 2^20", page_size);
+  if (num_pages < 1) return fail(BPC_EINVAL, "num_pages=%d must be >= 1", num_pages);
+  a.table = block_table, a.st_b = st_b, a.num_pages = num_pages, a.page_shift = shift;
+  return BPC_OK;
+}
+
+size_t bpc_chunk_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D, int window, int sinks) {
+  if (window < 0 || sinks < 0 || !attn_sizes_ok(B, Hq, Hkv, T, N, D)) return 0;
+  return chunk_plan(B, Hkv, Hq / Hkv, T, N, std::min(window, kMaxWindow), std::min(sinks, kMaxWindow)).total;
+}
+
+int bpc_chunk_cut(int B, int Hq, int Hkv, int T, int N, int D, int window, int sinks, int* row_blocks, int* pieces, int* streamed) {
+  g_last_error[0] = 0;
+  int st;
+  if ((st = check_attn_sizes(B, Hq, Hkv, T, N, D))) return st;
+  if ((st = check_window(window, sinks))) return st;
+  if (!row_blocks || !pieces || !streamed) return fail(BPC_EINVAL, "row_blocks, pieces and streamed must not be NULL");
+  const AttnPlan plan = chunk_plan(B, Hkv, Hq / Hkv, T, N, std::min(window, kMaxWindow), std::min(sinks, kMaxWindow));
+  *row_blocks = plan.rb, *pieces = plan.splits, *streamed = plan.once;
+  return BPC_OK;
+}
+
+int bpc_chunk_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t, const uint16_t* K, int64_t sK_b,
+                        int64_t sK_h, int64_t sK_n, const uint16_t* V, int64_t sV_b, int64_t sV_h, int64_t sV_n,
+                        const int32_t* block_table, int64_t st_b, int num_pages, int page_size, const int32_t* pos,
+                        const int32_t* count, int B, int Hq, int Hkv, int T, int N, int D, float sm_scale,
+                        float softcap, const float* slopes, int window, int sinks, uint16_t* out, int64_t so_b,
+                        int64_t so_h, int64_t so_t, float* lse, int64_t sl_b, int64_t sl_h, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  g_last_error[0] = 0;
+  int st;
+  if ((st = check_attn_sizes(B, Hq, Hkv, T, N, D))) return st;
+  if ((st = check_window(window, sinks))) return st;
+  AttnArgs a{};
+  a.q = q, a.sq_b = sq_b, a.sq_h = sq_h, a.sq_t = sq_t;
+  a.K = K, a.sK_b = sK_b, a.sK_h = sK_h, a.sK_n = sK_n;
+  a.V = V, a.sV_b = sV_b, a.sV_h = sV_h, a.sV_n = sV_n;
+  a.B = B, a.Hkv = Hkv, a.G = Hq / Hkv, a.T = T, a.N = N;
+  a.lens = pos, a.count = count;
+  a.window = std::min(window, kMaxWindow), a.sinks = window ? std::min(sinks, kMaxWindow) : 0;
+  a.sm_scale = sm_scale, a.softcap = softcap, a.slopes = slopes;
+  a.out = out, a.so_b = so_b, a.so_h = so_h, a.so_t = so_t;
+  a.lse = lse, a.sl_b = sl_b, a.sl_h = sl_h;
+  a.stream = static_cast<hipStream_t>(stream);
+  const AttnPlan plan = chunk_plan(B, Hkv, a.G, T, N, a.window, a.sinks);
+  if ((st = check_attn(a, Hq, D, plan, workspace, workspace_bytes))) return st;
+  if ((st = check_int32("pos", pos, 0))) return st;
+  if (count && (st = check_int32("count", count, 0))) return st;
+  if ((st = check_table(a, block_table, st_b, num_pages, page_size))) return st;
+  if ((st = check_apart("out", so_b, so_h, so_t, B, Hq, T))) return st;
+  if (lse && (st = check_floats("lse", lse, sl_b, sl_h))) return st;
+  if (lse && (st = check_floats_apart("lse", sl_b, sl_h, B, Hq, T))) return st;
+  attn_workspace(a, plan, workspace);
+  if (plan.total) a.part_e = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.off_e);
+  hipError_t e = launch_chunk(a, plan);
+  if (e != hipSuccess) return hip_fail(e, "bpc_chunk_attention launch");
+  return BPC_OK;
+}
+
+int bpc_key_weights(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t, const uint16_t* K, int64_t sK_b,
+                    int64_t sK_h, int64_t sK_n, const float* lse, int64_t sl_b, int64_t sl_h, float* weights,
+                    int64_t sw_b, int64_t sw_h, const int32_t* block_table, int64_t st_b, int num_pages, int page_size,
+                    const int32_t* pos, const int32_t* count, int B, int Hq, int Hkv, int T, int N, int D,
+                    float sm_scale, float softcap, const float* slopes, int window, int sinks, float decay,
+                    void* stream) {
+  g_last_error[0] = 0;
+  int st;
+  if ((st = check_attn_sizes(B, Hq, Hkv, T, N, D))) return st;
+  if ((st = check_window(window, sinks))) return st;
+  if ((st = check_rows("q", q, sq_b, sq_h, sq_t))) return st;
+  if ((st = check_kv("K", K, sK_b, sK_h, sK_n))) return st;
+  if ((st = check_scores(sm_scale, softcap, slopes))) return st;
+  if (!(decay >= 0.0f) || !__builtin_isfinite(decay)) return fail(BPC_EINVAL, "decay must be finite and >= 0");
+  if ((st = check_floats("lse", lse, sl_b, sl_h))) return st;
+  if ((st = check_floats("weights", weights, sw_b, sw_h))) return st;
+  if ((st = check_floats_apart("weights", sw_b, sw_h, B, Hkv, N))) return st;
+  if ((st = check_int32("pos", pos, 0))) return st;
+  if (count && (st = check_int32("count", count, 0))) return st;
+  AttnArgs pages{};
+  if ((st = check_table(pages, block_table, st_b, num_pages, page_size))) return st;
+  if (!launchable(weights_blocks(B, Hkv, N), 256)) return fail(BPC_EUNSUPPORTED, "B Hkv N: too many slots in one call");
+  WeightArgs a{};
+  a.q = q, a.sq_b = sq_b, a.sq_h = sq_h, a.sq_t = sq_t;
+  a.K = K, a.sK_b = sK_b, a.sK_h = sK_h, a.sK_n = sK_n;
+  a.lse = lse, a.sl_b = sl_b, a.sl_h = sl_h, a.weights = weights, a.sw_b = sw_b, a.sw_h = sw_h;
+  a.table = pages.table, a.st_b = pages.st_b, a.num_pages = pages.num_pages, a.page_shift = pages.page_shift;
+  a.pos = pos, a.count = count, a.B = B, a.Hkv = Hkv, a.G = Hq / Hkv, a.T = T, a.N = N;
+  a.sm_scale = sm_scale, a.softcap = softcap, a.slopes = slopes;
+  a.window = std::min(window, kMaxWindow), a.sinks = window ? std::min(sinks, kMaxWindow) : 0;
+  a.decay = decay, a.stream = static_cast<hipStream_t>(stream);
+  hipError_t e = launch_key_weights(a);
+  if (e != hipSuccess) return hip_fail(e, "bpc_key_weights launch");
+  return BPC_OK;
+}
+
+// addresses that an argument covers
+struct Range {
+  const char* name;
+  const void* p;
+  int64_t bytes;
+};
+static bool ranges_meet(const Range& x, const Range& y) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x.p), b = reinterpret_cast<uintptr_t>(y.p);
+  return x.p && y.p && a < b + (uint64_t)y.bytes && b < a + (uint64_t)x.bytes;
+}
+
+size_t bpc_evict_workspace_bytes(int B, int Hkv, int N, int keep) {
+  (void)B, (void)Hkv, (void)N, (void)keep;
+  return 0;
+}
+
+int bpc_evict_kv(const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n, const uint16_t* V, int64_t sV_b,
+                 int64_t sV_h, int64_t sV_n, const int32_t* block_table, int64_t st_b, int num_pages, int page_size,
+                 const float* weights, int64_t sw_b, int64_t sw_h, const int32_t* lens, int B, int Hkv, int N, int D,
+                 int keep, int sinks, int recent, uint16_t* K_out, int64_t sKo_b, int64_t sKo_h, int64_t sKo_n,
+                 uint16_t* V_out, int64_t sVo_b, int64_t sVo_h, int64_t sVo_n, const int32_t* table_out,
+                 int64_t sto_b, int out_pages, int out_page_size, const uint32_t* codes, int64_t sC_b, int64_t sC_h,
+                 uint32_t* codes_out, int64_t sCo_b, int64_t sCo_h, int W, float* weights_out, int64_t swo_b,
+                 int64_t swo_h, int cap, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error[0] = 0;
+  int st;
+  if ((st = check_sizes(B, Hkv, N))) return st;
+  if ((st = check_head_dim(D))) return st;
+  if (N > (1 << 30) || (int64_t)B * Hkv > (1 << 20)) return fail(BPC_EUNSUPPORTED, "N=%d, B Hkv=%lld: at most 2^30 and 2^20", N, (long long)B * Hkv);
+  if (keep < 1 || keep > N) return fail(BPC_EINVAL, "keep=%d must be in [1, N=%d]", keep, N);
+  if (sinks < 0 || recent < 0 || (int64_t)sinks + recent > keep)
+    return fail(BPC_EINVAL, "sinks=%d and recent=%d must be >= 0, together at most keep=%d", sinks, recent, keep);
+  if ((st = check_kv("K", K, sK_b, sK_h, sK_n))) return st;
+  if ((st = check_kv("V", V, sV_b, sV_h, sV_n))) return st;
+  AttnArgs from{}, to{};
+  if ((st = check_table(from, block_table, st_b, num_pages, page_size))) return st;
+  if ((st = check_table(to, table_out, sto_b, out_pages, out_page_size))) return st;
+  const int out_B = table_out ? out_pages : B, out_N = table_out ? out_page_size : keep;
+  if ((st = check_written("K_out", K_out, sKo_b, sKo_h, sKo_n, out_B, Hkv, out_N))) return st;
+  if ((st = check_written("V_out", V_out, sVo_b, sVo_h, sVo_n, out_B, Hkv, out_N))) return st;
+  if ((st = check_apart("K_out", sKo_b, sKo_h, sKo_n, out_B, Hkv, out_N))) return st;
+  if ((st = check_apart("V_out", sVo_b, sVo_h, sVo_n, out_B, Hkv, out_N))) return st;
+  const int in_B = block_table ? num_pages : B, in_N = block_table ? page_size : N;
+  const RowSet in[2] = {{"K", K, {sK_b, sK_h, sK_n}, {in_B, Hkv, in_N}}, {"V", V, {sV_b, sV_h, sV_n}, {in_B, Hkv, in_N}}};
+  const RowSet out[2] = {{"K_out", K_out, {sKo_b, sKo_h, sKo_n}, {out_B, Hkv, out_N}}, {"V_out", V_out, {sVo_b, sVo_h, sVo_n}, {out_B, Hkv, out_N}}};
+  if ((st = check_separate(out[0], out[1]))) return st;
+  // (the pages read and those written may be of one pool)
+  if (!block_table || !table_out)
+    for (int i = 0; i < 4; ++i)
+      if ((st = check_separate(out[i / 2], in[i % 2]))) return st;
+  if ((st = check_floats("weights", weights, sw_b, sw_h))) return st;
+  if ((st = check_int32("lens", lens, 0))) return st;
+  if ((st = check_int32("kept", kept, 0))) return st;
+  if (weights_out) {
+    if (cap < keep) return fail(BPC_EINVAL, "weights_out: %d columns, needs at least keep=%d", cap, keep);
+    if ((st = check_floats("weights_out", weights_out, swo_b, swo_h))) return st;
+    if ((st = check_floats_apart("weights_out", swo_b, swo_h, B, Hkv, cap))) return st;
+  }
+  if (!codes != !codes_out) return fail(BPC_EINVAL, "codes and codes_out are given together or not at all");
+  if (codes) {
+    if (W != 1 && W != 2 && W != 4) return fail(BPC_EUNSUPPORTED, "W=%d words: 1, 2 or 4", W);
+    if ((st = check_codes("codes", codes, sC_b, sC_h, W))) return st;
+    if ((st = check_codes("codes_out", codes_out, sCo_b, sCo_h, W))) return st;
+    if ((st = check_floats_apart("codes_out", sCo_b, sCo_h, B, Hkv, (int64_t)keep * W))) return st;
+  }
+  auto span = [&](int64_t sb, int64_t sh, int64_t len) { return 4 * (sb * (B - 1) + sh * (Hkv - 1) + len); };
+  const Range read[3] = {{"weights", weights, span(sw_b, sw_h, N)}, {"lens", lens, 4 * (int64_t)B}, {"codes", codes, span(sC_b, sC_h, (int64_t)N * W)}};
+  const Range wrote[3] = {{"kept", kept, 4 * (int64_t)B * Hkv * keep}, {"weights_out", weights_out, span(swo_b, swo_h, cap)},
+                          {"codes_out", codes_out, span(sCo_b, sCo_h, (int64_t)keep * W)}};
+  for (int i = 0; i < 3; ++i) {
+    for (const Range& r : read)
+      if (ranges_meet(wrote[i], r)) return fail(BPC_EINVAL, "%s overlaps %s", wrote[i].name, r.name);
+    for (int j = 0; j < i; ++j)
+      if (ranges_meet(wrote[i], wrote[j])) return fail(BPC_EINVAL, "%s overlaps %s", wrote[i].name, wrote[j].name);
+  }
+  if (!launchable(evict_blocks(B, Hkv, keep), 256) || !launchable((int64_t)B * Hkv, 1024))
+    return fail(BPC_EUNSUPPORTED, "B Hkv keep: too many slots in one call");
+  const size_t need = bpc_evict_workspace_bytes(B, Hkv, N, keep);
+  if (need) {
+    if (!workspace || workspace_bytes < need)
+      return fail(BPC_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : 0, need);
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(BPC_EALIGN, "workspace must be 256-byte aligned");
+  }
+  EvictArgs a{};
+  a.K = K, a.sK_b = sK_b, a.sK_h = sK_h, a.sK_n = sK_n, a.V = V, a.sV_b = sV_b, a.sV_h = sV_h, a.sV_n = sV_n;
+  a.table = from.table, a.st_b = from.st_b, a.num_pages = from.num_pages, a.page_shift = from.page_shift;
+  a.weights = weights, a.sw_b = sw_b, a.sw_h = sw_h, a.lens = lens;
+  a.B = B, a.Hkv = Hkv, a.N = N, a.keep = keep, a.sinks = sinks, a.recent = recent;
+  a.K_out = K_out, a.sKo_b = sKo_b, a.sKo_h = sKo_h, a.sKo_n = sKo_n;
+  a.V_out = V_out, a.sVo_b = sVo_b, a.sVo_h = sVo_h, a.sVo_n = sVo_n;
+  a.table_out = to.table, a.sto_b = to.st_b, a.out_pages = to.num_pages, a.out_shift = to.page_shift;
+  a.codes = codes, a.sC_b = sC_b, a.sC_h = sC_h, a.codes_out = codes_out, a.sCo_b = sCo_b, a.sCo_h = sCo_h, a.W = W;
+  a.weights_out = weights_out, a.swo_b = swo_b, a.swo_h = swo_h, a.cap = weights_out ? cap : 0;
+  a.kept = kept, a.stream = static_cast<hipStream_t>(stream);
+  hipError_t e = launch_evict(a);
+  if (e != hipSuccess) return hip_fail(e, "bpc_evict_kv launch");
   return BPC_OK;
 }
 

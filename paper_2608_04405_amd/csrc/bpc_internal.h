@@ -298,7 +298,7 @@ struct AttnArgs {
   int64_t s_begin;
   const int32_t* key_end;
   int64_t s_end;
-  const int32_t* lens;  // tree attention: cached tokens before the drafts
+  const int32_t* lens;  // tree attention: cached tokens before the drafts; a chunk's first slot
   const uint64_t* tree;
   int64_t s_tree;
   const int32_t* table;
@@ -314,16 +314,86 @@ struct AttnArgs {
   float2* part_ml;  // [B, Hkv, T G][splits] (max, in units of log2 or of the products, and sum), and o[128]
   float* part_o;
   hipStream_t stream;
+  // a chunk: new tokens (NULL: T), slots that a token sees before its own and at the start
+  const int32_t* count;
+  int window, sinks;
+  int rounds;    // pieces go round the XCDs
+  float* lse;    // [B, Hq, T] or NULL
+  int64_t sl_b, sl_h;
+  float* part_e;  // [B, Hkv, T G][splits] sums of unrounded exponentials
 };
 // how a call is cut: 32-row blocks per workgroup, and pieces of the key axis;
 // once: keys and values pass the last-level cache by
 struct AttnPlan {
   int rb, splits;
   bool once;
-  size_t off_ml, off_o, total;
+  size_t off_ml, off_o, off_e, total;
 };
 AttnPlan attn_plan(int B, int Hkv, int G, int T, int N, bool tree);
 hipError_t launch_attn(AttnArgs a, const AttnPlan& p);
+AttnPlan chunk_plan(int B, int Hkv, int G, int T, int N, int window, int sinks);
+hipError_t launch_chunk(AttnArgs a, const AttnPlan& p);
+hipError_t launch_chunk_paged(const AttnArgs& a, const AttnPlan& p);
+
+// ---- what slots gather, and which of them stay ------------------------------
+struct WeightArgs {
+  const uint16_t* q;
+  int64_t sq_b, sq_h, sq_t;
+  const uint16_t* K;  // sK_b: stride of a sequence, or of a page
+  int64_t sK_b, sK_h, sK_n;
+  const float* lse;
+  int64_t sl_b, sl_h;
+  float* weights;
+  int64_t sw_b, sw_h;
+  const int32_t* table;
+  int64_t st_b;
+  int num_pages, page_shift;
+  const int32_t* pos;
+  const int32_t* count;
+  int B, Hkv, G, T, N;
+  float sm_scale, softcap;
+  const float* slopes;
+  int window, sinks;
+  float decay;
+  FastDiv div_G, div_Hkv, div_blocks;
+  int blocks, rounds;  // key blocks of a (b, h); whether (b, h) go round the XCDs
+  hipStream_t stream;
+};
+int64_t weights_blocks(int B, int Hkv, int N);  // the most workgroups of a call
+hipError_t launch_key_weights(WeightArgs a);
+
+struct EvictArgs {
+  const uint16_t* K;  // strides as in WeightArgs
+  int64_t sK_b, sK_h, sK_n;
+  const uint16_t* V;
+  int64_t sV_b, sV_h, sV_n;
+  const int32_t* table;
+  int64_t st_b;
+  int num_pages, page_shift;
+  const float* weights;
+  int64_t sw_b, sw_h;
+  const int32_t* lens;
+  int B, Hkv, N, keep, sinks, recent;
+  uint16_t* K_out;
+  int64_t sKo_b, sKo_h, sKo_n;
+  uint16_t* V_out;
+  int64_t sVo_b, sVo_h, sVo_n;
+  const int32_t* table_out;
+  int64_t sto_b;
+  int out_pages, out_shift;
+  const uint32_t* codes;
+  int64_t sC_b, sC_h;
+  uint32_t* codes_out;
+  int64_t sCo_b, sCo_h;
+  int W;
+  float* weights_out;
+  int64_t swo_b, swo_h;
+  int cap;
+  int32_t* kept;
+  hipStream_t stream;
+};
+int64_t evict_blocks(int B, int Hkv, int keep);
+hipError_t launch_evict(const EvictArgs& a);
 
 struct BuildArgs {
   const uint16_t* K;
