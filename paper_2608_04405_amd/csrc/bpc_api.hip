@@ -1070,8 +1070,7 @@ static bool ranges_meet(const Range& x, const Range& y) {
 }
 
 size_t bpc_evict_workspace_bytes(int B, int Hkv, int N, int keep) {
-  (void)B, (void)Hkv, (void)N, (void)keep;
-  return 0;
+  return B >= 1 && Hkv >= 1 && N >= 1 && keep >= 1 && keep <= N && N <= (1 << 30) && (int64_t)B * Hkv <= (1 << 20) ? evict_workspace(B, Hkv, N) : 0;
 }
 
 int bpc_evict_kv(const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n, const uint16_t* V, int64_t sV_b,
@@ -1133,7 +1132,7 @@ int bpc_evict_kv(const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n, co
     for (int j = 0; j < i; ++j)
       if (ranges_meet(wrote[i], wrote[j])) return fail(BPC_EINVAL, "%s overlaps %s", wrote[i].name, wrote[j].name);
   }
-  if (!launchable(evict_blocks(B, Hkv, keep), 256) || !launchable((int64_t)B * Hkv, 1024))
+  if (!launchable(evict_blocks(B, Hkv, keep), 256) || !launchable((int64_t)B * Hkv * evict_segments(N), 1024))
     return fail(BPC_EUNSUPPORTED, "B Hkv keep: too many slots in one call");
   const size_t need = bpc_evict_workspace_bytes(B, Hkv, N, keep);
   if (need) {
@@ -1151,7 +1150,7 @@ int bpc_evict_kv(const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n, co
   a.table_out = to.table, a.sto_b = to.st_b, a.out_pages = to.num_pages, a.out_shift = to.page_shift;
   a.codes = codes, a.sC_b = sC_b, a.sC_h = sC_h, a.codes_out = codes_out, a.sCo_b = sCo_b, a.sCo_h = sCo_h, a.W = W;
   a.weights_out = weights_out, a.swo_b = swo_b, a.swo_h = swo_h, a.cap = weights_out ? cap : 0;
-  a.kept = kept, a.stream = static_cast<hipStream_t>(stream);
+  a.kept = kept, a.counts = static_cast<uint32_t*>(workspace), a.stream = static_cast<hipStream_t>(stream);
   hipError_t e = launch_evict(a);
   if (e != hipSuccess) return hip_fail(e, "bpc_evict_kv launch");
   return BPC_OK;

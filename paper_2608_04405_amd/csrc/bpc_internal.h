@@ -390,10 +390,14 @@ struct EvictArgs {
   int64_t swo_b, swo_h;
   int cap;
   int32_t* kept;
+  uint32_t* counts;  // [B, Hkv][segs] digits' counts of a segment of slots, and its state
+  int segs;
   hipStream_t stream;
 };
 int64_t evict_blocks(int B, int Hkv, int keep);
-hipError_t launch_evict(const EvictArgs& a);
+int evict_segments(int N);
+size_t evict_workspace(int B, int Hkv, int N);
+hipError_t launch_evict(EvictArgs a);
 
 struct BuildArgs {
   const uint16_t* K;

@@ -5,12 +5,27 @@
 // largest weights between them, found by a radix select over an order key of the
 // float (11, 11 and 10 bits, most significant first; a NaN lies below all, both
 // zeros are one).  Ties go to the lowest slot.
+//
+// A workgroup holds a segment of 16384 slots' weights in registers, 16 a thread,
+// and counts its keys' digits in LDS.  Up to one segment it finds all three digits
+// and writes the slots by itself; else there is a launch for each digit, whose
+// workgroups all add up what the one before counted, in the order of the segments,
+// so that each knows how many slots before its own stay as well.  Weights of a
+// kind have few exponents, so the first digit's counters are few: four of each,
+// in neighbouring banks, for every fourth lane.
 #include "bpc_internal.h"
 
 namespace bpc {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectBins = 2048;
+constexpr int kSelectRounds = 16;
+constexpr int kSegSlots = kSelectRounds * kSelectThreads;
+constexpr int kCopies = 4;  // of each counter
+// workspace of a segment: three digits' counts, then its state
+constexpr int kSegWords = 3 * kSelectBins + 4;
 
 __device__ __forceinline__ uint32_t weight_key(float w) {
   if (w != w) return 0u;
@@ -18,132 +33,254 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
-  __shared__ uint32_t hist[kSelectBins];
-  __shared__ int wave_tot[kSelectThreads / 64];
-  __shared__ int found[2];
-  const int bh = blockIdx.x, b = bh / a.Hkv, h = bh - b * a.Hkv, t = threadIdx.x;
+// ONE: all of it; else launch `pass` of four: it settles digit pass - 1, then
+// counts digit `pass`, or (the last) writes the slots that stay.
+template <bool ONE, int ROUNDS>
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a, int pass) {
+  constexpr int NW = kSelectThreads / 64;
+  __shared__ uint32_t hist[kSelectBins * kCopies];
+  __shared__ int wave_tot[NW];
+  __shared__ int found[4];
+  __shared__ int2 wave_cnt[NW];
+  const int segs = ONE ? 1 : a.segs;
+  const int bh = ONE ? (int)blockIdx.x : (int)(blockIdx.x / (uint32_t)segs), seg = ONE ? 0 : (int)blockIdx.x - bh * segs;
+  const int b = bh / a.Hkv, h = bh - b * a.Hkv, t = threadIdx.x;
+  const int lane = t & 63, wid = __builtin_amdgcn_readfirstlane(t >> 6);
   const int n = a.lens[b];
   if (n < 0 || n > a.N) return;
   const float* w = a.weights + b * a.sw_b + h * a.sw_h;
+  const int stay = min(n, a.keep);
+  const bool all = n <= a.keep;
+  const int lo = all ? n : a.sinks, hi = all ? n : n - a.recent;  // the slots between are chosen from
+  const int m = all ? 0 : a.keep - a.sinks - a.recent;
+  if (!ONE && pass < 3 && m == 0) return;
+  const int slot0 = seg * kSegSlots + wid * (ROUNDS * 64) + lane;
+
+  float x[ROUNDS];
+#pragma unroll
+  for (int j = 0; j < ROUNDS; ++j) {
+    const int i = slot0 + 64 * j;
+    x[j] = i < n ? w[i] : 0.f;
+  }
+
+  auto shift_of = [](int p) { return p == 0 ? 21 : p == 1 ? 10 : 0; };
+  auto mask_of = [](int p) { return p == 2 ? 1023u : 2047u; };
+  uint32_t prefix = 0u, pmask = 0u;
+  int need = m;      // slots of the key looked for and below, within the prefix
+  int before = 0, ties = 0;  // slots of earlier segments above the prefix, and equal to the key
+  uint32_t* counts = ONE ? nullptr : a.counts + ((int64_t)bh * segs) * kSegWords;
+  uint32_t* state = ONE ? nullptr : counts + (int64_t)seg * kSegWords + 3 * kSelectBins;
+
+  auto count = [&](int p) {
+    const int shift = shift_of(p);
+    const uint32_t mask = mask_of(p);
+    uint4* zero = reinterpret_cast<uint4*>(hist);
+#pragma unroll
+    for (int i = 0; i < kSelectBins * kCopies / 4 / kSelectThreads; ++i) zero[t + i * kSelectThreads] = make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < ROUNDS; ++j) {
+      const int i = slot0 + 64 * j;
+      const uint32_t k = weight_key(x[j]);
+      if (i >= lo && i < hi && (k & pmask) == prefix)
+        atomicAdd(&hist[((k >> shift) & mask) * kCopies + (lane & (kCopies - 1))], 1u);
+    }
+    __syncthreads();
+  };
+  // thread t's counters: the bins 2047 - 2t and 2046 - 2t
+  auto counted = [&](int bin) {
+    const uint4 c = *reinterpret_cast<const uint4*>(&hist[bin * kCopies]);
+    return (int)(c.x + c.y + c.z + c.w);
+  };
+  const int bin_top = kSelectBins - 1 - 2 * t, bin_low = bin_top - 1;
+  // digit p: the one in which the `need`th largest key lies
+  auto settle = [&](int p) {
+    int top = 0, low = 0, pre_top = 0, pre_low = 0;
+    if (ONE) {
+      top = counted(bin_top), low = counted(bin_low);
+    } else {
+      const uint32_t* c = counts + p * kSelectBins + bin_low;
+#pragma unroll 8
+      for (int s = 0; s < segs; ++s) {
+        const uint2 v = *reinterpret_cast<const uint2*>(c + (int64_t)s * kSegWords);
+        if (s < seg) pre_top += (int)v.y, pre_low += (int)v.x;
+        top += (int)v.y, low += (int)v.x;
+      }
+    }
+    if (t < 4) found[t] = 0;
+    int total;
+    const int above_top = block_exclusive_scan<kSelectThreads>(top + low, wave_tot, total), above_low = above_top + top;
+    if (above_top < need && need <= above_top + top) found[0] = bin_top, found[1] = above_top, found[3] = pre_top;
+    if (above_low < need && need <= above_low + low) found[0] = bin_low, found[1] = above_low, found[3] = pre_low;
+    __syncthreads();
+    const int digit = found[0];
+    if (!ONE) {
+      int pre = (bin_top > digit ? pre_top : 0) + (bin_low > digit ? pre_low : 0);
+#pragma unroll
+      for (int o = 32; o; o >>= 1) pre += __shfl_xor(pre, o, 64);
+      if (lane == 0 && pre) atomicAdd(&found[2], pre);
+      __syncthreads();
+      before += found[2], ties = found[3];
+    }
+    prefix |= (uint32_t)digit << shift_of(p);
+    pmask |= mask_of(p) << shift_of(p);
+    need -= found[1];
+    __syncthreads();
+  };
+
+  if (m > 0) {
+    if (ONE) {
+#pragma unroll 1
+      for (int p = 0; p < 3; ++p) {
+        count(p);
+        settle(p);
+      }
+    } else {
+      if (pass > 1) {
+        prefix = state[0], need = (int)state[1], before = (int)state[2];
+        pmask = ~0u << shift_of(pass - 2);
+      }
+      if (pass > 0) settle(pass - 1);
+      if (pass < 3) {
+        count(pass);
+        *reinterpret_cast<uint2*>(counts + (int64_t)seg * kSegWords + pass * kSelectBins + bin_low) =
+            make_uint2((uint32_t)counted(bin_low), (uint32_t)counted(bin_top));
+        if (t == 0) state[0] = prefix, state[1] = (uint32_t)need, state[2] = (uint32_t)before;
+        return;
+      }
+    }
+  }
+
+  // ---- the slots that stay, in order: `need` of those equal to the key ---------
   int32_t* kept = a.kept + (int64_t)bh * a.keep;
   float* wo = a.weights_out ? a.weights_out + b * a.swo_b + h * a.swo_h : nullptr;
-  const int stay = min(n, a.keep);
-  for (int i = stay + t; i < a.keep; i += kSelectThreads) kept[i] = -1;
+  for (int64_t i = stay + seg * kSelectThreads + t; i < a.keep; i += segs * kSelectThreads) kept[i] = -1;
   if (wo)
-    for (int i = stay + t; i < a.cap; i += kSelectThreads) wo[i] = 0.f;
-  if (n <= a.keep) {
-    for (int i = t; i < n; i += kSelectThreads) {
-      kept[i] = i;
-      if (wo) wo[i] = w[i];
-    }
-    return;
-  }
-  const int lo = a.sinks, hi = n - a.recent;
-  const int m = a.keep - a.sinks - a.recent;  // of [lo, hi), which has more
-  uint32_t prefix = 0u, pmask = 0u;
-  int need = m;
-  constexpr int kShift[3] = {21, 10, 0}, kBits[3] = {11, 11, 10};
+    for (int64_t i = stay + seg * kSelectThreads + t; i < a.cap; i += segs * kSelectThreads) wo[i] = 0.f;
+  int above = 0, equal = 0;  // in this wavefront
   if (m > 0) {
 #pragma unroll
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = kShift[pass];
-      const uint32_t dmask = (1u << kBits[pass]) - 1u;
-      hist[2 * t] = 0u, hist[2 * t + 1] = 0u;
-      __syncthreads();
-      for (int i = lo + t; i < hi; i += kSelectThreads) {
-        const uint32_t k = weight_key(w[i]);
-        if ((k & pmask) == prefix) atomicAdd(&hist[(k >> shift) & dmask], 1u);
-      }
-      __syncthreads();
-      // thread t holds bins 2047 - 2t and 2046 - 2t: the scan counts the bins above
-      const int top = (int)hist[kSelectBins - 1 - 2 * t], low = (int)hist[kSelectBins - 2 - 2 * t];
-      int total;
-      const int above_top = block_exclusive_scan<kSelectThreads>(top + low, wave_tot, total), above_low = above_top + top;
-      if (above_top < need && need <= above_top + top) found[0] = kSelectBins - 1 - 2 * t, found[1] = above_top;
-      if (above_low < need && need <= above_low + low) found[0] = kSelectBins - 2 - 2 * t, found[1] = above_low;
-      __syncthreads();
-      prefix |= (uint32_t)found[0] << shift;
-      pmask |= dmask << shift;
-      need -= found[1];
-      __syncthreads();
+    for (int j = 0; j < ROUNDS; ++j) {
+      const int i = slot0 + 64 * j;
+      const bool in = i >= lo && i < hi;
+      const uint32_t k = weight_key(x[j]);
+      above += __popcll(__ballot(in && k > prefix)), equal += __popcll(__ballot(in && k == prefix));
+    }
+    if (lane == 0) wave_cnt[wid] = make_int2(above, equal);
+    __syncthreads();
+    above = before, equal = ties;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      const int2 c = wave_cnt[v];
+      if (v < wid) above += c.x, equal += c.y;
     }
   }
-  // `need` slots of weight `prefix`, the lowest first, and all above it
-  int written = 0, ties = 0;
-  for (int c0 = 0; c0 < n; c0 += kSelectThreads) {
-    const int i = c0 + t;
-    const bool inside = i < n, middle = i >= lo && i < hi;
-    const float x = inside ? w[i] : 0.f;
-    const uint32_t k = weight_key(x);
-    const bool tie = m > 0 && inside && middle && k == prefix;
-    const bool sure = inside && (!middle || (m > 0 && k > prefix));
-    int tot;
-    const int pre = block_exclusive_scan<kSelectThreads>(((int)tie << 16) | (int)sure, wave_tot, tot);
-    const int rank_tie = ties + (pre >> 16);
-    const int rank = written + (pre & 0xFFFF) + min(rank_tie, need) - min(ties, need);
-    if (sure || (tie && rank_tie < need)) {
-      kept[rank] = i;
-      if (wo) wo[rank] = x;
+#pragma unroll
+  for (int j = 0; j < ROUNDS; ++j) {
+    const int i = slot0 + 64 * j;
+    bool mine = i < n && (i < lo || i >= hi);
+    int rank = i < lo ? i : a.keep - (n - i);
+    if (m > 0) {
+      const bool in = i >= lo && i < hi;
+      const uint32_t k = weight_key(x[j]);
+      const bool more = in && k > prefix, same = in && k == prefix;
+      const uint64_t mb = __ballot(more), sb = __ballot(same);
+      const int a0 = above + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mb >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mb, 0u));
+      const int e0 = equal + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(sb >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)sb, 0u));
+      if (more || (same && e0 < need)) mine = true, rank = lo + a0 + min(e0, need);
+      above += __popcll(mb), equal += __popcll(sb);
     }
-    written += (tot & 0xFFFF) + min(ties + (tot >> 16), need) - min(ties, need);
-    ties += tot >> 16;
+    if (mine) {
+      kept[rank] = i;
+      if (wo) wo[rank] = x[j];
+    }
   }
 }
 
-// A wavefront copies rows four at a time, 16 lanes a row.
-constexpr int kCopyRows = 16;  // of a wavefront
+// The rows that stay.  A wavefront moves 16 of each tensor, 16 lanes a row, all
+// under way at once; the 16 rows written lie in one page.
+constexpr int kCopyRows = 16;
 int64_t evict_blocks(int B, int Hkv, int keep) { return (int64_t)B * Hkv * ((keep + 4 * kCopyRows - 1) / (4 * kCopyRows)); }
+
 __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs a) {
   const int blocks = (a.keep + 4 * kCopyRows - 1) / (4 * kCopyRows);
-  const int bh = blockIdx.x / blocks, block = blockIdx.x - bh * blocks, b = bh / a.Hkv, h = bh - b * a.Hkv;
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+  const int bh = (int)(blockIdx.x / (uint32_t)blocks), block = (int)blockIdx.x - bh * blocks, b = bh / a.Hkv, h = bh - b * a.Hkv;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = a.lens[b];
-  if (n < 0 || n > a.N) return;
-  const int stay = min(n, a.keep);
-  const int base = (block * 4 + wid) * kCopyRows;
-  const int part = lane & 15, pmask = (1 << a.page_shift) - 1, omask = (1 << a.out_shift) - 1;
+  const int stay = min(n, a.keep), base = (block * 4 + wid) * kCopyRows;
+  if (n < 0 || n > a.N || base >= stay) return;
+  const int part = lane & 15, row0 = base + (lane >> 4);
   const int32_t* kept = a.kept + (int64_t)bh * a.keep;
-  uint4 kr[kCopyRows / 4], vr[kCopyRows / 4];
-  bool on[kCopyRows / 4];
+  constexpr int R = kCopyRows / 4;
+  int slot[R];
 #pragma unroll
-  for (int i = 0; i < kCopyRows / 4; ++i) {
-    const int row = base + 4 * i + (lane >> 4);
-    on[i] = row < stay;
-    if (!on[i]) continue;
-    const int s = kept[row];
-    int64_t page = b, at = s;
-    if (a.table) {
-      page = a.table[b * a.st_b + (s >> a.page_shift)], at = s & pmask;
-      if ((uint64_t)page >= (uint64_t)a.num_pages) on[i] = false;
-    }
-    if (on[i]) {
-      kr[i] = *reinterpret_cast<const uint4*>(a.K + page * a.sK_b + h * a.sK_h + at * a.sK_n + 8 * part);
-      vr[i] = *reinterpret_cast<const uint4*>(a.V + page * a.sV_b + h * a.sV_h + at * a.sV_n + 8 * part);
-    }
-    if (a.codes && part < a.W)
-      a.codes_out[b * a.sCo_b + h * a.sCo_h + (int64_t)row * a.W + part] = a.codes[b * a.sC_b + h * a.sC_h + (int64_t)s * a.W + part];
+  for (int i = 0; i < R; ++i) slot[i] = kept[min(row0 + 4 * i, stay - 1)];
+  int64_t page_out = b, at_out = row0;
+  bool room = true;
+  if (a.table_out) {
+    page_out = a.table_out[b * a.sto_b + (base >> a.out_shift)], at_out = row0 & ((1 << a.out_shift) - 1);
+    room = (uint64_t)page_out < (uint64_t)a.out_pages;
+    if (!room) page_out = 0;
   }
+  int64_t page[R], at[R];
+  bool on[R];
 #pragma unroll
-  for (int i = 0; i < kCopyRows / 4; ++i) {
-    const int row = base + 4 * i + (lane >> 4);
-    if (!on[i]) continue;
-    int64_t page = b, at = row;
-    if (a.table_out) {
-      page = a.table_out[b * a.sto_b + (row >> a.out_shift)], at = row & omask;
-      if ((uint64_t)page >= (uint64_t)a.out_pages) continue;
+  for (int i = 0; i < R; ++i) {
+    page[i] = b, at[i] = slot[i];
+    on[i] = room && row0 + 4 * i < stay;
+  }
+  if (a.table) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) page[i] = a.table[b * a.st_b + (slot[i] >> a.page_shift)];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      at[i] = slot[i] & ((1 << a.page_shift) - 1);
+      const bool there = (uint64_t)page[i] < (uint64_t)a.num_pages;
+      on[i] = on[i] && there, page[i] = there ? page[i] : 0;
     }
-    *reinterpret_cast<uint4*>(a.K_out + page * a.sKo_b + h * a.sKo_h + at * a.sKo_n + 8 * part) = kr[i];
-    *reinterpret_cast<uint4*>(a.V_out + page * a.sVo_b + h * a.sVo_h + at * a.sVo_n + 8 * part) = vr[i];
+  }
+  u32x4 kr[R], vr[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) kr[i] = *reinterpret_cast<const u32x4*>(a.K + page[i] * a.sK_b + h * a.sK_h + at[i] * a.sK_n + 8 * part);
+#pragma unroll
+  for (int i = 0; i < R; ++i) vr[i] = *reinterpret_cast<const u32x4*>(a.V + page[i] * a.sV_b + h * a.sV_h + at[i] * a.sV_n + 8 * part);
+  if (a.codes && part < a.W) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (row0 + 4 * i < stay)
+        a.codes_out[b * a.sCo_b + h * a.sCo_h + (int64_t)(row0 + 4 * i) * a.W + part] = a.codes[b * a.sC_b + h * a.sC_h + (int64_t)slot[i] * a.W + part];
+    }
+  }
+  uint16_t* ko = a.K_out + page_out * a.sKo_b + h * a.sKo_h + at_out * a.sKo_n + 8 * part;
+  uint16_t* vo = a.V_out + page_out * a.sVo_b + h * a.sVo_h + at_out * a.sVo_n + 8 * part;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (on[i]) {
+      *reinterpret_cast<u32x4*>(ko + 4 * i * a.sKo_n) = kr[i];
+      *reinterpret_cast<u32x4*>(vo + 4 * i * a.sVo_n) = vr[i];
+    }
   }
 }
 
-hipError_t launch_evict(const EvictArgs& a) {
+int evict_segments(int N) { return (N + kSegSlots - 1) / kSegSlots; }
+
+size_t evict_workspace(int B, int Hkv, int N) {
+  const int segs = evict_segments(N);
+  return segs == 1 ? 0 : (size_t)B * Hkv * segs * kSegWords * sizeof(uint32_t);
+}
+
+hipError_t launch_evict(EvictArgs a) {
   const int bh = a.B * a.Hkv;
-  evict_select_kernel<<<bh, kSelectThreads, 0, a.stream>>>(a);
+  a.segs = evict_segments(a.N);
+  if (a.segs == 1) {
+    auto* f = a.N <= 4 * kSelectThreads ? evict_select_kernel<true, 4> : evict_select_kernel<true, kSelectRounds>;
+    f<<<bh, kSelectThreads, 0, a.stream>>>(a, 0);
+  } else {
+    for (int pass = 0; pass < 4; ++pass) evict_select_kernel<false, kSelectRounds><<<bh * a.segs, kSelectThreads, 0, a.stream>>>(a, pass);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  evict_copy_kernel<<<bh * ((a.keep + 4 * kCopyRows - 1) / (4 * kCopyRows)), 256, 0, a.stream>>>(a);
+  evict_copy_kernel<<<(unsigned)evict_blocks(a.B, a.Hkv, a.keep), 256, 0, a.stream>>>(a);
   return hipGetLastError();
 }
 
