@@ -179,6 +179,25 @@ __device__ __forceinline__ int chunk_tokens(const Args& a, int b, int first) {
   return first < 0 || first > a.N - n ? 0 : n;
 }
 
+// The slots that rows row0 .. row0 + span - 1 of a chunk's `rows` see, in tiles of
+// `keys`: all tiles up to slot `end`, but that those from the `near`th on are `gap`
+// further on, past slots that lie behind the first ones and before every window.
+struct ChunkSlots {
+  int p0, p1, end, near, gap, tiles;
+};
+template <typename Args>
+__device__ __forceinline__ ChunkSlots chunk_slots(const Args& a, const FastDiv& div_G, int first, int rows, int row0, int span, int keys) {
+  ChunkSlots s;
+  s.p0 = first + div_G.quotient(row0), s.p1 = first + div_G.quotient(min(rows, row0 + span) - 1);
+  s.end = s.p1 + 1, s.near = s.gap = 0;
+  if (a.window) {
+    const int lo = max(0, s.p0 - a.window + 1);
+    s.near = (min(a.sinks, lo) + keys - 1) / keys, s.gap = max(0, lo / keys - s.near);
+  }
+  s.tiles = (s.end + keys - 1) / keys - s.gap;
+  return s;
+}
+
 
 template <int KW, int KT>
 struct AttnShape {
@@ -228,8 +247,6 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
   // ---- the keys that any row of the workgroup sees -------------------------
   int klo = 0, khi = 0, len = 0;
   int wg_all_lo = 0, wg_all_hi = 0;  // and those that every row sees
-  // a chunk: tiles from the `near`th on are `gap` further on, past slots that lie
-  // behind the first ones and before every window
   int near = 0, gap = 0;
   if (TREE) {
     len = uniform_load(a.lens + b);
@@ -237,13 +254,9 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
     khi = len + a.T;
     wg_all_hi = len;
   } else if (CHUNK) {
-    const int p0 = first + a.div_G.quotient(wg_row0), p1 = first + a.div_G.quotient(min(rows - 1, wg_row0 + RB * kBlockRows - 1));
-    khi = p1 + 1, wg_all_hi = p0 + 1;
-    if (a.window) {
-      const int lo = max(0, p0 - a.window + 1);
-      wg_all_lo = max(0, p1 - a.window + 1);
-      near = (min(a.sinks, lo) + KT - 1) / KT, gap = max(0, lo / KT - near);
-    }
+    const ChunkSlots s = chunk_slots(a, a.div_G, first, rows, wg_row0, RB * kBlockRows, KT);
+    khi = s.end, wg_all_hi = s.p0 + 1, near = s.near, gap = s.gap;
+    if (a.window) wg_all_lo = max(0, s.p1 - a.window + 1);
   } else {
     const int t0 = a.div_G.quotient(wg_row0), t1 = a.div_G.quotient(min(rows - 1, wg_row0 + RB * kBlockRows - 1));
     int lo = INT32_MAX, hi = 0, all_lo = 0, all_hi = INT32_MAX;
@@ -261,8 +274,12 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
   // ---- tiles of this workgroup ---------------------------------------------
   const int base0 = klo / KT * KT;
   const int total = (khi - base0 - gap * KT + KT * KW - 1) / (KT * KW);
-  const int per = a.div_splits.quotient(total + a.splits - 1);
+  // Pieces of a chunk are of equal length, so that those of short sequences take
+  // no longer than others; a prefill's and a tree's are as many for all rows.
+  const int per = CHUNK ? a.unit : a.div_splits.quotient(total + a.splits - 1);
   const int it0 = split * per, it1 = min(total, it0 + per);
+  if (CHUNK && it0 >= total) return;
+  const bool joined = CHUNK ? total > per : a.splits > 1;  // a second launch joins this row block's pieces
   auto tile_key = [&](int it) {  // first key of a tile
     const int v = it * KW + grp;
     return CHUNK ? (v < near ? v : v + gap) * KT : base0 + v * KT;
@@ -294,9 +311,28 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
 #pragma unroll
     for (int u = 0; u < NP; ++u) pages[u] = (uint32_t)uniform_load(table + (min(n0 + 16 * u, khi - 1) >> a.page_shift));
   };
+  // A chunk's workgroups of several row blocks look up 64 entries at a time, a lane
+  // each, a tile before they are needed: they lie in registers by then, where a
+  // scalar load would be waited for in every tile (2048 tokens over 32768 slots, 32
+  // heads, pages of 64: 1177 -> PAGED us; contiguous 1016).
+  constexpr bool AHEAD = CHUNK && paged && RB > 1;
+  constexpr int kAhead = 64 / NP;  // tiles whose entries a wavefront holds
+  uint32_t entry = 0, next_entry = 0;
+  uint64_t entry_bad = 0;
+  auto fetch_entries = [&](int it) {
+    const int n = min(tile_key(it + lane / NP) + 16 * (lane % NP), khi - 1);
+    next_entry = (uint32_t)table[n >> a.page_shift];
+  };
+  auto take_entries = [&]() {
+    const bool bad = next_entry >= (uint32_t)a.num_pages;
+    entry_bad = __ballot(bad), entry = bad ? 0u : next_entry;
+  };
   auto issue = [&](int it, int buf) {
     const int n0 = tile_key(it) + rbw * RPW;
-    if (paged) {
+    const int held = (it - it0) % kAhead * NP;  // this tile's entries
+    if (AHEAD) {
+      pages_bad = (uint32_t)(entry_bad >> held) & ((1u << NP) - 1u);
+    } else if (paged) {
       pages_bad = 0;
 #pragma unroll
       for (int u = 0; u < NP; ++u) {
@@ -309,9 +345,14 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
       const char *kt, *vt;
       if (paged) {
         static_assert(!paged || RPW % 16 == 0 || 16 % RPW == 0, "a run of a wavefront's rows lies in one page entry");
-        int64_t page = pages[u];
+        int64_t page;
+        if (AHEAD) {
+          page = (uint32_t)__builtin_amdgcn_readlane((int)entry, held + rbw * RPW / 16 + u);
+        } else {
+          page = pages[u];
 #pragma unroll
-        for (int w = 1; w < RB; ++w) page = rbw == w ? pages[(w * RPW) / 16 + u] : page;
+          for (int w = 1; w < RB; ++w) page = rbw == w ? pages[(w * RPW) / 16 + u] : page;
+        }
         kt = Kb + page * a.sK_b * 2 + (nu & pmask) * kstep;
         vt = Vb + page * a.sV_b * 2 + (nu & pmask) * vstep;
       } else {
@@ -339,7 +380,8 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
   };
   constexpr int kCopies = 2 * (RPW / 4);  // copies a wavefront issues per tile
 
-  if (paged && it0 < it1) look_up(it0);
+  if (AHEAD) fetch_entries(it0), take_entries();
+  else if (paged && it0 < it1) look_up(it0);
 
   // ---- this lane's row ------------------------------------------------------
   const int row = wg_row0 + rbw * kBlockRows + col;
@@ -633,7 +675,7 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
     // (pages are looked up where copies are waited for: a scalar load in flight
     // would make every read of LDS wait for it)
     if (RB > 1) {
-      if (paged && it + 1 < it1) look_up(it + 1);
+      if (paged && !AHEAD && it + 1 < it1) look_up(it + 1);
       dma_wait<0>();
     } else if (it + 1 < it1) {  // the other buffer is this wavefront's own: its next tile can be under way already
       issue(it + 1, buf ^ 1);
@@ -655,7 +697,9 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
       // reads the other buffer any more
       __builtin_amdgcn_s_barrier();
       asm volatile("" : : : "memory");
+      if (AHEAD && (it + 1 - it0) % kAhead == 0) take_entries();
       if (it + 1 < it1) issue(it + 1, buf ^ 1);
+      if (AHEAD && (it + 2 - it0) % kAhead == 0) fetch_entries(it + 2);
     }
     asm volatile("" : : : "memory");
     compute(it, buf, bad, partial, odd);
@@ -721,7 +765,7 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
   const int d0 = 8 * CW * (KW > 1 ? grp : 0) + 4 * half;
   const int end_row = (rb * RB + rbw) * kBlockRows + col, end_rows = la->T * la->G;
   if (end_row >= (CHUNK ? rows : end_rows)) return;
-  if (la->splits > 1) {
+  if (joined) {
     const int64_t at = ((int64_t)bh * end_rows + end_row) * la->splits + split;
     if (d0 == 0) la->part_ml[at] = make_float2(mrun, lsum);
     if (LSE && d0 == 0) la->part_e[at] = esum;
@@ -761,11 +805,18 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
     const int len = uniform_load(a.lens + b);
     if (len < 0 || len > a.N - a.T) return;
   }
-  if (CHUNK && t >= chunk_tokens(a, b, uniform_load(a.lens + b))) return;
+  int splits = a.splits;
+  if (CHUNK) {
+    const int first = uniform_load(a.lens + b), tokens = chunk_tokens(a, b, first), span = a.block_rows;
+    if (t >= tokens) return;
+    const ChunkSlots s = chunk_slots(a, a.div_G, first, tokens * a.G, row & -span, span, a.tile_keys);
+    splits = (s.tiles + a.tile_group * a.unit - 1) / (a.tile_group * a.unit);
+    if (splits == 1) return;
+  }
   const float2* ml = a.part_ml + (int64_t)r * a.splits;
   const float* po = a.part_o + (int64_t)r * a.splits * kHeadDim + d;
   float2 mine = make_float2(-INFINITY, 0.f);
-  if (lane < a.splits) mine = ml[lane];
+  if (lane < splits) mine = ml[lane];
   // a split that saw no key of this row has the sum 0, and its o was not written;
   // one whose weight is 0 beside the others' counts, for the NaN it may hold
   const uint64_t seen = __ballot(mine.y != 0.f);
@@ -784,11 +835,11 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
     if (lane == 0) a.lse[b * a.sl_b + (int64_t)(h * a.G + g) * a.sl_h + t] = log_of_sum<false>(mx, e, unit);
   }
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s0 = 0; s0 < a.splits; s0 += 8) {
+  for (int s0 = 0; s0 < splits; s0 += 8) {
     float4 v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      v[i] = *reinterpret_cast<const float4*>(po + (int64_t)min(s0 + 2 * i + half, a.splits - 1) * kHeadDim);
+      v[i] = *reinterpret_cast<const float4*>(po + (int64_t)min(s0 + 2 * i + half, splits - 1) * kHeadDim);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {  // (lanes from `splits` on have seen nothing)
       const float f = __shfl(w, (s0 + 2 * i + half) & 63, 64);

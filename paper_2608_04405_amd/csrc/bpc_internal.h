@@ -318,6 +318,8 @@ struct AttnArgs {
   const int32_t* count;
   int window, sinks;
   int rounds;    // pieces go round the XCDs
+  int unit;      // steps of a piece, of tile_group tiles of tile_keys slots each
+  int tile_keys, tile_group, block_rows;  // rows of a row block (a power of two)
   float* lse;    // [B, Hq, T] or NULL
   int64_t sl_b, sl_h;
   float* part_e;  // [B, Hkv, T G][splits] sums of unrounded exponentials
@@ -326,6 +328,7 @@ struct AttnArgs {
 // once: keys and values pass the last-level cache by
 struct AttnPlan {
   int rb, splits;
+  int unit;  // a chunk's pieces: their steps
   bool once;
   size_t off_ml, off_o, off_e, total;
 };
