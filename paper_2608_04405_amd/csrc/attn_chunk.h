@@ -1,20 +1,548 @@
-// Launches of the attention of a chunk of new tokens, of one kind of cache.
+// Attention of a chunk of new tokens, over one kind of cache: the kernel for many
+// rows, and the launches.
 #pragma once
 #include "attn_kernel.h"
 
 namespace bpc {
 
+// Eight row blocks of 32 rows a workgroup, a wavefront each, two wavefronts a SIMD:
+// tiles, operands and statistics as in attn_kernel, but a wavefront's work on a tile
+// is in two parts, products (O^T += V^T P^T of the tile before, S^T = K Q^T of this
+// one) and softmax, with a barrier behind each, and one half of the wavefronts is
+// one barrier behind the other.  So a SIMD's two wavefronts are never in the same
+// part: one's products run beside the other's exponentials, where attn_kernel's run
+// almost in turn.  A wavefront sends off its share of tile t + 2 at the softmax of t and
+// waits for it at the products of t + 1.  Where wavefronts 0-3 are at the softmax of t,
+// the others are at its products: K of t, V of t - 1 and all from there to t + 2 are in
+// use, so that there are four buffers of V (and of K, where three would do).
+constexpr int kPairRows = 8 * kBlockRows;
+constexpr int kPairKeys = 64;
+constexpr int kPairTile = kPairKeys * kRowBytes;
+#ifndef KLOOK
+#define KLOOK 6
+#endif
+constexpr int kLook = KLOOK;
+constexpr int kPairLds = 8 * kPairTile;
+
+// What a workgroup does: a row block of a piece of the slots of one KV head.
+struct PairItem {
+  int bh, b, h, split, rb;
+};
+template <typename Args>
+__device__ __forceinline__ PairItem pair_item(const Args& a) {
+  const FastDiv by_nrb{a.div_nrb.mul, a.div_nrb.shift}, by_splits{a.div_splits.mul, a.div_splits.shift}, by_Hkv{a.div_Hkv.mul, a.div_Hkv.shift};
+  const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3;
+  PairItem x{-1, 0, 0, 0, 0};
+  int piece;
+  if (a.rounds) {
+    const int round = by_nrb.quotient(turn);
+    x.rb = a.nrb - 1 - (turn - round * a.nrb), piece = round * 8 + xcd;
+    if (piece * a.nrb >= a.items) return x;
+  } else {
+    const int per = (a.items + 7) >> 3, item = xcd * per + turn;
+    if (item >= a.items || turn >= per) return x;
+    piece = by_nrb.quotient(item), x.rb = a.nrb - 1 - (item - piece * a.nrb);
+  }
+  x.bh = by_splits.quotient(piece), x.split = piece - x.bh * a.splits;
+  x.b = by_Hkv.quotient(x.bh), x.h = x.bh - x.b * a.Hkv;
+  return x;
+}
+
+template <bool paged, bool CAP, bool BIAS, bool LSE>
+__global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
+  constexpr int KT = kPairKeys, NB = KT / 32, RPW = KT / 8;
+  extern __shared__ __attribute__((aligned(256))) char pair_tiles[];
+  __shared__ uint64_t odd_rows[4][8];
+  const PairItem item = pair_item(a);
+  if (item.bh < 0) return;
+  const int b = item.b, h = item.h;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool behind = wid >= 4;
+  const int half = lane >> 5, col = lane & 31;
+  const int G = a.G;
+  const int first = uniform_load(a.lens + b);
+  const int rows = chunk_tokens(a, b, first) * G;
+  const int wg_row0 = item.rb * kPairRows;
+  if (wg_row0 >= rows) return;  // these rows stay as they are
+  const ChunkSlots slots = chunk_slots(a, a.div_G, first, rows, wg_row0, kPairRows, KT);
+  const int khi = slots.end, wg_all_hi = slots.p0 + 1, wg_all_lo = a.window ? max(0, slots.p1 - a.window + 1) : 0;
+  const int it0 = item.split * a.unit, it1 = min(slots.tiles, it0 + a.unit);
+  if (it0 >= slots.tiles) return;
+  auto tile_key = [&](int it) { return (it < slots.near ? it : it + slots.gap) * KT; };
+  auto kbuf = [&](int it) { return (uint32_t)((it - it0) & 3) * kPairTile; };
+  auto vbuf = [&](int it) { return (uint32_t)((it - it0) & 3) * kPairTile; };
+
+  const uint32_t ldsK = (uint32_t)(uintptr_t)(lds_char*)pair_tiles, ldsV = ldsK + 4 * kPairTile;
+  const char* Kb = reinterpret_cast<const char*>(a.K + (paged ? 0 : b * a.sK_b) + h * a.sK_h);
+  const char* Vb = reinterpret_cast<const char*>(a.V + (paged ? 0 : b * a.sV_b) + h * a.sV_h);
+  const uint32_t kstep = (uint32_t)a.sK_n * 2, vstep = (uint32_t)a.sV_n * 2;
+  const int64_t kpage = paged ? a.sK_b * 2 : 0, vpage = paged ? a.sV_b * 2 : 0;
+  const uint32_t pmask = (1u << a.page_shift) - 1;
+  const int r4 = lane >> 4;
+  uint32_t chunk[RPW / 4], koff[RPW / 4], voff[RPW / 4];
+#pragma unroll
+  for (int i = 0; i < RPW / 4; ++i) {
+    chunk[i] = (((uint32_t)lane & 15u) ^ swz((uint32_t)(wid * RPW + 4 * i + r4))) * 16;
+    koff[i] = (4 * i + r4) * kstep + chunk[i];
+    voff[i] = (4 * i + r4) * vstep + chunk[i];
+  }
+  // 64 page entries at a time, a lane each, one per 16, 32 or 64 slots: looked up a
+  // tile before they are needed
+  const int per_entry = paged ? min(a.page_shift, 6) : 6;        // (log2 of the slots)
+  const int ahead = 1 << per_entry;                              // tiles whose entries a wavefront holds
+  uint32_t entry = 0, next_entry = 0;
+  uint64_t entry_bad = 0;
+  auto fetch_entries = [&](int it) {
+    const int n = min(tile_key(it + (lane >> (6 - per_entry))) + ((lane << per_entry) & (KT - 1)), khi - 1);
+    const LateArgs la = late_args();
+    next_entry = (uint32_t)la->table[b * la->st_b + (n >> la->page_shift)];
+  };
+  auto take_entries = [&]() {
+    const bool bad = next_entry >= (uint32_t)late_args()->num_pages;
+    entry_bad = __ballot(bad), entry = bad ? 0u : next_entry;
+  };
+  auto entry_of = [&](int it, int n) { return ((it - it0) & (ahead - 1)) << (6 - per_entry) | n >> per_entry; };  // slot n of the tile
+  auto bad_of = [&](int it) {  // a bit per 16 slots
+    uint32_t bad = 0;
+    if (paged && entry_bad) {
+#pragma unroll
+      for (int u = 0; u < KT / 16; ++u) bad |= (uint32_t)(entry_bad >> entry_of(it, 16 * u) & 1) << u;
+    }
+    return bad;
+  };
+  // K and V of tile `it`, whose first slot is n0; FULL: all its slots are below khi
+  auto issue = [&](int it, int n0, auto full) {
+    constexpr bool FULL = decltype(full)::value;
+    const int nu = FULL ? n0 + wid * RPW : min(n0 + wid * RPW, khi - 1);
+    const char *kt, *vt;
+    if (paged) {
+      const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)entry, entry_of(it, wid * RPW));
+      const uint32_t at = (uint32_t)nu & pmask;
+      kt = Kb + (page * kpage + (int64_t)at * kstep);
+      vt = Vb + (page * vpage + (int64_t)at * vstep);
+    } else {
+      kt = Kb + (int64_t)(uint32_t)nu * kstep, vt = Vb + (int64_t)(uint32_t)nu * vstep;
+    }
+    kt = reinterpret_cast<const char*>(uniform64(reinterpret_cast<uint64_t>(kt)));
+    vt = reinterpret_cast<const char*>(uniform64(reinterpret_cast<uint64_t>(vt)));
+    const uint32_t dk = ldsK + kbuf(it) + wid * RPW * kRowBytes, dv = ldsV + vbuf(it) + wid * RPW * kRowBytes;
+    const int last = khi - 1 - nu;  // last row that may be read, from kt and vt on
+    if (FULL || last >= RPW - 1) {
+#pragma unroll
+      for (int i = 0; i < RPW / 4; ++i) {
+        dma16<false>(kt, koff[i], dk + 4 * i * kRowBytes);
+        dma16<false>(vt, voff[i], dv + 4 * i * kRowBytes);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < RPW / 4; ++i) {
+        const uint32_t r = min(4 * i + r4, last);
+        dma16<false>(kt, r * kstep + chunk[i], dk + 4 * i * kRowBytes);
+        dma16<false>(vt, r * vstep + chunk[i], dv + 4 * i * kRowBytes);
+      }
+    }
+  };
+  constexpr std::true_type whole;
+  constexpr std::false_type in_part;
+
+  if (paged) fetch_entries(it0), take_entries();
+
+  // ---- this lane's row ------------------------------------------------------
+  const int row = wg_row0 + wid * kBlockRows + col;
+  const bool live = row < rows;
+  const int t = live ? a.div_G.quotient(row) : 0, g = live ? row - t * G : 0;
+  const int place = first + t;
+  // rows past the last see everything: they never make a tile partial
+  const int lo = !live ? INT32_MIN : a.window ? max(0, place - a.window + 1) : 0, hi = live ? place + 1 : INT32_MAX;
+  const int all_lo = wave_max(lo), all_hi = wave_min(hi);
+  const float slope = BIAS && live ? a.slopes[h * G + g] * (CAP ? kLog2e : 1.f / a.sm_scale) : 0.f;
+  bf16x8 qf[8];
+  {
+    const uint16_t* qp = a.q + b * a.sq_b + (int64_t)(h * G + g) * a.sq_h + (int64_t)t * a.sq_t + 8 * half;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      u32x4 x = live ? *reinterpret_cast<const u32x4*>(qp + 16 * s) : u32x4{0, 0, 0, 0};
+      qf[s] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+  issue(it0, tile_key(it0), in_part);
+  if (it0 + 1 < it1) issue(it0 + 1, tile_key(it0 + 1), in_part);
+#pragma unroll
+  for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
+
+  f32x16 o[4], acc[NB];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+  }
+#pragma unroll
+  for (int k = 0; k < NB; ++k) acc[k] = f32x16{};
+  u32x4 pw[NB][2];
+#pragma unroll
+  for (int k = 0; k < NB; ++k) pw[k][0] = pw[k][1] = u32x4{0, 0, 0, 0};
+  // maximum, what a score has to exceed to move it, reference point (log2), sums
+  float mrun = -INFINITY, limit = -INFINITY, mu = 0.f, lsum = 0.f, esum = 0.f;
+
+  // operand s of a key block lies 2 s chunks on from kaddr, in exclusive or, and that
+  // of 32 coordinates d of V 4 d chunks from vaddr, its second half 2 chunks from its first
+  const uint32_t kaddr = ldsK + col * kRowBytes + (swz(col & 15) ^ half) * 16;
+  const uint32_t i16 = lane & 15, vrow = 4 * half + (i16 >> 2);
+  const uint32_t vaddr = ldsV + vrow * kRowBytes + ((2 * (r4 & 1) + ((i16 & 3) >> 1)) ^ swz(vrow)) * 16 + (i16 & 1) * 8;
+  const float c1 = log2_units<CAP>(a.sm_scale), c8 = 8.f / c1;
+  const float cap2 = a.softcap * kLog2e, capk = CAP ? 2.f * kLog2e * a.sm_scale / a.softcap : 0.f;
+  auto visible = [&](int n, int sinks) { return (n >= lo || n < sinks) && n < hi; };
+
+  // O^T += V^T P^T of the tile whose probabilities are in pw, its first operands read before
+  auto operand_v = [&](uint32_t a0, int k, int s) {
+    const uint32_t at = (32 * k + 16 * s) * kRowBytes;
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lds_read_tr(a0, at), lds_read_tr(a0 ^ 32u, at + 8 * kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  bf16x8 early[4];
+  auto read_early = [&](int it) {
+    const uint32_t v0 = vaddr + vbuf(it);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) early[d] = operand_v(opaque(v0 ^ 64u * d), 0, 0);
+  };
+  auto product_v = [&](int it) {
+    uint32_t va[4];
+    const uint32_t v0 = vaddr + vbuf(it);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) va[d] = opaque(v0 ^ 64u * d);
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, pw[k][s]);
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k || s ? operand_v(va[d], k, s) : early[d], pf, o[d], 0, 0, 0);
+      }
+    }
+  };
+  auto product_k = [&](int it) {
+    uint32_t ka[8];
+    const uint32_t k0 = kaddr + kbuf(it);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ka[i] = opaque(k0 ^ 32u * i);
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, lds_read<u32x4>(ka[s], k * 32 * kRowBytes));
+        acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], s ? acc[k] : f32x16{}, 0, 0, 0);
+      }
+    }
+  };
+  // values of V that clear_odd() took out of tile `it`
+  auto add_odd = [&](int it) {
+    const int n0 = tile_key(it);
+    uint64_t odd = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) odd |= odd_rows[(it - it0) & 3][w];
+    odd = uniform64(odd);
+    while (odd) {
+      const int i = __ffsll((long long)odd) - 1, n = n0 + i;
+      odd &= odd - 1;
+      if (n >= khi) continue;
+      const LateArgs la = late_args();
+      const char* vr = Vb + n * la->sV_n * 2;
+      if (paged) {
+        const uint32_t pg = (uint32_t)uniform_load(la->table + b * la->st_b + (n >> la->page_shift));
+        if (pg >= (uint32_t)la->num_pages) continue;
+        vr = Vb + (pg * la->sV_b + (n & ((1 << la->page_shift) - 1)) * la->sV_n) * 2;
+      }
+      const bool see = visible(n, la->sinks);
+#pragma unroll
+      for (int c = 0; c < 16; ++c) {  // coordinates 8 c + 4 half + 0..3
+        const u32x2 x = *reinterpret_cast<const u32x2*>(vr + 16 * c + 8 * half);
+        const uint32_t w[4] = {x[0] << 16, x[0] & 0xFFFF0000u, x[1] << 16, x[1] & 0xFFFF0000u};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (see && (w[e] & 0x7F800000u) == 0x7F800000u) o[c / 4][4 * (c % 4) + e] += __uint_as_float(w[e]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+
+  auto softmax = [&](int n0, uint32_t bad, bool plain) {
+    // every row sees every key
+    const bool full = plain || ((n0 >= all_lo || n0 + KT <= late_args()->sinks) && n0 + KT <= all_hi && !bad);
+    const int nl = n0 + 4 * half;  // key of score e of block k: nl + 32 k + 8 (e / 4) + e % 4
+    if (CAP || BIAS) {
+      const float ahead = (float)(place - nl);
+#pragma unroll
+      for (int k = 0; k < NB; ++k) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float z = acc[k][e];
+          // in units of log2: cap tanh(x) = cap - 2 cap / (1 + e^2x)
+          if (CAP) z = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * capk)), cap2);
+          if (BIAS) z = fmaf(-slope, fabsf(ahead - (float)(32 * k + 8 * (e / 4) + e % 4)), z);
+          acc[k][e] = z;
+        }
+      }
+    }
+    if (!full) {
+      // (two scores at a time: the compiler would hold all 32 masks at once, and
+      // everything else in scratch registers)
+      const int until = min(hi, khi), sinks = min(late_args()->sinks, until);
+      const uint32_t span = (uint32_t)until - (uint32_t)lo;
+#pragma unroll
+      for (int k = 0; k < NB; ++k) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int n = nl + 32 * k + 8 * (e / 4) + e % 4;
+          const float z = (uint32_t)n - (uint32_t)lo < span ? acc[k][e] : -INFINITY;
+          acc[k][e] = n < sinks ? acc[k][e] : z;
+          if (e & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      if (paged && bad) {
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            if (bad >> (2 * k + u) & 1) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) acc[k][8 * u + e] = -INFINITY;
+            }
+          }
+        }
+      }
+    }
+    float mt = acc[0][0];
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mt = fmaxf(mt, acc[k][e]);
+    }
+    mt = max_halves(mt);
+    // as in attn_kernel: the reference point moves only when a score lies more than
+    // 2^8 above it
+    if (__any(mt > limit)) {
+      const float mn = fmaxf(mrun, mt);
+      const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(reference_step<CAP>(mrun, mn, c1));
+      mrun = mn;
+      lsum *= f;
+      if (LSE) esum *= f;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] *= f;
+      }
+      limit = mn + (CAP ? 8.f : c8);
+      const float ref = mn == -INFINITY ? 0.f : mn;
+      mu = CAP ? ref : ref * c1;
+      const bool far = !CAP && far_from_zero(ref, c1);
+      if (__any(far)) {  // every tile of such a row comes this way
+        if (far) limit = -INFINITY, mu = 0.f;
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[k][e] -= far ? ref : 0.f;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        float p[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          p[i] = __builtin_amdgcn_exp2f(CAP ? acc[k][e + i] - mu : fmaf(acc[k][e + i], c1, -mu));
+        if (LSE) esum += p[0] + p[1];
+        const bf16x2 pp = {(__bf16)p[0], (__bf16)p[1]};
+        lsum = __builtin_amdgcn_fdot2_f32_bf16(pp, bf16x2{(__bf16)1.f, (__bf16)1.f}, lsum, false);
+        pw[k][e / 8][e % 8 / 2] = __builtin_bit_cast(uint32_t, pp);
+      }
+    }
+  };
+
+  // x, as a value that is computed where it is used: scalar registers are few in the loop
+  auto here = [](int x) {
+    asm volatile("" : "+s"(x));
+    return x;
+  };
+  // Values of V that are not finite leave a tile that some row sees in part, as in
+  // attn_kernel; a wavefront does this for the rows that it copied.
+  auto clear_odd = [&](int it) {
+    uint64_t rows_odd = 0;
+    const int w = here(wid);
+#pragma unroll
+    for (int i = 0; i < RPW / 4; ++i) {
+      const uint32_t at = ldsV + vbuf(it) + (w * RPW + 4 * i) * kRowBytes + 16 * lane;
+      u32x4 x = lds_read<u32x4>(at, 0);
+      uint32_t seen = 0;  // an exponent of all ones carries into bits 15 and 31
+#pragma unroll
+      for (int e = 0; e < 4; ++e) seen |= (x[e] & 0x7F807F80u) + 0x00800080u;
+      seen &= 0x80008000u;
+      const uint64_t lanes = __ballot(seen != 0);
+      if (lanes) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if ((x[e] & 0x7F80u) == 0x7F80u) x[e] &= 0xFFFF0000u;
+          if ((x[e] & 0x7F800000u) == 0x7F800000u) x[e] &= 0x0000FFFFu;
+        }
+        *(__attribute__((address_space(3))) u32x4*)(lds_char*)at = x;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if ((lanes >> (16 * r)) & 0xFFFFu) rows_odd |= 1ull << (w * RPW + 4 * i + r);
+      }
+    }
+    return rows_odd;
+  };
+  auto is_partial = [&](int n0, uint32_t bad) { return n0 + KT > wg_all_hi || (n0 < wg_all_lo && n0 + KT > late_args()->sinks) || bad; };
+  // this wavefront's share of tile `it`, the last one copied, there and cleared
+  auto arrive = [&](int it, uint32_t bad) {
+    dma_wait<0>();
+    if (it < it1 && is_partial(tile_key(it), bad)) {
+      const uint64_t odd = clear_odd(it);
+      if ((lane ^ here(0)) == 0) odd_rows[(it - it0) & 3][wid] = odd;
+    }
+  };
+  auto meet = [&]() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" : : : "memory");
+  };
+  auto copy_ahead = [&](int it) {  // tile `it`, and the entries of the next; its bad pages
+    if (paged && ((it - it0) & (ahead - 1)) == 0) take_entries();
+    const uint32_t bad = bad_of(it);
+    if (it < it1) issue(it, tile_key(it), in_part);
+    if (paged && ((it + 1 - it0) & (ahead - 1)) == 0) fetch_entries(it + 1);
+    return bad;
+  };
+  // The end of the run of tiles from `it` on that all rows of the workgroup see
+  // wholly, whose slots follow one another and whose entries are held.
+  auto run_end = [&](int it) {
+    int e;
+    if (it < slots.near) {
+      e = min(slots.near, min(late_args()->sinks, wg_all_hi) / KT);
+    } else {
+      e = (it + slots.gap) * KT >= wg_all_lo ? min(it1, wg_all_hi / KT - slots.gap) : it;
+    }
+    if (paged) e = entry_bad ? it : min(e, ((it - it0) | (ahead - 1)) + it0);
+    return e;
+  };
+
+  // The tile before the first: probabilities and values of zero.
+#pragma unroll
+  for (int i = 0; i < RPW / 4; ++i)
+    *(__attribute__((address_space(3))) u32x4*)(lds_char*)(ldsV + 3 * kPairTile + (wid * RPW + 4 * i) * kRowBytes + 16 * lane) = u32x4{0, 0, 0, 0};
+  uint32_t bad_now = bad_of(it0), bad_next = bad_of(it0 + 1);
+  arrive(it0, bad_now);
+  lds_done();
+  meet();
+  if (behind) meet();
+  read_early(it0 - 1);
+  bool partial_last = false;  // of the tile before
+  int run = it0;
+  for (int it = it0; it < it1; ++it) {
+    const int n0 = tile_key(it);
+    // Tiles that need no masks, and two more behind them that need none, most of
+    // them, go without the bookkeeping of the others.
+    if (it >= run) run = run_end(it) - 2;
+    const bool plain = it < run;
+    // ---- products
+    __builtin_amdgcn_s_setprio(1);
+    product_v(it - 1);
+    product_k(it);
+    // operands are read kLook products ahead
+    __builtin_amdgcn_sched_group_barrier(kSchedLds, 2 * (kLook - 4), 0);
+#pragma unroll
+    for (int i = 0; i < 16 - kLook; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kSchedLds, 2, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kSchedMfma, kLook, 0);
+    __builtin_amdgcn_s_setprio(0);
+    if (partial_last) add_odd(it - 1);
+    if (plain) dma_wait<0>();
+    else arrive(it + 1, bad_next);
+    lds_done();
+    meet();
+    // ---- softmax
+    const uint32_t bad = bad_now;
+    bad_now = bad_next;
+    if (plain) issue(it + 2, n0 + 2 * KT, whole);
+    else bad_next = copy_ahead(it + 2);
+    softmax(n0, bad, plain);
+    partial_last = !plain && is_partial(n0, bad);
+    read_early(it);
+    meet();
+  }
+  if (!behind) meet();
+  product_v(it1 - 1);
+  if (partial_last) add_odd(it1 - 1);
+
+  // ---- results ---------------------------------------------------------------
+  lsum = sum_halves(lsum);
+  if (LSE) esum = sum_halves(esum);
+  // (where the workgroup is, found again: scalar registers are few in the loop)
+  const LateArgs la = late_args();
+  const PairItem end = pair_item(*la);
+  const FastDiv by_G{la->div_G.mul, la->div_G.shift};
+  const int end_first = uniform_load(la->lens + end.b), end_rows = chunk_tokens(*la, end.b, end_first) * la->G;
+  const int end_row = end.rb * kPairRows + wid * kBlockRows + col;
+  const bool joined = chunk_slots(*la, by_G, end_first, end_rows, end.rb * kPairRows, kPairRows, KT).tiles > la->unit;
+  if (end_row >= end_rows) return;
+  const int d0 = 4 * half;
+  if (joined) {
+    const int64_t at = ((int64_t)end.bh * (la->T * la->G) + end_row) * la->splits + end.split;
+    if (d0 == 0) la->part_ml[at] = make_float2(mrun, lsum);
+    if (LSE && d0 == 0) la->part_e[at] = esum;
+    if (lsum == 0.f) return;
+    float* po = la->part_o + at * kHeadDim + d0;
+#pragma unroll
+    for (int c = 0; c < 16; ++c)
+      *reinterpret_cast<float4*>(po + 8 * c) = make_float4(o[c / 4][4 * (c % 4)], o[c / 4][4 * (c % 4) + 1], o[c / 4][4 * (c % 4) + 2], o[c / 4][4 * (c % 4) + 3]);
+    return;
+  }
+  const float inv = lsum == 0.f ? 0.f : 1.f / lsum;  // a row that sees no key: zeros
+  const int end_t = by_G.quotient(end_row), head = end.h * la->G + end_row - end_t * la->G;
+  if (LSE && d0 == 0)
+    la->lse[end.b * la->sl_b + head * la->sl_h + end_t] = log_of_sum<CAP>(mrun, esum, log2_units<CAP>(la->sm_scale));
+  uint16_t* op = la->out + end.b * la->so_b + head * la->so_h + end_t * la->so_t + d0;
+#pragma unroll
+  for (int c = 0; c < 16; ++c)
+    *reinterpret_cast<uint2*>(op + 8 * c) = make_uint2(cvt_pk_bf16(o[c / 4][4 * (c % 4)] * inv, o[c / 4][4 * (c % 4) + 1] * inv),
+                                                       cvt_pk_bf16(o[c / 4][4 * (c % 4) + 2] * inv, o[c / 4][4 * (c % 4) + 3] * inv));
+}
+
+template <bool paged, bool LSE>
+static hipError_t launch_chunk_rows(AttnArgs a) {
+  const int nrb = (a.T * a.G + kPairRows - 1) / kPairRows, items = a.B * a.Hkv * nrb * a.splits;
+  a.nrb = nrb, a.items = items, a.div_nrb = FastDiv::by(nrb);
+  const int grid = a.rounds ? (items / nrb + 7) / 8 * 8 * nrb : (items + 7) / 8 * 8;
+#define BPC_ROWS(CAP, BIAS)                                                                                          \
+  {                                                                                                                  \
+    auto* f = chunk_rows_kernel<paged, CAP, BIAS, LSE>;                                                              \
+    static std::atomic<uint64_t> allowed{0};                                                                         \
+    if (hipError_t e = allow_lds(reinterpret_cast<const void*>(f), kPairLds, allowed); e != hipSuccess) return e;    \
+    f<<<grid, 512, kPairLds, a.stream>>>(a);                                                                         \
+  }
+  if (a.softcap > 0.f) {
+    if (a.slopes) BPC_ROWS(true, true) else BPC_ROWS(true, false)
+  } else {
+    if (a.slopes) BPC_ROWS(false, true) else BPC_ROWS(false, false)
+  }
+#undef BPC_ROWS
+  return hipGetLastError();
+}
+
 template <AttnKind KIND, bool LSE>
 static hipError_t launch_chunk_lse(const AttnArgs& a, const AttnPlan& p) {
-  hipError_t e;
-  if (p.rb == 1) {
-    e = p.once ? launch_attn_shape<1, 4, 32, KIND, true, LSE>(a) : launch_attn_shape<1, 4, 32, KIND, false, LSE>(a);
-  } else if (p.rb == 4) {
-    e = launch_attn_shape<4, 1, 64, KIND, false, LSE>(a);
-  } else {
-    e = launch_attn_shape<8, 1, 64, KIND, false, LSE>(a);
-  }
-  return e;
+  if (p.rb == 1) return p.once ? launch_attn_shape<1, 4, 32, KIND, true, LSE>(a) : launch_attn_shape<1, 4, 32, KIND, false, LSE>(a);
+  if (p.rb == 4) return launch_attn_shape<4, 1, 64, KIND, false, LSE>(a);
+  return launch_chunk_rows<KIND == kPagedChunk, LSE>(a);
 }
 
 template <AttnKind KIND>
