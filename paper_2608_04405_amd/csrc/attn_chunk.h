@@ -11,10 +11,11 @@ namespace bpc {
 // one) and softmax, with a barrier behind each, and one half of the wavefronts is
 // one barrier behind the other.  So a SIMD's two wavefronts are never in the same
 // part: one's products run beside the other's exponentials, where attn_kernel's run
-// almost in turn.  A wavefront sends off its share of tile t + 2 at the softmax of t and
-// waits for it at the products of t + 1.  Where wavefronts 0-3 are at the softmax of t,
-// the others are at its products: K of t, V of t - 1 and all from there to t + 2 are in
-// use, so that there are four buffers of V (and of K, where three would do).
+// almost in turn.  A wavefront sends off its share of tile t + 3 at the softmax of t and
+// waits for it at the products of t + 2, so that even pages from memory, in any order,
+// are there in time.  Where wavefronts 0-3 are at the softmax of t, the others are at its
+// products: K of t, V of t - 1 and all from there to t + 3 are in use, four buffers of K
+// and five of V.
 constexpr int kPairRows = 8 * kBlockRows;
 constexpr int kPairKeys = 64;
 constexpr int kPairTile = kPairKeys * kRowBytes;
@@ -22,7 +23,7 @@ constexpr int kPairTile = kPairKeys * kRowBytes;
 #define KLOOK 6
 #endif
 constexpr int kLook = KLOOK;
-constexpr int kPairLds = 8 * kPairTile;
+constexpr int kPairLds = 9 * kPairTile;
 
 // What a workgroup does: a row block of a piece of the slots of one KV head.
 struct PairItem {
@@ -51,8 +52,9 @@ __device__ __forceinline__ PairItem pair_item(const Args& a) {
 template <bool paged, bool CAP, bool BIAS, bool LSE>
 __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
   constexpr int KT = kPairKeys, NB = KT / 32, RPW = KT / 8;
+  constexpr int kShare = 2 * RPW / 4;  // copies of a wavefront for a tile
   extern __shared__ __attribute__((aligned(256))) char pair_tiles[];
-  __shared__ uint64_t odd_rows[4][8];
+  __shared__ uint64_t odd_rows[5][8];
   const PairItem item = pair_item(a);
   if (item.bh < 0) return;
   const int b = item.b, h = item.h;
@@ -70,7 +72,11 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
   if (it0 >= slots.tiles) return;
   auto tile_key = [&](int it) { return (it < slots.near ? it : it + slots.gap) * KT; };
   auto kbuf = [&](int it) { return (uint32_t)((it - it0) & 3) * kPairTile; };
-  auto vbuf = [&](int it) { return (uint32_t)((it - it0) & 3) * kPairTile; };
+  int v5 = 0;  // V of tile `it` of the loop lies in this one of five buffers, that of it + k in vslot(k)
+  auto vslot = [&](int k) {
+    const int x = v5 + k;
+    return k < 0 ? (x < 0 ? x + 5 : x) : (x >= 5 ? x - 5 : x);
+  };
 
   const uint32_t ldsK = (uint32_t)(uintptr_t)(lds_char*)pair_tiles, ldsV = ldsK + 4 * kPairTile;
   const char* Kb = reinterpret_cast<const char*>(a.K + (paged ? 0 : b * a.sK_b) + h * a.sK_h);
@@ -111,7 +117,7 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
     return bad;
   };
   // K and V of tile `it`, whose first slot is n0; FULL: all its slots are below khi
-  auto issue = [&](int it, int n0, auto full) {
+  auto issue = [&](int it, int n0, int slot, auto full) {
     constexpr bool FULL = decltype(full)::value;
     const int nu = FULL ? n0 + wid * RPW : min(n0 + wid * RPW, khi - 1);
     const char *kt, *vt;
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
     }
     kt = reinterpret_cast<const char*>(uniform64(reinterpret_cast<uint64_t>(kt)));
     vt = reinterpret_cast<const char*>(uniform64(reinterpret_cast<uint64_t>(vt)));
-    const uint32_t dk = ldsK + kbuf(it) + wid * RPW * kRowBytes, dv = ldsV + vbuf(it) + wid * RPW * kRowBytes;
+    const uint32_t dk = ldsK + kbuf(it) + wid * RPW * kRowBytes, dv = ldsV + slot * kPairTile + wid * RPW * kRowBytes;
     const int last = khi - 1 - nu;  // last row that may be read, from kt and vt on
     if (FULL || last >= RPW - 1) {
 #pragma unroll
@@ -165,8 +171,9 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
       qf[s] = __builtin_bit_cast(bf16x8, x);
     }
   }
-  issue(it0, tile_key(it0), in_part);
-  if (it0 + 1 < it1) issue(it0 + 1, tile_key(it0 + 1), in_part);
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+    if (it0 + i < it1) issue(it0 + i, tile_key(it0 + i), i, in_part);
 #pragma unroll
   for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
 
@@ -199,14 +206,14 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lds_read_tr(a0, at), lds_read_tr(a0 ^ 32u, at + 8 * kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7));
   };
   bf16x8 early[4];
-  auto read_early = [&](int it) {
-    const uint32_t v0 = vaddr + vbuf(it);
+  auto read_early = [&](int slot) {
+    const uint32_t v0 = vaddr + slot * kPairTile;
 #pragma unroll
     for (int d = 0; d < 4; ++d) early[d] = operand_v(opaque(v0 ^ 64u * d), 0, 0);
   };
-  auto product_v = [&](int it) {
+  auto product_v = [&](int slot) {
     uint32_t va[4];
-    const uint32_t v0 = vaddr + vbuf(it);
+    const uint32_t v0 = vaddr + slot * kPairTile;
 #pragma unroll
     for (int d = 0; d < 4; ++d) va[d] = opaque(v0 ^ 64u * d);
 #pragma unroll
@@ -235,11 +242,11 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
     }
   };
   // values of V that clear_odd() took out of tile `it`
-  auto add_odd = [&](int it) {
+  auto add_odd = [&](int it, int slot) {
     const int n0 = tile_key(it);
     uint64_t odd = 0;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) odd |= odd_rows[(it - it0) & 3][w];
+    for (int w = 0; w < 8; ++w) odd |= odd_rows[slot][w];
     odd = uniform64(odd);
     while (odd) {
       const int i = __ffsll((long long)odd) - 1, n = n0 + i;
@@ -367,12 +374,12 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
   };
   // Values of V that are not finite leave a tile that some row sees in part, as in
   // attn_kernel; a wavefront does this for the rows that it copied.
-  auto clear_odd = [&](int it) {
+  auto clear_odd = [&](int slot) {
     uint64_t rows_odd = 0;
     const int w = here(wid);
 #pragma unroll
     for (int i = 0; i < RPW / 4; ++i) {
-      const uint32_t at = ldsV + vbuf(it) + (w * RPW + 4 * i) * kRowBytes + 16 * lane;
+      const uint32_t at = ldsV + slot * kPairTile + (w * RPW + 4 * i) * kRowBytes + 16 * lane;
       u32x4 x = lds_read<u32x4>(at, 0);
       uint32_t seen = 0;  // an exponent of all ones carries into bits 15 and 31
 #pragma unroll
@@ -394,12 +401,13 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
     return rows_odd;
   };
   auto is_partial = [&](int n0, uint32_t bad) { return n0 + KT > wg_all_hi || (n0 < wg_all_lo && n0 + KT > late_args()->sinks) || bad; };
-  // this wavefront's share of tile `it`, the last one copied, there and cleared
-  auto arrive = [&](int it, uint32_t bad) {
-    dma_wait<0>();
+  // this wavefront's share of tile `it`, the last but one that it copied, there and cleared
+  auto arrive = [&](int it, uint32_t bad, int slot) {
+    if (it + 1 < it1) dma_wait<kShare>();
+    else dma_wait<0>();
     if (it < it1 && is_partial(tile_key(it), bad)) {
-      const uint64_t odd = clear_odd(it);
-      if ((lane ^ here(0)) == 0) odd_rows[(it - it0) & 3][wid] = odd;
+      const uint64_t odd = clear_odd(slot);
+      if ((lane ^ here(0)) == 0) odd_rows[slot][wid] = odd;
     }
   };
   auto meet = [&]() {
@@ -411,7 +419,7 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
   auto copy_ahead = [&](int it) {  // tile `it`, and the entries of the next; its bad pages
     if (paged && ((it - it0) & (ahead - 1)) == 0) take_entries();
     const uint32_t bad = bad_of(it);
-    if (it < it1) issue(it, tile_key(it), in_part);
+    if (it < it1) issue(it, tile_key(it), vslot(3), in_part);
     if (paged && ((it + 1 - it0) & (ahead - 1)) == 0) fetch_entries(it + 1);
     return bad;
   };
@@ -431,24 +439,29 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
   // The tile before the first: probabilities and values of zero.
 #pragma unroll
   for (int i = 0; i < RPW / 4; ++i)
-    *(__attribute__((address_space(3))) u32x4*)(lds_char*)(ldsV + 3 * kPairTile + (wid * RPW + 4 * i) * kRowBytes + 16 * lane) = u32x4{0, 0, 0, 0};
-  uint32_t bad_now = bad_of(it0), bad_next = bad_of(it0 + 1);
-  arrive(it0, bad_now);
+    *(__attribute__((address_space(3))) u32x4*)(lds_char*)(ldsV + 4 * kPairTile + (wid * RPW + 4 * i) * kRowBytes + 16 * lane) = u32x4{0, 0, 0, 0};
+  uint32_t bad[3] = {bad_of(it0), bad_of(it0 + 1), bad_of(it0 + 2)};  // of this tile and the next
+  if (it0 + 2 < it1) dma_wait<2 * kShare>();
+  else dma_wait<0>();
+  if (is_partial(tile_key(it0), bad[0])) {
+    const uint64_t odd = clear_odd(0);
+    if (lane == 0) odd_rows[0][wid] = odd;
+  }
   lds_done();
   meet();
   if (behind) meet();
-  read_early(it0 - 1);
+  read_early(vslot(-1));
   bool partial_last = false;  // of the tile before
   int run = it0;
   for (int it = it0; it < it1; ++it) {
     const int n0 = tile_key(it);
-    // Tiles that need no masks, and two more behind them that need none, most of
+    // Tiles that need no masks, and three more behind them that need none, most of
     // them, go without the bookkeeping of the others.
-    if (it >= run) run = run_end(it) - 2;
+    if (it >= run) run = run_end(it) - 3;
     const bool plain = it < run;
     // ---- products
     __builtin_amdgcn_s_setprio(1);
-    product_v(it - 1);
+    product_v(vslot(-1));
     product_k(it);
     // operands are read kLook products ahead
     __builtin_amdgcn_sched_group_barrier(kSchedLds, 2 * (kLook - 4), 0);
@@ -464,24 +477,25 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
     }
     __builtin_amdgcn_sched_group_barrier(kSchedMfma, kLook, 0);
     __builtin_amdgcn_s_setprio(0);
-    if (partial_last) add_odd(it - 1);
-    if (plain) dma_wait<0>();
-    else arrive(it + 1, bad_next);
+    if (partial_last) add_odd(it - 1, vslot(-1));
+    if (plain) dma_wait<kShare>();
+    else arrive(it + 1, bad[1], vslot(1));
     lds_done();
     meet();
     // ---- softmax
-    const uint32_t bad = bad_now;
-    bad_now = bad_next;
-    if (plain) issue(it + 2, n0 + 2 * KT, whole);
-    else bad_next = copy_ahead(it + 2);
-    softmax(n0, bad, plain);
-    partial_last = !plain && is_partial(n0, bad);
-    read_early(it);
+    const uint32_t bad_here = bad[0];
+    bad[0] = bad[1], bad[1] = bad[2];
+    if (plain) issue(it + 3, n0 + 3 * KT, vslot(3), whole);
+    else bad[2] = copy_ahead(it + 3);
+    softmax(n0, bad_here, plain);
+    partial_last = !plain && is_partial(n0, bad_here);
+    read_early(v5);
+    v5 = vslot(1);
     meet();
   }
   if (!behind) meet();
-  product_v(it1 - 1);
-  if (partial_last) add_odd(it1 - 1);
+  product_v(vslot(-1));
+  if (partial_last) add_odd(it1 - 1, vslot(-1));
 
   // ---- results ---------------------------------------------------------------
   lsum = sum_halves(lsum);
