@@ -11,18 +11,15 @@ namespace bpc {
 // one) and softmax, with a barrier behind each, and one half of the wavefronts is
 // one barrier behind the other.  So a SIMD's two wavefronts are never in the same
 // part: one's products run beside the other's exponentials, where attn_kernel's run
-// almost in turn.  A wavefront sends off its share of tile t + 3 at the softmax of t and
-// waits for it at the products of t + 2, so that even pages from memory, in any order,
-// are there in time.  Where wavefronts 0-3 are at the softmax of t, the others are at its
-// products: K of t, V of t - 1 and all from there to t + 3 are in use, four buffers of K
-// and five of V.
+// almost in turn.  A wavefront sends off its share of tile t + 3 between the products of t and
+// waits for it at those of t + 2, so that even pages from memory, in any
+// order, are there in time (and scalar arithmetic, 50 instructions a tile for pages, runs
+// beside the matrix unit; before the exponentials it cost 26 %).  Where wavefronts 0-3
+// are at the products of t + 1, the others are at the softmax of t and then at t + 1: V of
+// t and all from there to t + 4 are in use, five buffers, and four of K.
 constexpr int kPairRows = 8 * kBlockRows;
 constexpr int kPairKeys = 64;
 constexpr int kPairTile = kPairKeys * kRowBytes;
-#ifndef KLOOK
-#define KLOOK 6
-#endif
-constexpr int kLook = KLOOK;
 constexpr int kPairLds = 9 * kPairTile;
 
 // What a workgroup does: a row block of a piece of the slots of one KV head.
@@ -116,40 +113,50 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
     }
     return bad;
   };
-  // K and V of tile `it`, whose first slot is n0; FULL: all its slots are below khi
-  auto issue = [&](int it, int n0, int slot, auto full) {
-    constexpr bool FULL = decltype(full)::value;
-    const int nu = FULL ? n0 + wid * RPW : min(n0 + wid * RPW, khi - 1);
-    const char *kt, *vt;
+  // where slot nu, the wavefront's first of tile `it`, lies in K and V
+  struct Source {
+    const char *k, *v;
+  };
+  auto locate = [&](int it, int nu) {
+    Source x;
     if (paged) {
       const uint32_t page = (uint32_t)__builtin_amdgcn_readlane((int)entry, entry_of(it, wid * RPW));
       const uint32_t at = (uint32_t)nu & pmask;
-      kt = Kb + (page * kpage + (int64_t)at * kstep);
-      vt = Vb + (page * vpage + (int64_t)at * vstep);
+      x.k = Kb + (page * kpage + (int64_t)at * kstep), x.v = Vb + (page * vpage + (int64_t)at * vstep);
     } else {
-      kt = Kb + (int64_t)(uint32_t)nu * kstep, vt = Vb + (int64_t)(uint32_t)nu * vstep;
+      x.k = Kb + (int64_t)(uint32_t)nu * kstep, x.v = Vb + (int64_t)(uint32_t)nu * vstep;
     }
-    kt = reinterpret_cast<const char*>(uniform64(reinterpret_cast<uint64_t>(kt)));
-    vt = reinterpret_cast<const char*>(uniform64(reinterpret_cast<uint64_t>(vt)));
-    const uint32_t dk = ldsK + kbuf(it) + wid * RPW * kRowBytes, dv = ldsV + slot * kPairTile + wid * RPW * kRowBytes;
-    const int last = khi - 1 - nu;  // last row that may be read, from kt and vt on
-    if (FULL || last >= RPW - 1) {
+    x.k = reinterpret_cast<const char*>(uniform64(reinterpret_cast<uint64_t>(x.k)));
+    x.v = reinterpret_cast<const char*>(uniform64(reinterpret_cast<uint64_t>(x.v)));
+    return x;
+  };
+  const uint32_t wave_rows = wid * RPW * kRowBytes;
+  auto copy_k = [&](const char* from, int it) {
+    const uint32_t dk = ldsK + kbuf(it) + wave_rows;
 #pragma unroll
-      for (int i = 0; i < RPW / 4; ++i) {
-        dma16<false>(kt, koff[i], dk + 4 * i * kRowBytes);
-        dma16<false>(vt, voff[i], dv + 4 * i * kRowBytes);
-      }
+    for (int i = 0; i < RPW / 4; ++i) dma16<false>(from, koff[i], dk + 4 * i * kRowBytes);
+  };
+  auto copy_v = [&](const char* from, int slot) {
+    const uint32_t dv = ldsV + slot * kPairTile + wave_rows;
+#pragma unroll
+    for (int i = 0; i < RPW / 4; ++i) dma16<false>(from, voff[i], dv + 4 * i * kRowBytes);
+  };
+  auto issue = [&](int it, int slot) {
+    const int nu = min(tile_key(it) + wid * RPW, khi - 1);
+    const Source x = locate(it, nu);
+    const int last = khi - 1 - nu;  // last row that may be read, from there on
+    if (last >= RPW - 1) {
+      copy_k(x.k, it), copy_v(x.v, slot);
     } else {
+      const uint32_t dk = ldsK + kbuf(it) + wave_rows, dv = ldsV + slot * kPairTile + wave_rows;
 #pragma unroll
       for (int i = 0; i < RPW / 4; ++i) {
         const uint32_t r = min(4 * i + r4, last);
-        dma16<false>(kt, r * kstep + chunk[i], dk + 4 * i * kRowBytes);
-        dma16<false>(vt, r * vstep + chunk[i], dv + 4 * i * kRowBytes);
+        dma16<false>(x.k, r * kstep + chunk[i], dk + 4 * i * kRowBytes);
+        dma16<false>(x.v, r * vstep + chunk[i], dv + 4 * i * kRowBytes);
       }
     }
   };
-  constexpr std::true_type whole;
-  constexpr std::false_type in_part;
 
   if (paged) fetch_entries(it0), take_entries();
 
@@ -173,7 +180,7 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
   }
 #pragma unroll
   for (int i = 0; i < 3; ++i)
-    if (it0 + i < it1) issue(it0 + i, tile_key(it0 + i), i, in_part);
+    if (it0 + i < it1) issue(it0 + i, i);
 #pragma unroll
   for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
 
@@ -200,32 +207,21 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
   const float cap2 = a.softcap * kLog2e, capk = CAP ? 2.f * kLog2e * a.sm_scale / a.softcap : 0.f;
   auto visible = [&](int n, int sinks) { return (n >= lo || n < sinks) && n < hi; };
 
-  // O^T += V^T P^T of the tile whose probabilities are in pw, its first operands read before
-  auto operand_v = [&](uint32_t a0, int k, int s) {
-    const uint32_t at = (32 * k + 16 * s) * kRowBytes;
-    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lds_read_tr(a0, at), lds_read_tr(a0 ^ 32u, at + 8 * kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7));
-  };
-  bf16x8 early[4];
-  auto read_early = [&](int slot) {
-    const uint32_t v0 = vaddr + slot * kPairTile;
+  // O^T += V^T P^T of the tile whose probabilities are in pw, 16 keys at a time
+  bf16x8 operand[2][4];
+  auto read_v = [&](int slot, int keys) {
+    const uint32_t v0 = vaddr + slot * kPairTile, at = 16 * keys * kRowBytes;
 #pragma unroll
-    for (int d = 0; d < 4; ++d) early[d] = operand_v(opaque(v0 ^ 64u * d), 0, 0);
-  };
-  auto product_v = [&](int slot) {
-    uint32_t va[4];
-    const uint32_t v0 = vaddr + slot * kPairTile;
-#pragma unroll
-    for (int d = 0; d < 4; ++d) va[d] = opaque(v0 ^ 64u * d);
-#pragma unroll
-    for (int k = 0; k < NB; ++k) {
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const bf16x8 pf = __builtin_bit_cast(bf16x8, pw[k][s]);
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k || s ? operand_v(va[d], k, s) : early[d], pf, o[d], 0, 0, 0);
-      }
+    for (int d = 0; d < 4; ++d) {
+      const uint32_t x = opaque(v0 ^ 64u * d);
+      operand[keys & 1][d] = __builtin_bit_cast(
+          bf16x8, __builtin_shufflevector(lds_read_tr(x, at), lds_read_tr(x ^ 32u, at + 8 * kRowBytes), 0, 1, 2, 3, 4, 5, 6, 7));
     }
+  };
+  auto product_v = [&](int keys) {
+    const bf16x8 pf = __builtin_bit_cast(bf16x8, pw[keys / 2][keys % 2]);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand[keys & 1][d], pf, o[d], 0, 0, 0);
   };
   auto product_k = [&](int it) {
     uint32_t ka[8];
@@ -419,7 +415,7 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
   auto copy_ahead = [&](int it) {  // tile `it`, and the entries of the next; its bad pages
     if (paged && ((it - it0) & (ahead - 1)) == 0) take_entries();
     const uint32_t bad = bad_of(it);
-    if (it < it1) issue(it, tile_key(it), vslot(3), in_part);
+    if (it < it1) issue(it, vslot(3));
     if (paged && ((it + 1 - it0) & (ahead - 1)) == 0) fetch_entries(it + 1);
     return bad;
   };
@@ -450,7 +446,7 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
   lds_done();
   meet();
   if (behind) meet();
-  read_early(vslot(-1));
+  read_v(vslot(-1), 0);
   bool partial_last = false;  // of the tile before
   int run = it0;
   for (int it = it0; it < it1; ++it) {
@@ -459,42 +455,54 @@ __global__ __launch_bounds__(512, 2) void chunk_rows_kernel(AttnArgs a) {
     // them, go without the bookkeeping of the others.
     if (it >= run) run = run_end(it) - 3;
     const bool plain = it < run;
-    // ---- products
+    // ---- products; the copies, and where from, beside them
     __builtin_amdgcn_s_setprio(1);
-    product_v(vslot(-1));
+    read_v(vslot(-1), 1);
+    product_v(0);
+    const Source from = locate(it + 3, n0 + 3 * KT + wid * RPW);  // (used where this lies before khi)
+    if (plain) copy_k(from.k, it + 3);
+    read_v(vslot(-1), 2);
+    product_v(1);
+    if (plain) copy_v(from.v, vslot(3));
+    read_v(vslot(-1), 3);
+    product_v(2);
+    product_v(3);
     product_k(it);
-    // operands are read kLook products ahead
-    __builtin_amdgcn_sched_group_barrier(kSchedLds, 2 * (kLook - 4), 0);
+    // operands are read eight, then four products ahead
+    __builtin_amdgcn_sched_group_barrier(kSchedLds, 8, 0);
 #pragma unroll
-    for (int i = 0; i < 16 - kLook; ++i) {
-      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(kSchedLds, 2, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 4; ++i) {
       __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
       __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(kSchedMfma, kLook, 0);
+#pragma unroll
+    for (int i = 0; i < 12; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kSchedMfma, 8, 0);
     __builtin_amdgcn_s_setprio(0);
     if (partial_last) add_odd(it - 1, vslot(-1));
-    if (plain) dma_wait<kShare>();
+    if (plain) dma_wait<2 * kShare>();
     else arrive(it + 1, bad[1], vslot(1));
     lds_done();
     meet();
     // ---- softmax
     const uint32_t bad_here = bad[0];
     bad[0] = bad[1], bad[1] = bad[2];
-    if (plain) issue(it + 3, n0 + 3 * KT, vslot(3), whole);
-    else bad[2] = copy_ahead(it + 3);
+    if (!plain) bad[2] = copy_ahead(it + 3);
     softmax(n0, bad_here, plain);
     partial_last = !plain && is_partial(n0, bad_here);
-    read_early(v5);
+    read_v(v5, 0);
     v5 = vslot(1);
     meet();
   }
   if (!behind) meet();
-  product_v(vslot(-1));
+#pragma unroll
+  for (int keys = 0; keys < 4; ++keys) {
+    if (keys) read_v(vslot(-1), keys);
+    product_v(keys);
+  }
   if (partial_last) add_odd(it1 - 1, vslot(-1));
 
   // ---- results ---------------------------------------------------------------
