@@ -28,7 +28,7 @@ struct PairItem {
 };
 template <typename Args>
 __device__ __forceinline__ PairItem pair_item(const Args& a) {
-  const FastDiv by_nrb{a.div_nrb.mul, a.div_nrb.shift}, by_splits{a.div_splits.mul, a.div_splits.shift}, by_Hkv{a.div_Hkv.mul, a.div_Hkv.shift};
+  const FastDiv by_nrb{a.div_nrb.mul, a.div_nrb.shift}, by_bh{a.div_bh.mul, a.div_bh.shift}, by_Hkv{a.div_Hkv.mul, a.div_Hkv.shift};
   const int xcd = blockIdx.x & 7, turn = blockIdx.x >> 3;
   PairItem x{-1, 0, 0, 0, 0};
   int piece;
@@ -41,7 +41,7 @@ __device__ __forceinline__ PairItem pair_item(const Args& a) {
     if (item >= a.items || turn >= per) return x;
     piece = by_nrb.quotient(item), x.rb = a.nrb - 1 - (item - piece * a.nrb);
   }
-  x.bh = by_splits.quotient(piece), x.split = piece - x.bh * a.splits;
+  x.split = by_bh.quotient(piece), x.bh = piece - x.split * a.B * a.Hkv;
   x.b = by_Hkv.quotient(x.bh), x.h = x.bh - x.b * a.Hkv;
   return x;
 }

@@ -6,23 +6,62 @@
 
 namespace bpc {
 
-// The model of a prefill over the slots that a workgroup's rows see.
+// Pieces go round the XCDs where each gets as many, or nearly, so that long sequences'
+// pieces do not come to one; else each XCD gets a run of row blocks.
+static bool pieces_go_round(int64_t pieces) { return pieces % 8 == 0 || pieces >= 32; }
+
+// How a call is cut, by a model of its time (us) over the shapes and the lengths of
+// a piece: row blocks of 32 rows a workgroup, steps (tiles, or groups of four) of a
+// piece.  A round of workgroups costs 3, a step of one, four or eight row blocks as in
+// the comment of attn_plan but for the last, 1.95; with several sequences whose
+// pieces go round the XCDs a quarter of the work is taken to be missing (some are
+// shorter than the longest, where no window makes them alike), and pieces fill up each
+// other's rounds.  The join costs 2.5 and its partial results' way out
+// and back.  Measured (S: pieces of the longest sequence):
+//   2048 tokens of 2 requests over 32768 slots: eight row blocks 1384 us with S = 1,
+//   1473, 1343, 1508 with 2, 3, 4; four 1538, 1814, 1600
+//   1000 tokens of 2 requests over 16384 slots, cap and bias: eight 637, 668, 468, 529
+//   with S = 1 to 4; four 533, 642, 535
+//   257 tokens of 3 requests: one row block 27.5, four 19.7, eight 22.6
+//   one token, window 4096: S = 4, 8, 16, 32: 28.4, 21.1, 17.7, 16.1
 AttnPlan chunk_plan(int B, int Hkv, int G, int T, int N, int window, int sinks) {
-  const int64_t all = N;
-  if (window) N = (int)std::min<int64_t>(N, (int64_t)window + sinks + std::min(T, 256 / G));
-  AttnPlan p = attn_plan(B, Hkv, G, T, N, false);
-  if (getenv("BPC_RB") && atoi(getenv("BPC_RB"))) p.rb = atoi(getenv("BPC_RB"));
-  if (getenv("BPC_S") && atoi(getenv("BPC_S"))) p.splits = atoi(getenv("BPC_S"));
-  // the most steps of a row block
-  const int64_t keys = p.rb == 1 ? 32 : 64, group = p.rb == 1 ? 4 : 1;
-  int64_t tiles = (all + keys - 1) / keys;
-  if (window) tiles = std::min(tiles, (sinks + keys - 1) / keys + ((int64_t)window + std::min<int64_t>(T, (p.rb * 32 + G - 1) / G + 1)) / keys + 2);
-  const int64_t steps = (tiles + group - 1) / group;
-  p.unit = (int)((steps + p.splits - 1) / p.splits);
-  p.splits = (int)((steps + p.unit - 1) / p.unit);
-  p.total = 0;
+  AttnPlan p{};
+  const int64_t rows = (int64_t)T * G, bh = (int64_t)B * Hkv;
+  double best = 0;
+  int64_t best_pieces = 1;
+  // (as in attn_plan; of a window's slots only those are read)
+  const int64_t seen = window ? std::min<int64_t>(N, (int64_t)window + sinks + T) : N;
+  const bool ragged = B > 1 && 2 * seen > N;
+  for (int rb = 1; rb <= 8; rb = rb == 1 ? 4 : 2 * rb) {
+    if (rb > 1 && rows <= rb / 2 * kBlockRows) break;
+    const int64_t nrb = (rows + rb * kBlockRows - 1) / (rb * kBlockRows);
+    const int slots = rb == 4 ? 512 : 256;
+    // the most steps of a row block
+    const int64_t keys = rb == 1 ? 32 : 64, group = rb == 1 ? 4 : 1;
+    int64_t tiles = (N + keys - 1) / keys;
+    if (window) tiles = std::min(tiles, (sinks + keys - 1) / keys + ((int64_t)window + std::min<int64_t>(T, (rb * 32 + G - 1) / G + 1)) / keys + 2);
+    const int64_t steps = (tiles + group - 1) / group;
+    for (int64_t want = 1; want <= kMaxSplits && want <= steps; ++want) {
+      const int64_t unit = (steps + want - 1) / want, pieces = (steps + unit - 1) / unit;
+      if (pieces != want) continue;
+      const double wgs = (double)(bh * nrb * pieces);
+      const bool spread = pieces_go_round(bh * pieces);
+      const double full = (double)(spread ? (bh * pieces + 7) / 8 * nrb : (bh * pieces * nrb + 7) / 8) / (slots / 8);
+      const double busy = ragged ? 0.75 * wgs : wgs;
+      const double step = rb == 8 ? 1.95 : rb == 4 ? (wgs > 256 ? 2.1 : 1.5) : nrb > 1 ? 1.4 : busy > 161 ? 2.7 * (busy < 256 ? busy / 256 : 1) : 1.7;
+      // rounds of workgroups; a last one that is not full takes as long as another
+      double rounds = full <= 1 ? 1 : full < 8 ? ceil(full) : full;
+      if (ragged && spread && full > 1) rounds = std::max(1.0, 0.75 * full + 0.5);
+      const double mean = rounds <= 1 || window ? 1 : 1.2 - 0.5 * (T < N ? (double)T / N : 1);
+      const double join = pieces == 1 ? 0 : 2.5 + (ragged ? 0.75 : 1) * (double)(bh * rows) * pieces * (2 * (kHeadDim + 2) * sizeof(float)) / 4e6;
+      const double us = 3 + rounds * (3 + std::min(mean, 1.0) * (double)unit * step) + join;
+      if (!p.rb || us < best) best = us, p.rb = rb, p.unit = (int)unit, best_pieces = pieces;
+    }
+  }
+  p.splits = (int)best_pieces;
+  p.once = rows <= kBlockRows && bh * seen * (4 * kHeadDim) > (int64_t)320 << 20;
   if (p.splits > 1) {
-    const size_t n = (size_t)B * Hkv * T * G * p.splits;
+    const size_t n = (size_t)(bh * rows) * p.splits;
     auto take = [&](size_t bytes) {
       const size_t at = p.total;
       p.total += (bytes + 255) / 256 * 256;
@@ -36,10 +75,9 @@ AttnPlan chunk_plan(int B, int Hkv, int G, int T, int N, int window, int sinks) 
 }
 
 hipError_t launch_chunk(AttnArgs a, const AttnPlan& p) {
-  a.div_G = FastDiv::by(a.G), a.div_Hkv = FastDiv::by(a.Hkv), a.div_splits = FastDiv::by(a.splits);
-  const int pieces = a.B * a.Hkv * a.splits;
+  a.div_G = FastDiv::by(a.G), a.div_Hkv = FastDiv::by(a.Hkv), a.div_bh = FastDiv::by(a.B * a.Hkv);
   a.unit = p.unit, a.tile_keys = p.rb == 1 ? 32 : 64, a.tile_group = p.rb == 1 ? 4 : 1, a.block_rows = p.rb * kBlockRows;
-  a.rounds = pieces % 8 == 0 || pieces >= 32;
+  a.rounds = pieces_go_round((int64_t)a.B * a.Hkv * a.splits);
   const hipError_t e = a.table ? launch_chunk_paged(a, p) : launch_chunk_as<kChunk>(a, p);
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.T * a.G;

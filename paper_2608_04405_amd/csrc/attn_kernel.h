@@ -233,7 +233,10 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
     if (item >= a.items || turn >= (a.items + 7) >> 3) return;
     piece = a.div_nrb.quotient(item), rb = a.nrb - 1 - (item - piece * a.nrb);
   }
-  const int bh = a.div_splits.quotient(piece), split = piece - bh * a.splits;
+  // (a chunk's pieces begin with the first of every KV head, so that those that short
+  // sequences do not have come to no XCD more than to others)
+  const int whole = CHUNK ? a.div_bh.quotient(piece) : a.div_splits.quotient(piece);
+  const int bh = CHUNK ? piece - whole * a.B * a.Hkv : whole, split = CHUNK ? whole : piece - bh * a.splits;
   const int b = a.div_Hkv.quotient(bh), h = bh - b * a.Hkv;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int grp = wid / RB, rbw = wid % RB;

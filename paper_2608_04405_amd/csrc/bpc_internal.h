@@ -317,7 +317,8 @@ struct AttnArgs {
   // a chunk: new tokens (NULL: T), slots that a token sees before its own and at the start
   const int32_t* count;
   int window, sinks;
-  int rounds;    // pieces go round the XCDs
+  FastDiv div_bh;  // by B Hkv
+  int rounds;      // pieces go round the XCDs
   int unit;      // steps of a piece, of tile_group tiles of tile_keys slots each
   int tile_keys, tile_group, block_rows;  // rows of a row block (a power of two)
   float* lse;    // [B, Hq, T] or NULL

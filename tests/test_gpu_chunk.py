@@ -100,8 +100,8 @@ def test_window(B, Hq, Hkv, T, pos, count, N, window, sinks, page):
 
 # sizes, window and sinks for each cut: row blocks of a workgroup, in pieces or not
 CUTS = [((1, 8, 2, 9, 120), 0, 0, 1, False), ((1, 4, 1, 7, 3000), 0, 0, 1, True), ((8, 20, 4, 100, 130), 0, 0, 4, False),
-        ((3, 24, 2, 140, 700), 0, 0, 4, True), ((6, 40, 5, 130, 150), 0, 0, 8, False), ((1, 128, 1, 41, 5000), 0, 0, 8, True),
-        ((6, 40, 5, 130, 400), 60, 10, 8, False), ((1, 40, 2, 130, 3000), 2000, 70, 4, True)]
+        ((3, 24, 2, 140, 700), 0, 0, 4, True), ((6, 40, 5, 130, 150), 0, 0, 8, False), ((1, 128, 1, 41, 5000), 0, 0, 4, True), ((1, 64, 1, 130, 5000), 0, 0, 8, True),
+        ((6, 40, 5, 130, 400), 60, 10, 8, False), ((1, 40, 2, 130, 3000), 2000, 70, 4, True), ((1, 64, 1, 130, 5000), 2500, 70, 8, True)]
 
 
 @pytest.mark.parametrize("page", [0, 16])
