@@ -637,6 +637,8 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (see && (w[e] & 0x7F800000u) == 0x7F800000u) o[c / 4][4 * (c % 4) + e] += __uint_as_float(w[e]);
+        // (else the compiler holds 64 masks at once, and the loop's scalars in vector registers)
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   };

@@ -361,6 +361,7 @@ struct WeightArgs {
   float decay;
   FastDiv div_G, div_Hkv, div_blocks;
   int blocks, rounds;  // key blocks of a (b, h); whether (b, h) go round the XCDs
+  int run;             // few rows: keys of a workgroup
   hipStream_t stream;
 };
 int64_t weights_blocks(int B, int Hkv, int N);  // the most workgroups of a call
