@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <array>
 #include <mutex>
 
 #include "bpc_internal.h"
@@ -624,7 +625,8 @@ static bool rows_meet(int64_t away, const Distances* d, int dims) {
   return false;
 }
 
-static int check_separate(const RowSet& out, const RowSet& in) {
+// strict: nor may the ranges of addresses meet where the strides differ.
+static int check_separate(const RowSet& out, const RowSet& in, bool strict = false) {
   if (!out.p || !in.p) return BPC_OK;
   int64_t out_span = kHeadDim, in_span = kHeadDim;
   Distances d[3];
@@ -641,7 +643,7 @@ static int check_separate(const RowSet& out, const RowSet& in) {
   std::sort(d, d + dims, [](const Distances& x, const Distances& y) { return x.stride > y.stride; });
   int64_t span = kHeadDim;
   for (int i = dims; i--;) alike = alike && d[i].stride >= span, span += d[i].reach();
-  return alike && rows_meet(away, d, dims) ? fail(BPC_EINVAL, "%s overlaps %s", out.name, in.name) : BPC_OK;
+  return (alike ? rows_meet(away, d, dims) : strict) ? fail(BPC_EINVAL, "%s overlaps %s", out.name, in.name) : BPC_OK;
 }
 
 static int check_rotation(const float* cos_sin, int table_rows, int R) {
@@ -985,6 +987,16 @@ int bpc_chunk_cut(int B, int Hq, int Hkv, int T, int N, int D, int window, int s
   return BPC_OK;
 }
 
+// Calls of the same sizes come one after another, and the model that cuts them takes
+// some microseconds.
+static AttnPlan last_chunk_plan(int B, int Hkv, int G, int T, int N, int window, int sinks) {
+  static thread_local std::array<int, 7> sizes{};
+  static thread_local AttnPlan plan;
+  const std::array<int, 7> now{B, Hkv, G, T, N, window, sinks};
+  if (now != sizes) plan = chunk_plan(B, Hkv, G, T, N, window, sinks), sizes = now;
+  return plan;
+}
+
 int bpc_chunk_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t, const uint16_t* K, int64_t sK_b,
                         int64_t sK_h, int64_t sK_n, const uint16_t* V, int64_t sV_b, int64_t sV_h, int64_t sV_n,
                         const int32_t* block_table, int64_t st_b, int num_pages, int page_size, const int32_t* pos,
@@ -1007,7 +1019,7 @@ int bpc_chunk_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t s
   a.out = out, a.so_b = so_b, a.so_h = so_h, a.so_t = so_t;
   a.lse = lse, a.sl_b = sl_b, a.sl_h = sl_h;
   a.stream = static_cast<hipStream_t>(stream);
-  const AttnPlan plan = chunk_plan(B, Hkv, a.G, T, N, a.window, a.sinks);
+  const AttnPlan plan = last_chunk_plan(B, Hkv, a.G, T, N, a.window, a.sinks);
   if ((st = check_attn(a, Hq, D, plan, workspace, workspace_bytes))) return st;
   if ((st = check_int32("pos", pos, 0))) return st;
   if (count && (st = check_int32("count", count, 0))) return st;
@@ -1034,6 +1046,7 @@ int bpc_key_weights(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
   if ((st = check_window(window, sinks))) return st;
   if ((st = check_rows("q", q, sq_b, sq_h, sq_t))) return st;
   if ((st = check_kv("K", K, sK_b, sK_h, sK_n))) return st;
+  if (sK_n > (1 << 24)) return fail(BPC_EUNSUPPORTED, "row stride of K: at most 2^24 elements");
   if ((st = check_scores(sm_scale, softcap, slopes))) return st;
   if (!(decay >= 0.0f) || !__builtin_isfinite(decay)) return fail(BPC_EINVAL, "decay must be finite and >= 0");
   if ((st = check_floats("lse", lse, sl_b, sl_h))) return st;
@@ -1106,7 +1119,7 @@ int bpc_evict_kv(const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n, co
   // (the pages read and those written may be of one pool)
   if (!block_table || !table_out)
     for (int i = 0; i < 4; ++i)
-      if ((st = check_separate(out[i / 2], in[i % 2]))) return st;
+      if ((st = check_separate(out[i / 2], in[i % 2], true))) return st;
   if ((st = check_floats("weights", weights, sw_b, sw_h))) return st;
   if ((st = check_int32("lens", lens, 0))) return st;
   if ((st = check_int32("kept", kept, 0))) return st;
