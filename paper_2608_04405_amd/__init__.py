@@ -731,19 +731,20 @@ def _cache(t: torch.Tensor, name: str):
     return a, b, c, (x, y, z if c > 1 else 128)
 
 
-def _written(t: torch.Tensor, name: str, B: int, H: int, T: int):
-    """The strides of a [B, H, T, 128] tensor whose rows a call writes."""
+def _written(t: torch.Tensor, name: str, B: Optional[int] = None, H: Optional[int] = None, T: Optional[int] = None):
+    """The strides of a [B, H, T, 128] tensor whose rows a call writes, behind its
+    extents where these are not given."""
     a, b, c, x, y, z = _rows(t, name)
-    if a != B or b != H or c != T:
+    if B is not None and (a != B or b != H or c != T):
         _extent(t, name, (B, H, T, 128))
-    if not t.is_contiguous():
+    if (z < 128 or y < z * c or x < y * b) and not t.is_contiguous():
         span = 128  # a stride is no smaller than what those below it span
-        for stride, extent in sorted(((x, B), (y, H), (z, T))):
+        for stride, extent in sorted(((x, a), (y, b), (z, c))):
             if extent > 1:
                 if stride < span:
                     raise ValueError(f"{name}: its rows must not overlap (strides {tuple(t.stride())})")
                 span += stride * (extent - 1)
-    return x, y, z
+    return (x, y, z) if B is not None else (a, b, c, (x, y, z))
 
 
 def _dense(B: int, H: int, T: int):
@@ -1110,17 +1111,21 @@ def _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, V=None, weights=None):
     return N, pages, page, st
 
 
-def _float_rows(t: Optional[torch.Tensor], name: str, shape, written: bool):
-    """(batch, head) strides of an fp32 [B, H, n] tensor with contiguous rows
-    (spec of n as for _extent); rows that are written must not overlap."""
+def _float_rows(t: Optional[torch.Tensor], name: str, B: int, H: int, n: int, more: bool, written: bool):
+    """(batch, head) strides of an fp32 [B, H, n] tensor (or wider, with `more`)
+    with contiguous rows; rows that are written must not overlap."""
     if t is None:
         return 0, 0
-    if type(t) is not torch.Tensor or t.dtype is not torch.float32 or t.dim() != 3 or t.shape != shape or t.stride(2) != 1:
+    fits = False
+    if type(t) is torch.Tensor and t.dtype is torch.float32 and t.dim() == 3:
+        (b, h, m), (x, y, one) = t.shape, t.stride()
+        fits = b == B and h == H and one == 1 and (m == n or more and m > n)
+    if not fits:
         _need(t, name, torch.float32, 3)
-        _extent(t, name, shape)
-    (B, H, n), (x, y, _) = t.shape, t.stride()
-    if written and not t.is_contiguous():
-        span = n
+        _extent(t, name, (B, H, ("ge", n) if more else n))
+        (_, _, m), (x, y, _) = t.shape, t.stride()
+    if written and (y < m or x < y * H) and not t.is_contiguous():
+        span = m
         for stride, extent in sorted(((x, B), (y, H))):
             if extent > 1:
                 if stride < span:
@@ -1159,7 +1164,7 @@ def chunk_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, pos: torc
     _window(window, sinks)
     _indices(pos, "pos", (B,))
     _indices(count, "count", (B,))
-    sl = _float_rows(lse_out, "lse_out", (B, Hq, T), True)
+    sl = _float_rows(lse_out, "lse_out", B, Hq, T, False, True)
     _on_gpu(q, K, V, pos, count, block_table, slopes, out, lse_out, workspace)
     dev = q.get_device()
     if stream is not None or dev != _current_device():
@@ -1206,8 +1211,8 @@ def key_weights(q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, weights: to
     _window(window, sinks)
     _indices(pos, "pos", (B,))
     _indices(count, "count", (B,))
-    sl = _float_rows(lse, "lse", (B, Hq, T), False)
-    sw = _float_rows(weights, "weights", (B, Hkv, ("ge", N)), True)
+    sl = _float_rows(lse, "lse", B, Hq, T, False, False)
+    sw = _float_rows(weights, "weights", B, Hkv, N, True, True)
     _on_gpu(q, K, lse, weights, pos, count, block_table, slopes)
     dev = q.get_device()
     if stream is not None or dev != _current_device():
@@ -1259,21 +1264,26 @@ def evict_kv(K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, lens: torc
         raise ValueError(f"keep={keep} must be in [1, N={N}]")
     if sinks < 0 or recent < 0 or sinks + recent > keep:
         raise ValueError(f"sinks={sinks} and recent={recent} must be >= 0, together at most keep={keep}")
-    Ob, Oh, On, *_ = _rows(K_out, "K_out")
+    Ob, Oh, On, sKo = _written(K_out, "K_out")
+    Pb, Ph, Pn, sVo = _written(V_out, "V_out")
     out_pages = out_page = sto = 0
     if table_out is None:
         if Ob != B or Oh != Hkv or On < keep:
             _extent(K_out, "K_out", (B, Hkv, ("ge", keep), 128))
-        _extent(V_out, "V_out", (B, Hkv, ("ge", keep), 128))
+        if Pb != B or Ph != Hkv or Pn < keep:
+            _extent(V_out, "V_out", (B, Hkv, ("ge", keep), 128))
     else:
+        if Oh != Hkv:
+            _extent(K_out, "K_out", (Ob, Hkv, On, 128))
+        if Pb != Ob or Ph != Hkv or Pn != On:
+            _extent(V_out, "V_out", (Ob, Hkv, On, 128))
         out_pages, out_page = Ob, On
         _page_rows(out_page)
         sto, most = _block_table(table_out, B)
         if most * out_page < keep:
             raise ValueError(f"table_out holds {most * out_page} slots per sequence, keep={keep}")
-    sKo, sVo = _written(K_out, "K_out", Ob, Hkv, On), _written(V_out, "V_out", Ob, Hkv, V_out.shape[2] if table_out is None else On)
-    sw = _float_rows(weights, "weights", (B, Hkv, ("ge", N)), False)
-    swo = _float_rows(weights_out, "weights_out", (B, Hkv, ("ge", keep)), True)
+    sw = _float_rows(weights, "weights", B, Hkv, N, True, False)
+    swo = _float_rows(weights_out, "weights_out", B, Hkv, keep, True, True)
     if (codes is None) != (codes_out is None):
         raise ValueError("codes and codes_out are given together or not at all")
     W, sC, sCo = 0, (0, 0), (0, 0)
