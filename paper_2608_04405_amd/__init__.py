@@ -1251,8 +1251,9 @@ def evict_kv(K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, lens: torc
     a sequence]) pools of pages, which may be K and V themselves as long as no page
     that is written is read or written twice.  codes as build_hash gives them.  N:
     slots that any sequence may use (default: what the cache or the table, and the
-    weights, hold); one whose lens[b] is not in [0, N] is skipped.  The sequences'
-    new lengths are lens.clamp(max=keep)."""
+    weights, hold); one whose lens[b] is not in [0, N] is skipped (its slots in the
+    result are undefined where that is allocated here).  The sequences' new lengths
+    are lens.clamp(max=keep)."""
     Kb, Hkv, Kn, sK = _cache(K, "K")
     Vb, Vh, Vn, sV = _cache(V, "V")
     _indices(lens, "lens", (lens.shape[0],) if isinstance(lens, torch.Tensor) and lens.dim() == 1 else (1,))

@@ -1,5 +1,6 @@
-// Dense attention of many query rows: a masked prefill, and a tree of drafted
-// tokens over a contiguous or paged cache.
+// Dense attention of many query rows: a masked prefill, a tree of drafted
+// tokens over a contiguous or paged cache, and a chunk of few new tokens over either
+// (of many: chunk_rows_kernel).
 //
 // The G query heads of a KV head share its keys, so a row of the product is a
 // (token, head) pair, r = t G + g, and 32 rows make a row block.  A wavefront
@@ -25,7 +26,8 @@
 // other vector instructions 35 % and more; 512 queries over 65536 keys with a bias
 // 0.57 ms, 41 and 50 %; capped scores (8001 tokens in documents, 0.19 ms, 0.55 PFLOP/s)
 // 22 and 37 %, three of their instructions transcendental.  Where rows are few by
-// memory (8 tokens over 16 x 131072 slots: 0.94 ms, 6.8 TB/s).
+// memory (8 tokens over 16 x 131072 slots: 0.94 ms, 6.8 TB/s; one token over the last
+// 16384 of 16 sequences' slots: 0.165 ms, 6.5 TB/s).
 #pragma once
 #include <math.h>
 
@@ -317,7 +319,7 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
   // A chunk's workgroups of several row blocks look up 64 entries at a time, a lane
   // each, a tile before they are needed: they lie in registers by then, where a
   // scalar load would be waited for in every tile (2048 tokens over 32768 slots, 32
-  // heads, pages of 64: 1177 -> PAGED us; contiguous 1016).
+  // heads, pages of 64: 1177 -> 1065 us; contiguous 1016).
   constexpr bool AHEAD = CHUNK && paged && RB > 1;
   constexpr int kAhead = 64 / NP;  // tiles whose entries a wavefront holds
   uint32_t entry = 0, next_entry = 0;
