@@ -935,9 +935,10 @@ int bpc_tree_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq
 }
 
 // fp32 rows [B, H][len], the innermost dimension contiguous
+constexpr int64_t kMaxStride = (int64_t)1 << 40;
 static int check_floats(const char* name, const void* p, int64_t sb, int64_t sh) {
   if (!p) return fail(BPC_EINVAL, "%s is NULL", name);
-  if (sb < 0 || sh < 0) return fail(BPC_EINVAL, "%s strides must be >= 0", name);
+  if (sb < 0 || sh < 0 || sb > kMaxStride || sh > kMaxStride) return fail(BPC_EINVAL, "%s strides must be in [0, 2^40]", name);
   if (!aligned4(p)) return fail(BPC_EALIGN, "%s must be 4-byte aligned", name);
   return BPC_OK;
 }
@@ -947,7 +948,6 @@ static int check_floats_apart(const char* name, int64_t sb, int64_t sh, int B, i
   const bool heads_inside = sh <= sb;
   const int64_t in = heads_inside ? sh : sb, out = heads_inside ? sb : sh;
   const int in_n = heads_inside ? H : B, out_n = heads_inside ? B : H;
-  if (out > INT64_MAX / 4 / std::max(B, H)) return fail(BPC_EINVAL, "%s: strides (%lld, %lld)", name, (long long)sb, (long long)sh);
   if ((in_n > 1 && in < len) || (out_n > 1 && out < (in_n > 1 ? in * (in_n - 1) : 0) + len))
     return fail(BPC_EINVAL, "%s: written rows must not overlap, strides (%lld, %lld)", name, (long long)sb, (long long)sh);
   return BPC_OK;
@@ -1115,7 +1115,7 @@ int bpc_evict_kv(const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n, co
   const int in_B = block_table ? num_pages : B, in_N = block_table ? page_size : N;
   const RowSet in[2] = {{"K", K, {sK_b, sK_h, sK_n}, {in_B, Hkv, in_N}}, {"V", V, {sV_b, sV_h, sV_n}, {in_B, Hkv, in_N}}};
   const RowSet out[2] = {{"K_out", K_out, {sKo_b, sKo_h, sKo_n}, {out_B, Hkv, out_N}}, {"V_out", V_out, {sVo_b, sVo_h, sVo_n}, {out_B, Hkv, out_N}}};
-  if ((st = check_separate(out[0], out[1]))) return st;
+  if ((st = check_separate(out[0], out[1], true))) return st;
   // (the pages read and those written may be of one pool)
   if (!block_table || !table_out)
     for (int i = 0; i < 4; ++i)
@@ -1133,6 +1133,7 @@ int bpc_evict_kv(const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n, co
     if (W != 1 && W != 2 && W != 4) return fail(BPC_EUNSUPPORTED, "W=%d words: 1, 2 or 4", W);
     if ((st = check_codes("codes", codes, sC_b, sC_h, W))) return st;
     if ((st = check_codes("codes_out", codes_out, sCo_b, sCo_h, W))) return st;
+    if (std::max({sC_b, sC_h, sCo_b, sCo_h}) > kMaxStride) return fail(BPC_EINVAL, "codes strides must be in [0, 2^40]");
     if ((st = check_floats_apart("codes_out", sCo_b, sCo_h, B, Hkv, (int64_t)keep * W))) return st;
   }
   auto span = [&](int64_t sb, int64_t sh, int64_t len) { return 4 * (sb * (B - 1) + sh * (Hkv - 1) + len); };

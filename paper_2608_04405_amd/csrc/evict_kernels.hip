@@ -60,6 +60,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   const int lo = all ? n : a.sinks, hi = all ? n : n - a.recent;  // the slots between are chosen from
   const int m = all ? 0 : a.keep - a.sinks - a.recent;
   if (!ONE && pass < 3 && m == 0) return;
+  // segments that hold slots of the sequence; the others have nothing to say
+  const int used = ONE ? 1 : max(1, (n + kSegSlots - 1) / kSegSlots);
+  if (seg >= used) return;
   const int slot0 = seg * kSegSlots + wid * (ROUNDS * 64) + lane;
 
   float x[ROUNDS];
@@ -107,7 +110,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     } else {
       const uint32_t* c = counts + p * kSelectBins + bin_low;
 #pragma unroll 8
-      for (int s = 0; s < segs; ++s) {
+      for (int s = 0; s < used; ++s) {
         const uint2 v = *reinterpret_cast<const uint2*>(c + (int64_t)s * kSegWords);
         if (s < seg) pre_top += (int)v.y, pre_low += (int)v.x;
         top += (int)v.y, low += (int)v.x;
@@ -160,9 +163,9 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   // ---- the slots that stay, in order: `need` of those equal to the key ---------
   int32_t* kept = a.kept + (int64_t)bh * a.keep;
   float* wo = a.weights_out ? a.weights_out + b * a.swo_b + h * a.swo_h : nullptr;
-  for (int64_t i = stay + seg * kSelectThreads + t; i < a.keep; i += segs * kSelectThreads) kept[i] = -1;
+  for (int64_t i = stay + seg * kSelectThreads + t; i < a.keep; i += used * kSelectThreads) kept[i] = -1;
   if (wo)
-    for (int64_t i = stay + seg * kSelectThreads + t; i < a.cap; i += segs * kSelectThreads) wo[i] = 0.f;
+    for (int64_t i = stay + seg * kSelectThreads + t; i < a.cap; i += used * kSelectThreads) wo[i] = 0.f;
   int above = 0, equal = 0;  // in this wavefront
   if (m > 0) {
 #pragma unroll

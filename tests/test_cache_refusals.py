@@ -171,3 +171,13 @@ def test_sizes(lib):
     ev = lib.bpc_evict_workspace_bytes
     assert ev(2, 8, 16384, 100) == 0 and ev(2, 8, 16385, 100) > 0 and ev(2, 8, 16385, 100) % 4 == 0
     assert ev(0, 8, 20000, 5) == ev(2, 8, 20000, 0) == ev(2, 8, 20000, 20001) == 0
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(Vo=5 * FAR + 256, Vo_t=256, Vo_h=2000 * 256, Vo_b=4000 * 256), b"overlaps"), (dict(w_b=(1 << 40) + 1), b"2^40"), (dict(wo=8 * FAR, wo_h=1 << 41), b"2^40"),
+    (dict(CODES, C_b=1 << 41), b"2^40"),
+])
+def test_evict_entry_says_why(lib, kw, word):
+    """Results at other strides within one another's reach, and strides that no memory has."""
+    assert call(lib, "bpc_evict_kv", EVICT, kw) == EINVAL
+    assert word in lib.bpc_last_error()

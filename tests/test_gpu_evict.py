@@ -181,3 +181,9 @@ def test_long():
     check(gathered(7, 1, 2, 131072), [131072], 65536, 4, 4096)
     check(gathered(8, 1, 1, 200001), [200001], 1000, 4, 96)
     check(gathered(9, 24, 16, 1500), [1500 - 7 * b for b in range(24)], 800, 16, 64, W=1)
+
+
+@pytest.mark.parametrize("keep", [60, 17000])
+def test_lengths_far_below_the_room(keep):
+    """Sequences that use some of the segments, one, or none."""
+    check(gathered(10, 6, 1, 50000), [50000, 16384, 16385, 100, 0, 33000], keep, 4, 16)
