@@ -52,9 +52,17 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   const int bh = ONE ? (int)blockIdx.x : (int)(blockIdx.x / (uint32_t)segs), seg = ONE ? 0 : (int)blockIdx.x - bh * segs;
   const int b = bh / a.Hkv, h = bh - b * a.Hkv, t = threadIdx.x;
   const int lane = t & 63, wid = __builtin_amdgcn_readfirstlane(t >> 6);
+  // weights, state and length are on their way at once (the weights of all N slots are there)
+  const float* w = a.weights + b * a.sw_b + h * a.sw_h;
+  const int slot0 = seg * kSegSlots + wid * (ROUNDS * 64) + lane;
+  float x[ROUNDS];
+#pragma unroll
+  for (int j = 0; j < ROUNDS; ++j) {
+    const int i = slot0 + 64 * j;
+    x[j] = w[min(i, a.N - 1)];
+  }
   const int n = a.lens[b];
   if (n < 0 || n > a.N) return;
-  const float* w = a.weights + b * a.sw_b + h * a.sw_h;
   const int stay = min(n, a.keep);
   const bool all = n <= a.keep;
   const int lo = all ? n : a.sinks, hi = all ? n : n - a.recent;  // the slots between are chosen from
@@ -63,14 +71,6 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   // segments that hold slots of the sequence; the others have nothing to say
   const int used = ONE ? 1 : max(1, (n + kSegSlots - 1) / kSegSlots);
   if (seg >= used) return;
-  const int slot0 = seg * kSegSlots + wid * (ROUNDS * 64) + lane;
-
-  float x[ROUNDS];
-#pragma unroll
-  for (int j = 0; j < ROUNDS; ++j) {
-    const int i = slot0 + 64 * j;
-    x[j] = i < n ? w[i] : 0.f;
-  }
 
   auto shift_of = [](int p) { return p == 0 ? 21 : p == 1 ? 10 : 0; };
   auto mask_of = [](int p) { return p == 2 ? 1023u : 2047u; };
@@ -215,15 +215,19 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs a) {
   const int blocks = (a.keep + 4 * kCopyRows - 1) / (4 * kCopyRows);
   const int bh = (int)(blockIdx.x / (uint32_t)blocks), block = (int)blockIdx.x - bh * blocks, b = bh / a.Hkv, h = bh - b * a.Hkv;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = a.lens[b];
-  const int stay = min(n, a.keep), base = (block * 4 + wid) * kCopyRows;
-  if (n < 0 || n > a.N || base >= stay) return;
+  const int base = (block * 4 + wid) * kCopyRows;
+  if (base >= a.keep) return;
   const int part = lane & 15, row0 = base + (lane >> 4);
   const int32_t* kept = a.kept + (int64_t)bh * a.keep;
   constexpr int R = kCopyRows / 4;
   int slot[R];
 #pragma unroll
-  for (int i = 0; i < R; ++i) slot[i] = kept[min(row0 + 4 * i, stay - 1)];
+  for (int i = 0; i < R; ++i) slot[i] = kept[min(row0 + 4 * i, a.keep - 1)];
+  const int n = a.lens[b];
+  const int stay = min(n, a.keep);
+  if (n < 0 || n > a.N || base >= stay) return;
+#pragma unroll
+  for (int i = 0; i < R; ++i) slot[i] = max(slot[i], 0);  // (rows past the last one)
   int64_t page_out = b, at_out = row0;
   bool room = true;
   if (a.table_out) {
