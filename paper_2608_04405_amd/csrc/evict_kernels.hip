@@ -15,7 +15,7 @@
 // in neighbouring banks, for every fourth lane.
 //
 // Measured: 4096 slots 9.6 us in one launch, three rounds of count and scan; more slots
-// 7.6 (8 x 8 rows of 32749) to 9.1 us (4 x 8 of 131072) for each of four launches, most
+// 7.4 (8 x 8 rows of 32749) to 9.1 us (4 x 8 of 131072) for each of four launches, most
 // of it the way from length to weights to counters; a workgroup with 32768 slots, 32 a
 // thread, takes 57 us.  The copy of 8001 rows of 64 heads takes 101 to 114 us, 5.2 to 4.6
 // TB/s read and written, that of 65536 of 32 heads 409 to 430: a copy's rate.

@@ -20,8 +20,8 @@
 //
 // Measured with 32 heads (8 KV heads): 500 tokens of 2 requests over 32768 slots 0.20 ms,
 // 0.78 PFLOP/s of visible pairs, matrix units busy 33 % of the cycles, other vector
-// instructions 35 to 43 % (an exponential, a multiply-add and an addition a score: these
-// alone are as long as the products); one token over 16 x 65536 slots 0.30 ms, 5.5 TB/s
+// instructions 35 to 43 % (an exponential, a multiply-add and an addition a score; with
+// them spread evenly over the products it took as long); one token over 16 x 65536 slots 0.30 ms, 5.5 TB/s
 // (6.2 to 6.8 where no weight is written: reads and writes take turns at the memory).
 #include <algorithm>
 
