@@ -305,3 +305,20 @@ def test_wrong_device_and_stream():
         bpc.chunk_attention(q, K, K, zero, stream=3)
     with pytest.raises(bpc.BPCError, match="overlaps"):  # a cache is not cut in place
         bpc.evict_kv(K, K.clone(), torch.zeros(1, 1, 5, device=DEV), ints([5]), 3, K[:, :, :3], torch.zeros(1, 1, 3, 128, dtype=torch.bfloat16, device=DEV))
+
+
+@pytest.mark.parametrize("T", [1, 20, 100, 300])
+@pytest.mark.parametrize("N", [300, 5000])
+def test_sequences_without_new_tokens(T, N):
+    """No tokens: the slots before decay, nothing else changes; and chunks that end at the last slot, or one behind."""
+    q, K = dev(rand(1, 3, 8, T, 128)), dev(rand(2, 3, 2, N, 128))
+    lse, h = torch.full((3, 8, T), 5.0, device=DEV), N // 2
+    out, sums = torch.full((3, 8, T, 128), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((3, 8, T), 7.0, device=DEV)
+    pos, count = ints([h, 0, N + 1]), ints([0, -3, 0])
+    for decay in (0.5, 0.0):
+        w = bpc.key_weights(q, K, lse, torch.ones(3, 2, N, device=DEV), pos, count=count, decay=decay)
+        assert bool((w[0, :, :h] == decay).all()) and bool((w[0, :, h:] == 1).all()) and bool((w[1:] == 1).all())
+    bpc.chunk_attention(q, K, K, pos, count=count, out=out, lse_out=sums)
+    assert bool((out == 7).all()) and bool((sums == 7).all())
+    bpc.chunk_attention(q, K, K, ints([N - T, N - T + 1, -1]), out=out, lse_out=sums)
+    assert bool((out[1:] == 7).all()) and bool((sums[1:] == 7).all()) and bool((sums[0] != 7).all())
