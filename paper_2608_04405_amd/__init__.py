@@ -1084,21 +1084,21 @@ def chunk_cut(B: int, Hq: int, Hkv: int, T: int, N: int, window: int = 0, sinks:
     return row_blocks.value, pieces.value, bool(streamed.value)
 
 
-def _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, V=None, weights=None):
+def _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, V=None, Vs=None, weights=None):
     """(N, pages, page, table stride) of a call over a contiguous cache or pools
-    of pages, whose extents it checks; N: by default what they and the weights
-    hold."""
+    of pages, whose extents (Vs: V's first three) it checks; N: by default what they
+    and the weights hold."""
     most_weights = weights.shape[2] if isinstance(weights, torch.Tensor) and weights.dim() == 3 else 1 << 30
     if block_table is None:
         N = min(Kn, most_weights) if N is None else N
         if Kb != B or Kn < N:
             _extent(K, "K", (B, Hkv, ("ge", N), 128))
-        if V is not None and (V.shape[0] != B or V.shape[1] != Hkv or V.shape[2] < N):
+        if V is not None and (Vs[0] != B or Vs[1] != Hkv or Vs[2] < N):
             _extent(V, "V", (B, Hkv, ("ge", N), 128))
         pages = page = st = 0
     else:
         pages, page = Kb, Kn
-        if V is not None and V.shape[:3] != K.shape[:3]:
+        if V is not None and Vs != (pages, Hkv, page):
             _extent(V, "V", (pages, Hkv, page, 128))
         _page_rows(page)
         st, most = _block_table(block_table, B)
@@ -1111,11 +1111,9 @@ def _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, V=None, weights=None):
     return N, pages, page, st
 
 
-def _float_rows(t: Optional[torch.Tensor], name: str, B: int, H: int, n: int, more: bool, written: bool):
+def _float_rows(t: torch.Tensor, name: str, B: int, H: int, n: int, more: bool, written: bool):
     """(batch, head) strides of an fp32 [B, H, n] tensor (or wider, with `more`)
     with contiguous rows; rows that are written must not overlap."""
-    if t is None:
-        return 0, 0
     fits = False
     if type(t) is torch.Tensor and t.dtype is torch.float32 and t.dim() == 3:
         (b, h, m), (x, y, one) = t.shape, t.stride()
@@ -1134,9 +1132,11 @@ def _float_rows(t: Optional[torch.Tensor], name: str, B: int, H: int, n: int, mo
     return x if B > 1 else 0, y if H > 1 else 0
 
 
-def _window(window: int, sinks: int) -> None:
+def _window(window: int, sinks: int):
+    """Both, as the C entries take them."""
     if window < 0 or sinks < 0:
         raise ValueError(f"window={window} and sinks={sinks} must be >= 0")
+    return min(window, 1 << 30), min(sinks, 1 << 30)
 
 
 def chunk_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, pos: torch.Tensor, sm_scale: Optional[float] = None,
@@ -1160,11 +1160,15 @@ def chunk_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, pos: torc
     from count[b] on, and of a sequence whose slots are not all in [0, N), stay as
     they are (undefined where `out` is allocated here)."""
     B, Hq, Hkv, T, sq, so, Kb, Kn, sK, Vb, Vh, Vn, sV = _attn_inputs(q, K, V, slopes, out, workspace)
-    N, pages, page, st = _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, V)
-    _window(window, sinks)
+    N, pages, page, st = _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, V, (Vb, Vh, Vn))
+    if window or sinks:
+        window, sinks = _window(window, sinks)
     _indices(pos, "pos", (B,))
-    _indices(count, "count", (B,))
-    sl = _float_rows(lse_out, "lse_out", B, Hq, T, False, True)
+    if count is not None:
+        _indices(count, "count", (B,))
+    l_b = l_h = 0
+    if lse_out is not None:
+        l_b, l_h = _float_rows(lse_out, "lse_out", B, Hq, T, False, True)
     _on_gpu(q, K, V, pos, count, block_table, slopes, out, lse_out, workspace)
     dev = q.get_device()
     if stream is not None or dev != _current_device():
@@ -1180,7 +1184,7 @@ def chunk_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, pos: torc
     status = _lib.bpc_chunk_attention(
         q.data_ptr(), *sq, K.data_ptr(), *sK, V.data_ptr(), *sV, _ptr(block_table), st, pages, page, pos.data_ptr(),
         _ptr(count), B, Hq, Hkv, T, N, 128, _SM_SCALE if sm_scale is None else sm_scale, softcap, _ptr(slopes),
-        min(window, 1 << 30), min(sinks, 1 << 30), out.data_ptr(), *so, _ptr(lse_out), *sl, _ptr(workspace),
+        window, sinks, out.data_ptr(), *so, _ptr(lse_out), l_b, l_h, _ptr(workspace),
         0 if workspace is None else workspace.numel(), _current_stream(dev))
     if status:
         _check(status, "bpc_chunk_attention")
@@ -1200,19 +1204,21 @@ def key_weights(q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, weights: to
     count[b] on, and sequences whose slots are not all in [0, N), stay as they are
     (N: by default what the cache or the table, and the weights, hold).  Returns
     weights."""
-    B, Hq, T, *sq = _rows(q, "q")
-    Kb, Hkv, Kn, sK = _cache(K, "K")
+    B, Hq, T, q_b, q_h, q_t = _rows(q, "q")
+    Kb, Hkv, Kn, (K_b, K_h, K_n) = _cache(K, "K")
     if Hq % Hkv:
         raise ValueError(f"Hq={Hq} must be a multiple of Hkv={Hkv}")
     if slopes is not None:
         _need(slopes, "slopes", torch.float32, 1)
         _extent(slopes, "slopes", (Hq,))
-    N, pages, page, st = _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, None, weights)
-    _window(window, sinks)
+    N, pages, page, st = _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, weights=weights)
+    if window or sinks:
+        window, sinks = _window(window, sinks)
     _indices(pos, "pos", (B,))
-    _indices(count, "count", (B,))
-    sl = _float_rows(lse, "lse", B, Hq, T, False, False)
-    sw = _float_rows(weights, "weights", B, Hkv, N, True, True)
+    if count is not None:
+        _indices(count, "count", (B,))
+    l_b, l_h = _float_rows(lse, "lse", B, Hq, T, False, False)
+    w_b, w_h = _float_rows(weights, "weights", B, Hkv, N, True, True)
     _on_gpu(q, K, lse, weights, pos, count, block_table, slopes)
     dev = q.get_device()
     if stream is not None or dev != _current_device():
@@ -1220,9 +1226,9 @@ def key_weights(q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, weights: to
             return key_weights(q, K, lse, weights, pos, sm_scale, N, count=count, block_table=block_table, softcap=softcap,
                                slopes=slopes, window=window, sinks=sinks, decay=decay)
     status = _lib.bpc_key_weights(
-        q.data_ptr(), *sq, K.data_ptr(), *sK, lse.data_ptr(), *sl, weights.data_ptr(), *sw, _ptr(block_table), st, pages, page,
-        pos.data_ptr(), _ptr(count), B, Hq, Hkv, T, N, 128, _SM_SCALE if sm_scale is None else sm_scale, softcap,
-        _ptr(slopes), min(window, 1 << 30), min(sinks, 1 << 30), decay, _current_stream(dev))
+        q.data_ptr(), q_b, q_h, q_t, K.data_ptr(), K_b, K_h, K_n, lse.data_ptr(), l_b, l_h, weights.data_ptr(), w_b, w_h,
+        _ptr(block_table), st, pages, page, pos.data_ptr(), _ptr(count), B, Hq, Hkv, T, N, 128,
+        _SM_SCALE if sm_scale is None else sm_scale, softcap, _ptr(slopes), window, sinks, decay, _current_stream(dev))
     if status:
         _check(status, "bpc_key_weights")
     return weights
@@ -1254,19 +1260,20 @@ def evict_kv(K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, lens: torc
     weights, hold); one whose lens[b] is not in [0, N] is skipped (its slots in the
     result are undefined where that is allocated here).  The sequences' new lengths
     are lens.clamp(max=keep)."""
-    Kb, Hkv, Kn, sK = _cache(K, "K")
-    Vb, Vh, Vn, sV = _cache(V, "V")
-    _indices(lens, "lens", (lens.shape[0],) if isinstance(lens, torch.Tensor) and lens.dim() == 1 else (1,))
+    Kb, Hkv, Kn, (K_b, K_h, K_n) = _cache(K, "K")
+    Vb, Vh, Vn, (V_b, V_h, V_n) = _cache(V, "V")
+    if type(lens) is not torch.Tensor or lens.dtype is not torch.int32 or lens.dim() != 1 or not lens.is_contiguous():
+        _need(lens, "lens", torch.int32, 1)
     B = lens.shape[0]
     if Vh != Hkv:
         _extent(V, "V", (Vb, Hkv, Vn, 128))
-    N, pages, page, st = _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, V, weights)
+    N, pages, page, st = _paged_or_not(K, B, Hkv, Kb, Kn, N, block_table, V, (Vb, Vh, Vn), weights)
     if not 1 <= keep <= N:
         raise ValueError(f"keep={keep} must be in [1, N={N}]")
     if sinks < 0 or recent < 0 or sinks + recent > keep:
         raise ValueError(f"sinks={sinks} and recent={recent} must be >= 0, together at most keep={keep}")
-    Ob, Oh, On, sKo = _written(K_out, "K_out")
-    Pb, Ph, Pn, sVo = _written(V_out, "V_out")
+    Ob, Oh, On, (Ko_b, Ko_h, Ko_n) = _written(K_out, "K_out")
+    Pb, Ph, Pn, (Vo_b, Vo_h, Vo_n) = _written(V_out, "V_out")
     out_pages = out_page = sto = 0
     if table_out is None:
         if Ob != B or Oh != Hkv or On < keep:
@@ -1283,8 +1290,11 @@ def evict_kv(K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, lens: torc
         sto, most = _block_table(table_out, B)
         if most * out_page < keep:
             raise ValueError(f"table_out holds {most * out_page} slots per sequence, keep={keep}")
-    sw = _float_rows(weights, "weights", B, Hkv, N, True, False)
-    swo = _float_rows(weights_out, "weights_out", B, Hkv, keep, True, True)
+    w_b, w_h = _float_rows(weights, "weights", B, Hkv, N, True, False)
+    wo_b = wo_h = cap = 0
+    if weights_out is not None:
+        wo_b, wo_h = _float_rows(weights_out, "weights_out", B, Hkv, keep, True, True)
+        cap = weights_out.shape[2]
     if (codes is None) != (codes_out is None):
         raise ValueError("codes and codes_out are given together or not at all")
     W, sC, sCo = 0, (0, 0), (0, 0)
@@ -1297,7 +1307,8 @@ def evict_kv(K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, lens: torc
         _extent(codes, "codes", (B, Hkv, ("ge", N), W))
         _extent(codes_out, "codes_out", (B, Hkv, ("ge", keep), W))
         sC, sCo = (codes.stride(0), codes.stride(1)), (codes_out.stride(0), codes_out.stride(1))
-    _exact_out(kept_out, "kept_out", torch.int32, (B, Hkv, keep))
+    if kept_out is not None:
+        _exact_out(kept_out, "kept_out", torch.int32, (B, Hkv, keep))
     if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous uint8 tensor")
     _on_gpu(K, V, weights, lens, K_out, V_out, block_table, table_out, codes, codes_out, weights_out, kept_out, workspace)
@@ -1314,11 +1325,10 @@ def evict_kv(K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, lens: torc
         if need:
             workspace = lens.new_empty(need, dtype=torch.uint8)
     status = _lib.bpc_evict_kv(
-        K.data_ptr(), *sK, V.data_ptr(), *sV, _ptr(block_table), st, pages, page, weights.data_ptr(), *sw, lens.data_ptr(),
-        B, Hkv, N, 128, keep, sinks, recent, K_out.data_ptr(), *sKo, V_out.data_ptr(), *sVo, _ptr(table_out), sto, out_pages,
-        out_page, _ptr(codes), *sC, _ptr(codes_out), *sCo, W, _ptr(weights_out), *swo,
-        0 if weights_out is None else weights_out.shape[2], kept_out.data_ptr(), _ptr(workspace),
-        0 if workspace is None else workspace.numel(), _current_stream(dev))
+        K.data_ptr(), K_b, K_h, K_n, V.data_ptr(), V_b, V_h, V_n, _ptr(block_table), st, pages, page, weights.data_ptr(), w_b, w_h,
+        lens.data_ptr(), B, Hkv, N, 128, keep, sinks, recent, K_out.data_ptr(), Ko_b, Ko_h, Ko_n, V_out.data_ptr(), Vo_b, Vo_h, Vo_n,
+        _ptr(table_out), sto, out_pages, out_page, _ptr(codes), *sC, _ptr(codes_out), *sCo, W, _ptr(weights_out), wo_b, wo_h, cap,
+        kept_out.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(), _current_stream(dev))
     if status:
         _check(status, "bpc_evict_kv")
     return kept_out
