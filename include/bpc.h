@@ -743,7 +743,8 @@ int bpc_chunk_cut(int B, int Hq, int Hkv, int T, int N, int D, int window, int s
  *            another argument.
  * decay      finite, >= 0; 1 adds to what is there
  * fp32 scores, exponentials and sums; equal calls give equal bits.  A sum over many
- * tokens loses no more than its last rounding and those of 16 terms at a time.
+ * tokens loses no more than its last rounding and those of 16 terms at a time; one
+ * past fp32's range (of an lse that is not of these tokens) is infinite.
  * No workspace; one kernel launch.
  */
 int bpc_key_weights(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,

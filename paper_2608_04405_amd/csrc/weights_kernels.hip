@@ -327,7 +327,8 @@ __global__ __launch_bounds__(kWeightThreads, 2) void key_weights_kernel(WeightAr
 #pragma unroll
   for (int k = 0; k < KB; ++k) {
     const int n = n_wave + 32 * k + col;
-    const float x = sum_halves(sum[k] + lost[k]);
+    // (what an infinite sum lost is not a number)
+    const float x = sum_halves(fabsf(sum[k]) < INFINITY ? sum[k] + lost[k] : sum[k]);
     const float base = a.decay != 0.f ? a.decay * old[k] : 0.f;
     if (half == 0 && n < khi) wp[n] = base + ((bad >> (2 * k + (col >> 4)) & 1) ? 0.f : x);
   }
