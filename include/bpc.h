@@ -698,7 +698,8 @@ int bpc_attention_cut(int B, int Hq, int Hkv, int T, int N, int D, int tree,
  * sinks      first slots that stay visible (ignored without a window)
  * sm_scale, softcap, slopes, out  as in bpc_prefill_attention
  * lse        [B, Hq, T] fp32, strides (sl_b, sl_h), or NULL (written).  Its rows
- *            overlap neither one another nor another argument.
+ *            overlap neither one another nor another argument.  (out, lse and the
+ *            workspace are refused where they do.)
  * workspace  at least bpc_chunk_workspace_bytes(...) bytes, as in
  *            bpc_prefill_attention, whose limits hold here too
  */

@@ -646,6 +646,84 @@ static int check_separate(const RowSet& out, const RowSet& in, bool strict = fal
   return (alike ? rows_meet(away, d, dims) : strict) ? fail(BPC_EINVAL, "%s overlaps %s", out.name, in.name) : BPC_OK;
 }
 
+// Memory that an argument covers: rows of `row` bytes, `stride` bytes apart along up to
+// three dimensions.
+struct Region {
+  const char* name;
+  uintptr_t p;
+  int64_t row;
+  int dims = 0;
+  int64_t stride[3], extent[3];
+  uint64_t span;  // to the end of the last row
+
+  Region(const char* name, const void* p, int64_t row) : name(name), p(reinterpret_cast<uintptr_t>(p)), row(row), span(row) {}
+  // (the smallest strides first; rows that follow one another are one)
+  Region& by(int64_t bytes, int64_t count) {
+    if (count < 2 || !bytes) return *this;
+    span += (uint64_t)bytes * (uint64_t)(count - 1);
+    int i = dims++;
+    for (; i && stride[i - 1] > bytes; --i) stride[i] = stride[i - 1], extent[i] = extent[i - 1];
+    stride[i] = bytes, extent[i] = count;
+    while (dims && stride[0] == row) {
+      row *= extent[0], --dims;
+      for (int k = 0; k < dims; ++k) stride[k] = stride[k + 1], extent[k] = extent[k + 1];
+    }
+    return *this;
+  }
+};
+static Region bf16_rows(const char* name, const void* p, int64_t sb, int64_t sh, int64_t st, int64_t B, int64_t H, int64_t T) {
+  return Region(name, p, 2 * kHeadDim).by(2 * st, T).by(2 * sh, H).by(2 * sb, B);
+}
+static Region float_rows(const char* name, const void* p, int64_t sb, int64_t sh, int64_t B, int64_t H, int64_t len) {
+  return Region(name, p, 4 * len).by(4 * sh, H).by(4 * sb, B);
+}
+
+// Whether some steps along the dimensions, each first to last of its strides, take
+// `away` to a place between -below and above.  No more than `budget` steps are tried.
+struct Steps {
+  int64_t stride, first, last;
+};
+static bool steps_meet(__int128 away, const Steps* d, int dims, int64_t below, int64_t above, int& budget) {
+  if (!dims) return away > -below && away < above;
+  __int128 least = 0, most = 0;  // of the later dimensions
+  for (int i = 1; i < dims; ++i) least += (__int128)d[i].stride * d[i].first, most += (__int128)d[i].stride * d[i].last;
+  const auto floor_div = [](__int128 x, int64_t y) { return x / y - (x % y < 0); };
+  const __int128 from = floor_div(away - above - most, d->stride) + 1, to = floor_div(away + below - least - 1, d->stride);
+  if (from > d->last || to < d->first) return false;
+  const int64_t x0 = from > d->first ? (int64_t)from : d->first, x1 = to < d->last ? (int64_t)to : d->last;
+  for (int64_t x = x0; x <= x1 && budget > 0; ++x)
+    if (--budget, steps_meet(away - (__int128)x * d->stride, d + 1, dims - 1, below, above, budget)) return true;
+  return false;
+}
+
+// Whether two regions have a byte in common: exactly, but for strides so unlike that it
+// would take thousands of steps to tell.
+static bool regions_meet(const Region& x, const Region& y) {
+  if (!x.p || !y.p || x.p >= y.p + y.span || y.p >= x.p + x.span) return false;
+  Steps d[6];
+  int dims = 0, i = x.dims, j = y.dims;
+  while (i || j) {  // the largest strides first
+    const int64_t sx = i ? x.stride[i - 1] : 0, sy = j ? y.stride[j - 1] : 0;
+    Steps& s = d[dims++];
+    s = {std::max(sx, sy), 0, 0};
+    if (sx == s.stride) s.last = x.extent[--i] - 1;
+    if (sy == s.stride) s.first = 1 - y.extent[--j];
+  }
+  int budget = 1 << 12;
+  return steps_meet((__int128)y.p - (__int128)x.p, d, dims, y.row, x.row, budget);
+}
+
+// What is written shares no memory with anything else.
+static int check_regions(const Region* wrote, int writes, const Region* read, int reads) {
+  for (int i = 0; i < writes; ++i) {
+    for (int j = i + 1; j < writes; ++j)
+      if (regions_meet(wrote[i], wrote[j])) return fail(BPC_EINVAL, "%s overlaps %s", wrote[i].name, wrote[j].name);
+    for (int j = 0; j < reads; ++j)
+      if (regions_meet(wrote[i], read[j])) return fail(BPC_EINVAL, "%s overlaps %s", wrote[i].name, read[j].name);
+  }
+  return BPC_OK;
+}
+
 static int check_rotation(const float* cos_sin, int table_rows, int R) {
   if (R < 0 || R > kHeadDim || R % 16) return fail(BPC_EINVAL, "R=%d must be a multiple of 16, 0 to 128", R);
   if (R == 0) return BPC_OK;
@@ -971,6 +1049,10 @@ static int check_table(AttnArgs& a, const int32_t* block_table, int64_t st_b, in
   return BPC_OK;
 }
 
+static Region table_region(const int32_t* block_table, int64_t st_b, int B, int N, int page_size) {
+  return Region("block_table", block_table, block_table ? 4 * (((int64_t)N + page_size - 1) / page_size) : 0).by(4 * st_b, B);
+}
+
 size_t bpc_chunk_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D, int window, int sinks) {
   if (window < 0 || sinks < 0 || !attn_sizes_ok(B, Hq, Hkv, T, N, D)) return 0;
   return chunk_plan(B, Hkv, Hq / Hkv, T, N, std::min(window, kMaxWindow), std::min(sinks, kMaxWindow)).total;
@@ -1027,6 +1109,13 @@ int bpc_chunk_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t s
   if ((st = check_apart("out", so_b, so_h, so_t, B, Hq, T))) return st;
   if (lse && (st = check_floats("lse", lse, sl_b, sl_h))) return st;
   if (lse && (st = check_floats_apart("lse", sl_b, sl_h, B, Hq, T))) return st;
+  const int64_t places = block_table ? num_pages : B, rows = block_table ? page_size : N;
+  const Region wrote[3] = {bf16_rows("out", out, so_b, so_h, so_t, B, Hq, T), float_rows("lse", lse, sl_b, sl_h, B, Hq, T),
+                           Region("workspace", plan.total ? workspace : nullptr, (int64_t)plan.total)};
+  const Region read[7] = {bf16_rows("q", q, sq_b, sq_h, sq_t, B, Hq, T), bf16_rows("K", K, sK_b, sK_h, sK_n, places, Hkv, rows),
+                          bf16_rows("V", V, sV_b, sV_h, sV_n, places, Hkv, rows), table_region(block_table, st_b, B, N, page_size),
+                          Region("pos", pos, 4 * (int64_t)B), Region("count", count, 4 * (int64_t)B), Region("slopes", slopes, 4 * (int64_t)Hq)};
+  if ((st = check_regions(wrote, 3, read, 7))) return st;
   attn_workspace(a, plan, workspace);
   if (plan.total) a.part_e = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.off_e);
   hipError_t e = launch_chunk(a, plan);
