@@ -741,7 +741,7 @@ int bpc_chunk_cut(int B, int Hq, int Hkv, int T, int N, int D, int window, int s
  * lse        [B, Hq, T] fp32, strides (sl_b, sl_h)
  * weights    [B, Hkv, >=N] fp32, strides (sw_b, sw_h) (read and written; with
  *            decay 0 written only).  Its rows overlap neither one another nor
- *            another argument.
+ *            another argument (refused).
  * decay      finite, >= 0; 1 adds to what is there
  * fp32 scores, exponentials and sums; equal calls give equal bits.  A sum over many
  * tokens loses no more than its last rounding and those of 16 terms at a time; one

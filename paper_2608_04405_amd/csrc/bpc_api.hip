@@ -1146,6 +1146,12 @@ int bpc_key_weights(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
   AttnArgs pages{};
   if ((st = check_table(pages, block_table, st_b, num_pages, page_size))) return st;
   if (!launchable(weights_blocks(B, Hkv, N), 256)) return fail(BPC_EUNSUPPORTED, "B Hkv N: too many slots in one call");
+  const int64_t places = block_table ? num_pages : B, rows = block_table ? page_size : N;
+  const Region wrote[1] = {float_rows("weights", weights, sw_b, sw_h, B, Hkv, N)};
+  const Region read[7] = {bf16_rows("q", q, sq_b, sq_h, sq_t, B, Hq, T), bf16_rows("K", K, sK_b, sK_h, sK_n, places, Hkv, rows),
+                          float_rows("lse", lse, sl_b, sl_h, B, Hq, T), table_region(block_table, st_b, B, N, page_size),
+                          Region("pos", pos, 4 * (int64_t)B), Region("count", count, 4 * (int64_t)B), Region("slopes", slopes, 4 * (int64_t)Hq)};
+  if ((st = check_regions(wrote, 1, read, 7))) return st;
   WeightArgs a{};
   a.q = q, a.sq_b = sq_b, a.sq_h = sq_h, a.sq_t = sq_t;
   a.K = K, a.sK_b = sK_b, a.sK_h = sK_h, a.sK_n = sK_n;

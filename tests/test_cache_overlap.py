@@ -1,11 +1,11 @@
-"""What chunk_attention writes shares no memory with anything else, on the CPU (fake
-pointers; every call fails a check)."""
+"""What chunk_attention and key_weights write shares no memory with anything else, on
+the CPU (fake pointers; every call fails a check)."""
 
 import random
 
 import pytest
 
-from test_cache_refusals import CHUNK
+from test_cache_refusals import CHUNK, WEIGHTS
 from test_rows_and_attn_refusals import EINVAL, call, lib, pytestmark  # noqa: F401
 
 FAR = 1 << 40  # further than any argument here reaches
@@ -102,3 +102,28 @@ def test_chunk_results_in_any_layout(lib):
         assert got == want, (case, o, s, away)
         met += want
     assert 100 < met < 350, met
+
+
+WEIGHTS_GOOD = dict(SIZES, **{k: v for k, v in DENSE.items() if k[:2] in ("q_", "K_")}, **apart(["q", "K", "pos", "count", "slopes", "lse", "w"]), table=None,
+                    lse_b=40, lse_h=5, w_b=10000, w_h=5000)
+
+
+@pytest.mark.parametrize("name,bytes", [("q", 20480), ("K", 5120000), ("pos", 8), ("count", 8), ("slopes", 32), ("lse", LSE)])
+def test_weights_refuse_inputs(lib, name, bytes):
+    for at in (WEIGHTS_GOOD[name], WEIGHTS_GOOD[name] + bytes - 4, WEIGHTS_GOOD[name] - 79996):
+        refused(lib, "bpc_key_weights", WEIGHTS, dict(WEIGHTS_GOOD, w=at), "weights", name)
+
+
+def test_weights_refuse_pools_and_tables(lib):
+    pool = {k: v for k, v in POOL.items() if k[0] != "V"}
+    for name, at in (("K", WEIGHTS_GOOD["K"] + 900 * 8192 - 16), ("block_table", pool["table"] + 4 * (400 + 312))):
+        refused(lib, "bpc_key_weights", WEIGHTS, dict(WEIGHTS_GOOD, **pool, w=at), "weights", name)
+
+
+def test_weights_take_what_lies_between(lib):
+    """The log-sums of a head behind its weights, in one buffer; the call then fails at the lengths."""
+    at = WEIGHTS_GOOD["w"]
+    spaced = dict(WEIGHTS_GOOD, B=1, Hq=2, w_h=5008, lse_h=5008, pos=at + 4 * 4999)
+    refused(lib, "bpc_key_weights", WEIGHTS, dict(spaced, lse=at + 4 * 5000), "weights", "pos")
+    refused(lib, "bpc_key_weights", WEIGHTS, dict(spaced, lse=at + 4 * 4999), "weights", "lse")
+    refused(lib, "bpc_key_weights", WEIGHTS, dict(spaced, lse=at + 4 * 5004), "weights", "lse")
