@@ -786,7 +786,8 @@ int bpc_key_weights(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
  *            bpc_build_hash, W 1, 2 or 4, or both NULL
  * weights_out [B, Hkv, cap] fp32, strides (swo_b, swo_h), cap >= keep, or NULL
  * kept       [B, Hkv, keep] int32 contiguous
- * No output's range of addresses meets another's or an input's (K and V: above).
+ * No output's range of addresses meets another's or an input's (K and V: above);
+ * memory in common is refused.
  * workspace  at least bpc_evict_workspace_bytes(...) bytes (may be 0), 256-byte
  *            aligned; its contents on entry do not matter.
  */

@@ -1049,8 +1049,8 @@ static int check_table(AttnArgs& a, const int32_t* block_table, int64_t st_b, in
   return BPC_OK;
 }
 
-static Region table_region(const int32_t* block_table, int64_t st_b, int B, int N, int page_size) {
-  return Region("block_table", block_table, block_table ? 4 * (((int64_t)N + page_size - 1) / page_size) : 0).by(4 * st_b, B);
+static Region table_region(const char* name, const int32_t* table, int64_t st_b, int B, int N, int page_size) {
+  return Region(name, table, table ? 4 * (((int64_t)N + page_size - 1) / page_size) : 0).by(4 * st_b, B);
 }
 
 size_t bpc_chunk_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D, int window, int sinks) {
@@ -1113,7 +1113,7 @@ int bpc_chunk_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t s
   const Region wrote[3] = {bf16_rows("out", out, so_b, so_h, so_t, B, Hq, T), float_rows("lse", lse, sl_b, sl_h, B, Hq, T),
                            Region("workspace", plan.total ? workspace : nullptr, (int64_t)plan.total)};
   const Region read[7] = {bf16_rows("q", q, sq_b, sq_h, sq_t, B, Hq, T), bf16_rows("K", K, sK_b, sK_h, sK_n, places, Hkv, rows),
-                          bf16_rows("V", V, sV_b, sV_h, sV_n, places, Hkv, rows), table_region(block_table, st_b, B, N, page_size),
+                          bf16_rows("V", V, sV_b, sV_h, sV_n, places, Hkv, rows), table_region("block_table", block_table, st_b, B, N, page_size),
                           Region("pos", pos, 4 * (int64_t)B), Region("count", count, 4 * (int64_t)B), Region("slopes", slopes, 4 * (int64_t)Hq)};
   if ((st = check_regions(wrote, 3, read, 7))) return st;
   attn_workspace(a, plan, workspace);
@@ -1149,7 +1149,7 @@ int bpc_key_weights(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
   const int64_t places = block_table ? num_pages : B, rows = block_table ? page_size : N;
   const Region wrote[1] = {float_rows("weights", weights, sw_b, sw_h, B, Hkv, N)};
   const Region read[7] = {bf16_rows("q", q, sq_b, sq_h, sq_t, B, Hq, T), bf16_rows("K", K, sK_b, sK_h, sK_n, places, Hkv, rows),
-                          float_rows("lse", lse, sl_b, sl_h, B, Hq, T), table_region(block_table, st_b, B, N, page_size),
+                          float_rows("lse", lse, sl_b, sl_h, B, Hq, T), table_region("block_table", block_table, st_b, B, N, page_size),
                           Region("pos", pos, 4 * (int64_t)B), Region("count", count, 4 * (int64_t)B), Region("slopes", slopes, 4 * (int64_t)Hq)};
   if ((st = check_regions(wrote, 1, read, 7))) return st;
   WeightArgs a{};
@@ -1249,6 +1249,16 @@ int bpc_evict_kv(const uint16_t* K, int64_t sK_b, int64_t sK_h, int64_t sK_n, co
       return fail(BPC_EWORKSPACE, "workspace of %zu bytes given, %zu needed", workspace ? workspace_bytes : 0, need);
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(BPC_EALIGN, "workspace must be 256-byte aligned");
   }
+  // (K_out and V_out against K, V and one another: above)
+  const Region rows_out[2] = {bf16_rows("K_out", K_out, sKo_b, sKo_h, sKo_n, out_B, Hkv, out_N), bf16_rows("V_out", V_out, sVo_b, sVo_h, sVo_n, out_B, Hkv, out_N)};
+  const Region given[9] = {float_rows("weights", weights, sw_b, sw_h, B, Hkv, N), Region("lens", lens, 4 * (int64_t)B),
+                           float_rows("codes", codes, sC_b, sC_h, B, Hkv, (int64_t)N * W), table_region("block_table", block_table, st_b, B, N, page_size),
+                           table_region("table_out", table_out, sto_b, B, keep, out_page_size),
+                           bf16_rows("K", K, sK_b, sK_h, sK_n, in_B, Hkv, in_N), bf16_rows("V", V, sV_b, sV_h, sV_n, in_B, Hkv, in_N), rows_out[0], rows_out[1]};
+  const Region results[4] = {Region("kept", kept, 4 * (int64_t)B * Hkv * keep), float_rows("weights_out", weights_out, swo_b, swo_h, B, Hkv, cap),
+                             float_rows("codes_out", codes_out, sCo_b, sCo_h, B, Hkv, (int64_t)keep * W), Region("workspace", need ? workspace : nullptr, (int64_t)need)};
+  if ((st = check_regions(rows_out, 2, given, 5))) return st;
+  if ((st = check_regions(results, 4, given, 9))) return st;
   EvictArgs a{};
   a.K = K, a.sK_b = sK_b, a.sK_h = sK_h, a.sK_n = sK_n, a.V = V, a.sV_b = sV_b, a.sV_h = sV_h, a.sV_n = sV_n;
   a.table = from.table, a.st_b = from.st_b, a.num_pages = from.num_pages, a.page_shift = from.page_shift;

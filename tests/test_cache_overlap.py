@@ -1,11 +1,11 @@
-"""What chunk_attention and key_weights write shares no memory with anything else, on
-the CPU (fake pointers; every call fails a check)."""
+"""What chunk_attention, key_weights and evict_kv write shares no memory with anything
+else, on the CPU (fake pointers; every call fails a check)."""
 
 import random
 
 import pytest
 
-from test_cache_refusals import CHUNK, WEIGHTS
+from test_cache_refusals import CHUNK, CODES, EVICT, WEIGHTS
 from test_rows_and_attn_refusals import EINVAL, call, lib, pytestmark  # noqa: F401
 
 FAR = 1 << 40  # further than any argument here reaches
@@ -127,3 +127,31 @@ def test_weights_take_what_lies_between(lib):
     refused(lib, "bpc_key_weights", WEIGHTS, dict(spaced, lse=at + 4 * 5000), "weights", "pos")
     refused(lib, "bpc_key_weights", WEIGHTS, dict(spaced, lse=at + 4 * 4999), "weights", "lse")
     refused(lib, "bpc_key_weights", WEIGHTS, dict(spaced, lse=at + 4 * 5004), "weights", "lse")
+
+
+# K, V, weights, lens, K_out, V_out, kept, codes, codes_out at 0, 2, 3 .. 9 (EVICT's own), then:
+EVICT_GOOD = dict(CODES, K=FAR, wo=10 * FAR, to=11 * FAR, sto=70, opages=900, opage=16, Ko_b=4096, Ko_h=2048, Vo_b=4096, Vo_h=2048)
+AT = dict(K=FAR, V=2 * FAR, weights=3 * FAR, lens=4 * FAR, K_out=5 * FAR, V_out=6 * FAR, kept=7 * FAR, codes=8 * FAR,
+          table_out=11 * FAR)
+POOLS = dict(POOL, K=FAR)
+
+
+@pytest.mark.parametrize("result,word", [("Ko", "K_out"), ("Vo", "V_out")])
+@pytest.mark.parametrize("name,bytes", [("weights", 80000), ("lens", 8), ("codes", 160000), ("table_out", 4 * (70 + 63))])
+def test_evict_refuses_rows_on_its_inputs(lib, result, word, name, bytes):
+    for at in (AT[name], AT[name] + (bytes - 1) // 16 * 16, AT[name] - 900 * 8192 + 16):
+        refused(lib, "bpc_evict_kv", EVICT, dict(EVICT_GOOD, **{result: at}), word, name)
+    refused(lib, "bpc_evict_kv", EVICT, dict(EVICT_GOOD, **dict(POOLS, table=AT["K_out"] + 900 * 8192 - 4)), "K_out", "block_table")
+
+
+@pytest.mark.parametrize("result,word", [("wo", "weights_out"), ("co", "codes_out"), ("kept", "kept")])
+@pytest.mark.parametrize("name,bytes", [("K", 5120000), ("V", 5120000), ("K_out", 900 * 8192), ("V_out", 900 * 8192), ("table_out", 4 * (70 + 63))])
+def test_evict_refuses_results_on_rows_and_tables(lib, result, word, name, bytes):
+    for at in (AT[name], AT[name] + (bytes - 1) // 16 * 16):
+        refused(lib, "bpc_evict_kv", EVICT, dict(EVICT_GOOD, **{result: at}), word, name)
+
+
+def test_evict_refuses_a_workspace_on_anything(lib):
+    need = dict(EVICT_GOOD, N=50000, K_h=50000 * 128, K_b=10 ** 8, V_h=50000 * 128, V_b=10 ** 8, w_h=50000, w_b=10 ** 5, C_h=10 ** 5, C_b=2 * 10 ** 5, wsb=1 << 40)
+    for name, at in AT.items():
+        refused(lib, "bpc_evict_kv", EVICT, dict(need, ws=at), name, "workspace")
