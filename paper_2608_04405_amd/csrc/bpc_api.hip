@@ -657,18 +657,25 @@ struct Region {
   uint64_t span;  // to the end of the last row
 
   Region(const char* name, const void* p, int64_t row) : name(name), p(reinterpret_cast<uintptr_t>(p)), row(row), span(row) {}
-  // (the smallest strides first; rows that follow one another are one)
   Region& by(int64_t bytes, int64_t count) {
     if (count < 2 || !bytes) return *this;
+    stride[dims] = bytes, extent[dims++] = count;
     span += (uint64_t)bytes * (uint64_t)(count - 1);
-    int i = dims++;
-    for (; i && stride[i - 1] > bytes; --i) stride[i] = stride[i - 1], extent[i] = extent[i - 1];
-    stride[i] = bytes, extent[i] = count;
-    while (dims && stride[0] == row) {
-      row *= extent[0], --dims;
-      for (int k = 0; k < dims; ++k) stride[k] = stride[k + 1], extent[k] = extent[k + 1];
-    }
     return *this;
+  }
+  // The same bytes with the smallest strides first, rows that follow one another as one.
+  Region sorted() const {
+    Region r(name, reinterpret_cast<const void*>(p), row);
+    for (int i = 0; i < dims; ++i) {
+      int k = r.dims++;
+      for (; k && r.stride[k - 1] > stride[i]; --k) r.stride[k] = r.stride[k - 1], r.extent[k] = r.extent[k - 1];
+      r.stride[k] = stride[i], r.extent[k] = extent[i];
+    }
+    while (r.dims && r.stride[0] == r.row) {
+      r.row *= r.extent[0], --r.dims;
+      for (int k = 0; k < r.dims; ++k) r.stride[k] = r.stride[k + 1], r.extent[k] = r.extent[k + 1];
+    }
+    return r;
   }
 };
 static Region bf16_rows(const char* name, const void* p, int64_t sb, int64_t sh, int64_t st, int64_t B, int64_t H, int64_t T) {
@@ -698,8 +705,9 @@ static bool steps_meet(__int128 away, const Steps* d, int dims, int64_t below, i
 
 // Whether two regions have a byte in common: exactly, but for strides so unlike that it
 // would take thousands of steps to tell.
-static bool regions_meet(const Region& x, const Region& y) {
-  if (!x.p || !y.p || x.p >= y.p + y.span || y.p >= x.p + x.span) return false;
+static bool regions_meet(const Region& a, const Region& b) {
+  if (!a.p || !b.p || a.p >= b.p + b.span || b.p >= a.p + a.span) return false;
+  const Region x = a.sorted(), y = b.sorted();
   Steps d[6];
   int dims = 0, i = x.dims, j = y.dims;
   while (i || j) {  // the largest strides first
