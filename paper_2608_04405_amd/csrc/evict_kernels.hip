@@ -44,7 +44,8 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 template <bool ONE, int ROUNDS>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a, int pass) {
   constexpr int NW = kSelectThreads / 64;
-  __shared__ uint32_t hist[kSelectBins * kCopies];
+  __shared__ __attribute__((aligned(16))) uint32_t hist[kSelectBins * kCopies];
+  static_assert(__alignof__(hist) >= alignof(uint4), "cleared and read 16 bytes at a time");
   __shared__ int wave_tot[NW];
   __shared__ int found[4];
   __shared__ int2 wave_cnt[NW];
