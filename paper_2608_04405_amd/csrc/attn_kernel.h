@@ -216,7 +216,7 @@ __global__ __launch_bounds__(RB* KW * 64, KW > 1 ? 1 : 2) void attn_kernel(AttnA
   constexpr int NB = KT / 32;   // 32-key blocks of a tile
   constexpr int RPW = KT / RB;  // rows of a tile's K (and V) that a wavefront copies
   static_assert(RPW % 4 == 0, "a copy moves four rows");
-  extern __shared__ char smem[];
+  extern __shared__ __attribute__((aligned(64))) char smem[];  // (the halves of V's operands are an exclusive or of 32 apart)
   __shared__ uint64_t odd_rows[2][RB * KW];
   __shared__ int draft_place[TREE && BIAS ? 64 : 1];
   // Consecutive workgroups go to different XCDs.  A prefill gives each XCD a run
