@@ -396,6 +396,7 @@ struct EvictArgs {
   int cap;
   int32_t* kept;
   uint32_t* counts;  // [B, Hkv][segs] digits' counts of a segment of slots, and its state
+  uint32_t* totals;  // [B, Hkv] counts of a digit in all segments, or NULL: each workgroup adds them up
   int segs;
   hipStream_t stream;
 };

@@ -10,7 +10,8 @@
 // and counts its keys' digits in LDS.  Up to one segment it finds all three digits
 // and writes the slots by itself; else there is a launch for each digit, whose
 // workgroups all add up what the one before counted, in the order of the segments,
-// so that each knows how many slots before its own stay as well.  Weights of a
+// so that each knows how many slots before its own stay as well (of many segments a launch
+// between the two adds up).  Weights of a
 // kind have few exponents, so the first digit's counters are few: four of each,
 // in neighbouring banks, for every fourth lane.
 //
@@ -110,11 +111,17 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
       top = counted(bin_top), low = counted(bin_low);
     } else {
       const uint32_t* c = counts + p * kSelectBins + bin_low;
+      if (a.totals) {
+        const uint2 v = *reinterpret_cast<const uint2*>(c + (int64_t)seg * kSegWords);
+        const uint2 all = *reinterpret_cast<const uint2*>(a.totals + (int64_t)bh * kSelectBins + bin_low);
+        pre_top = (int)v.y, pre_low = (int)v.x, top = (int)all.y, low = (int)all.x;
+      } else {
 #pragma unroll 8
-      for (int s = 0; s < used; ++s) {
-        const uint2 v = *reinterpret_cast<const uint2*>(c + (int64_t)s * kSegWords);
-        if (s < seg) pre_top += (int)v.y, pre_low += (int)v.x;
-        top += (int)v.y, low += (int)v.x;
+        for (int s = 0; s < used; ++s) {
+          const uint2 v = *reinterpret_cast<const uint2*>(c + (int64_t)s * kSegWords);
+          if (s < seg) pre_top += (int)v.y, pre_low += (int)v.x;
+          top += (int)v.y, low += (int)v.x;
+        }
       }
     }
     if (t < 4) found[t] = 0;
@@ -207,6 +214,29 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   }
 }
 
+// Many segments: their counters of a digit added up once, a thread a counter, to those
+// of the segments before each and of all.
+constexpr int kTotalThreads = 256;
+__global__ __launch_bounds__(kTotalThreads) void evict_totals_kernel(EvictArgs a, int pass) {
+  constexpr int kBlocks = kSelectBins / kTotalThreads, R = 16;
+  const int bh = (int)(blockIdx.x / kBlocks), bin = (int)(blockIdx.x % kBlocks) * kTotalThreads + threadIdx.x;
+  const int n = a.lens[bh / a.Hkv];
+  if (n <= a.keep || n > a.N || a.keep == a.sinks + a.recent) return;
+  const int used = (n + kSegSlots - 1) / kSegSlots;
+  uint32_t* c = a.counts + (int64_t)bh * a.segs * kSegWords + pass * kSelectBins + bin;
+  uint32_t before = 0u;
+  for (int s0 = 0; s0 < used; s0 += R) {
+    uint32_t x[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) x[i] = c[(int64_t)min(s0 + i, used - 1) * kSegWords];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (s0 + i < used) c[(int64_t)(s0 + i) * kSegWords] = before, before += x[i];
+    }
+  }
+  a.totals[(int64_t)bh * kSelectBins + bin] = before;
+}
+
 // The rows that stay.  A wavefront moves 16 of each tensor, 16 lanes a row, all
 // under way at once; the 16 rows written lie in one page.
 constexpr int kCopyRows = 16;
@@ -278,9 +308,16 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(EvictArgs a) {
 
 int evict_segments(int N) { return (N + kSegSlots - 1) / kSegSlots; }
 
+// Whether the segments' counters are added up by launches of their own.  Where each
+// workgroup adds up all of them, the work grows with the square of the segments: 8, 32, 64,
+// 128 and 256 segments of 8 heads take 38, 52, 110, 288 and 884 us, with three launches more
+// 42, 53, 88, 156 and 286; of 32 heads 50, 169, 394 and 1321 (up to 128), and 54, 143, 250 and 510.
+static bool evict_adds_up(int segs) { return segs >= 32; }
+
 size_t evict_workspace(int B, int Hkv, int N) {
   const int segs = evict_segments(N);
-  return segs == 1 ? 0 : (size_t)B * Hkv * segs * kSegWords * sizeof(uint32_t);
+  const size_t bh = (size_t)B * Hkv;
+  return segs == 1 ? 0 : (bh * segs * kSegWords + (evict_adds_up(segs) ? bh * kSelectBins : 0)) * sizeof(uint32_t);
 }
 
 hipError_t launch_evict(EvictArgs a) {
@@ -290,7 +327,11 @@ hipError_t launch_evict(EvictArgs a) {
     auto* f = a.N <= 4 * kSelectThreads ? evict_select_kernel<true, 4> : evict_select_kernel<true, kSelectRounds>;
     f<<<bh, kSelectThreads, 0, a.stream>>>(a, 0);
   } else {
-    for (int pass = 0; pass < 4; ++pass) evict_select_kernel<false, kSelectRounds><<<bh * a.segs, kSelectThreads, 0, a.stream>>>(a, pass);
+    a.totals = evict_adds_up(a.segs) ? a.counts + (int64_t)bh * a.segs * kSegWords : nullptr;
+    for (int pass = 0; pass < 4; ++pass) {
+      evict_select_kernel<false, kSelectRounds><<<bh * a.segs, kSelectThreads, 0, a.stream>>>(a, pass);
+      if (a.totals && pass < 3) evict_totals_kernel<<<bh * (kSelectBins / kTotalThreads), kTotalThreads, 0, a.stream>>>(a, pass);
+    }
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
