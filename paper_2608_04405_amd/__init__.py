@@ -1072,15 +1072,20 @@ def tree_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torc
     return out
 
 
+def _slots(n: int) -> int:
+    """A window or a number of first slots, as the C entries take it: slots are below 2^30."""
+    return max(-1, min(n, 1 << 30))
+
+
 @functools.lru_cache(maxsize=4096)
 def chunk_workspace_bytes(B: int, Hq: int, Hkv: int, T: int, N: int, window: int = 0, sinks: int = 0, D: int = 128) -> int:
-    return int(_lib.bpc_chunk_workspace_bytes(B, Hq, Hkv, T, N, D, window, sinks))
+    return int(_lib.bpc_chunk_workspace_bytes(B, Hq, Hkv, T, N, D, _slots(window), _slots(sinks)))
 
 
 def chunk_cut(B: int, Hq: int, Hkv: int, T: int, N: int, window: int = 0, sinks: int = 0, D: int = 128):
     """(row_blocks, pieces, streamed) of chunk_attention, as attention_cut."""
     row_blocks, pieces, streamed = _i(), _i(), _i()
-    _check(_lib.bpc_chunk_cut(B, Hq, Hkv, T, N, D, window, sinks, row_blocks, pieces, streamed), "bpc_chunk_cut")
+    _check(_lib.bpc_chunk_cut(B, Hq, Hkv, T, N, D, _slots(window), _slots(sinks), row_blocks, pieces, streamed), "bpc_chunk_cut")
     return row_blocks.value, pieces.value, bool(streamed.value)
 
 
@@ -1136,7 +1141,7 @@ def _window(window: int, sinks: int):
     """Both, as the C entries take them."""
     if window < 0 or sinks < 0:
         raise ValueError(f"window={window} and sinks={sinks} must be >= 0")
-    return min(window, 1 << 30), min(sinks, 1 << 30)
+    return _slots(window), _slots(sinks)
 
 
 def chunk_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, pos: torch.Tensor, sm_scale: Optional[float] = None,
