@@ -702,6 +702,11 @@ int bpc_attention_cut(int B, int Hq, int Hkv, int T, int N, int D, int tree,
  *            workspace are refused where they do.)
  * workspace  at least bpc_chunk_workspace_bytes(...) bytes, as in
  *            bpc_prefill_attention, whose limits hold here too
+ * fp32 scores, statistics and sums.  The probabilities enter the second product as
+ * bf16, and out is divided by the sum of these, so that it is off by a rounding of
+ * them beside its own (random inputs: 0.0017 to 0.0019 relative to the 64-bit result,
+ * the rounding of out alone 0.0017); lse is of the exponentials before they are rounded.
+ * Equal calls give equal bits.
  */
 size_t bpc_chunk_workspace_bytes(int B, int Hq, int Hkv, int T, int N, int D, int window, int sinks);
 int bpc_chunk_attention(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
@@ -770,7 +775,9 @@ int bpc_key_weights(const uint16_t* q, int64_t sq_b, int64_t sq_h, int64_t sq_t,
  *     weights_out[b][h][i] = weights[b][h][s_i] (0 from min(n, keep) on)
  * Sequences then have min(n, keep) slots, in the order of the old ones, and
  * bpc_append_kv_paged and the others go on from there (with positions of the tokens'
- * own as rope_pos).  A sequence whose lens[b] is not in [0, N] is skipped.  Nothing
+ * own as rope_pos).  What they call a slot's place is then its index among those that
+ * are left: a window of bpc_chunk_attention or bpc_key_weights is of that many of them,
+ * and slopes weigh the slots between, not the tokens that once were there.  A sequence whose lens[b] is not in [0, N] is skipped.  Nothing
  * else is written; rows whose page, read or written, is not in its pool are left out.
  *
  * K, V       [B, Hkv, >=N, D], or with block_table pools of pages, as in

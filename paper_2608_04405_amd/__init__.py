@@ -1264,7 +1264,8 @@ def evict_kv(K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, lens: torc
     slots that any sequence may use (default: what the cache or the table, and the
     weights, hold); one whose lens[b] is not in [0, N] is skipped (its slots in the
     result are undefined where that is allocated here).  The sequences' new lengths
-    are lens.clamp(max=keep)."""
+    are lens.clamp(max=keep); windows and slopes of chunk_attention and key_weights
+    count the slots that are left from then on."""
     Kb, Hkv, Kn, (K_b, K_h, K_n) = _cache(K, "K")
     Vb, Vh, Vn, (V_b, V_h, V_n) = _cache(V, "V")
     if type(lens) is not torch.Tensor or lens.dtype is not torch.int32 or lens.dim() != 1 or not lens.is_contiguous():

@@ -17,13 +17,21 @@ static bool pieces_go_round(int64_t pieces) { return pieces % 8 == 0 || pieces >
 // pieces go round the XCDs a quarter of the work is taken to be missing (some are
 // shorter than the longest, where no window makes them alike), and pieces fill up each
 // other's rounds.  The join costs 2.5 and its partial results' way out
-// and back.  Measured (S: pieces of the longest sequence):
-//   2048 tokens of 2 requests over 32768 slots: eight row blocks 1384 us with S = 1,
-//   1473, 1343, 1508 with 2, 3, 4; four 1538, 1814, 1600
-//   1000 tokens of 2 requests over 16384 slots, cap and bias: eight 637, 668, 468, 529
-//   with S = 1 to 4; four 533, 642, 535
-//   257 tokens of 3 requests: one row block 27.5, four 19.7, eight 22.6
-//   one token, window 4096: S = 4, 8, 16, 32: 28.4, 21.1, 17.7, 16.1
+// and back.  Measured (us; S: pieces of the longest sequence; lengths from half of the
+// longest up; * the choice):
+//   2048 tokens of 2 requests over 32768 slots: eight row blocks 1430, 1469, 1371, 1316*,
+//   1326, 1378 with S = 1 to 6, four 1423, 1457, 1412 with S = 1, 2, 4
+//   1000 tokens of 2 requests over 16384 slots, cap and bias: eight 636, 643, 474, 517*, 478,
+//   494, four 456, 540, 462: where the last round ends depends on lengths that are not
+//   known here, and decides more than the model's terms
+//   1000 tokens of 4 requests over 16384 slots: eight 692, 725, 692*, 722, 730, 737, four 725, 668, 665
+//   512 tokens of 4 requests over 8192 slots: eight 229*, 252, 223, 222, 242, 238, four 196, 228, 209
+//   257 tokens of 3 requests: one row block 23.0, four 14.7*, eight 20.5
+//   one token, window 4096: S = 4, 17*: 20.5, 12.9
+// The quarter is a guess about lengths.  Without it the first two calls take S = 1: 1430
+// and 636, 9 and 23 % more.  Requests that are all as long as the longest pay for it: these
+// calls take 2176 and 740 us with S = 4, 2060 and 685 with S = 1; the third 1130 and 1041;
+// the fourth has S = 1 in both.
 AttnPlan chunk_plan(int B, int Hkv, int G, int T, int N, int window, int sinks) {
   AttnPlan p{};
   const int64_t rows = (int64_t)T * G, bh = (int64_t)B * Hkv;
