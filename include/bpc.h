@@ -704,7 +704,7 @@ int bpc_attention_cut(int B, int Hq, int Hkv, int T, int N, int D, int tree,
  *            bpc_prefill_attention, whose limits hold here too
  * fp32 scores, statistics and sums.  The probabilities enter the second product as
  * bf16, and out is divided by the sum of these, so that it is off by a rounding of
- * them beside its own (random inputs: 0.0017 to 0.0019 relative to the 64-bit result,
+ * them beside its own (random inputs: 0.0017 to 0.0020 relative to the 64-bit result,
  * the rounding of out alone 0.0017); lse is of the exponentials before they are rounded.
  * Equal calls give equal bits.
  */
